@@ -426,6 +426,98 @@ int pd_kv_scatter_fp8(pd_ctx *ctx, const void *packed, const int64_t *packed_pag
                       float *kv_scales, const int32_t *page_table, const int32_t *page_begin,
                       const int32_t *page_end, int32_t batch, void *stream);
 
+/* ---- 4-bit KV pages. The paper has no counterpart; the reason is the FP8 pages' (fewer bytes read per concurrent
+ * sequence, Eq. 1), the format is this library's:
+ *   kv4   [num_pages][num_kv_heads][18 * head_dim] bytes, device, 16-byte aligned. A block is 16 rows of head_dim / 2
+ *         bytes of K codes, 16 of V codes, then for every slot and group of 64 values of head_dim four bf16 numbers
+ *         {k_scale, k_min, v_scale, v_min}: 4.5 bits per value. Value 2i of a row is the low nibble of byte i, 2i + 1
+ *         the high one; the row's 16-byte piece c is stored at piece position c ^ ((slot >> 1) & 3) at head_dim 128,
+ *         c ^ ((slot >> 2) & 1) at 64.
+ * A value is scale * code + min, code in [0, 15]. Quantising a group: min = its smallest value (a bf16, stored exactly);
+ * scale = (max - min) / 15 in fp32, rounded UP to bf16; code = (x - min) / scale to the nearest integer, ties to even,
+ * with x - min rounded to fp32. So a value is off by at most scale / 2. Inputs below 2^-126 in magnitude count as 0, a
+ * scale below 2^-100 as 0 (every code 0). A group that holds a NaN or infinity, or whose max - min leaves fp32, gets the
+ * scale NaN: all of it reads back as NaN. A token's row never touches another token's bytes, so slots can be written
+ * in any order. head_dim 64 or 128. Calls of one context share its workspace: enqueue them on one stream or order
+ * them with events. None of them allocates or synchronises, so all can be captured in CUDA graphs after one eager call.
+ */
+
+/*
+ * Append of one token per sequence (pd_kv_append_q4: k_new / v_new [batch][num_kv_heads][head_dim]) and of packed new
+ * tokens (pd_kv_append_tokens_q4: rows as in pd_kv_append_tokens), quantised as they are written. Positions, skipping and error reporting as
+ * pd_kv_append and pd_kv_append_tokens. PD_APPEND_NO_ADVANCE leaves ctx_lens as it is, for the layers of a model that
+ * share one length array.
+ */
+int pd_kv_append_q4(pd_ctx *ctx, const void *k_new, const void *v_new, void *kv4, const int32_t *page_table,
+                    int32_t *ctx_lens, int32_t batch, uint32_t call_flags, void *stream);
+int pd_kv_append_tokens_q4(pd_ctx *ctx, const void *k_new, const void *v_new, const int32_t *q_indptr, void *kv4,
+                           const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
+                           uint32_t call_flags, void *stream);
+
+/*
+ * Reads a 4-bit cache back: tokens [first_token[b], ctx_lens[b]) of every sequence (first_token NULL = from 0) go to the
+ * same slots of bf16 pools k_pages / v_pages of num_pages pages, at the physical pages of dst_page_table
+ * ([batch][max_pages_per_seq], may be page_table). A value is fma(scale, code, min) in fp32, rounded once to bf16. Other slots of
+ * the destination keep what they hold. With this an append-prefill (pd_prefill_attn) can run over a prefix that is
+ * held in 4 bits. A page id outside [0, num_pages) in either table skips that page, a negative first_token or a length past
+ * the table skips the sequence; both are latched for pd_device_status.
+ */
+int pd_kv_dequantize_q4(pd_ctx *ctx, const void *kv4, const int32_t *page_table, const int32_t *first_token,
+                        const int32_t *ctx_lens, void *k_pages, void *v_pages, const int32_t *dst_page_table, int32_t batch,
+                        void *stream);
+
+/*
+ * pd_decode_attn over 4-bit pages: same outputs, plan, split_pages meaning, error behaviour and bit-reproducibility.
+ * K and V are scale * code + min unrounded. q must be finite and below 2^100; the products run in fp16 with fp32
+ * accumulation, q scaled per head to fp16's range.
+ * pd_decode_step_q4: pd_kv_append_q4 (advancing) followed by pd_decode_attn_q4, enqueued by one call after every
+ * argument is validated; ctx_lens holds the lengths BEFORE the append on entry.
+ */
+int pd_decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *page_table, const int32_t *ctx_lens,
+                      void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream);
+int pd_decode_step_q4(pd_ctx *ctx, const void *q, const void *k_new, const void *v_new, void *kv4, const int32_t *page_table,
+                      int32_t *ctx_lens, void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream);
+
+/* ---- Rotary positions with one to four axes (text; time, height, width of images and video). The rotation that
+ * queries and keys get before attention; the paper has no counterpart.
+ *
+ * The first rot_dim values of a head form rot_dim / 2 pairs: (i, i + rot_dim / 2), or (2i, 2i + 1) with `adjacent`.
+ * Pair i turns by position[axis_of_pair[i]] * inv_freq[i] radians: (a, b) -> magnitude * (a cos - b sin, a sin + b cos).
+ * Values past rot_dim are copied. The angle is exact to 2^-32 turns at every int32 position; sums are fp32, results are
+ * rounded once to bf16. The structure lies in HOST memory and is read during the call. */
+typedef struct pd_rope_config {
+    int32_t rot_dim;          /* multiple of 16, 16 .. head_dim                                          */
+    int32_t num_axes;         /* 1 .. 4                                                                   */
+    int32_t adjacent;         /* 0: pairs (i, i + rot_dim / 2); 1: pairs (2i, 2i + 1)                     */
+    float magnitude;          /* factor on cosine and sine; 1 for a pure rotation                         */
+    uint8_t axis_of_pair[64]; /* < num_axes, for i < rot_dim / 2                                          */
+    float inv_freq[64];       /* radians per position, magnitude below 402 (64 turns), i < rot_dim / 2    */
+} pd_rope_config;
+
+/*
+ * positions: int32 DEVICE array [num_axes][position_stride]; entry [axis][row] belongs to packed row `row`.
+ *
+ * pd_rope_tokens rotates rows [0, total) of q ([total][num_q_heads][head_dim] bf16) into q_out and of k
+ * ([total][num_kv_heads][head_dim]) into k_out. q_out may be q and k_out may be k (other overlaps are not allowed).
+ *
+ * pd_rope_append_tokens / _q4 rotate the packed new tokens' q into q_out (may be q) and append the rotated k_new and v_new as they
+ * are to bf16 pools or, quantised, to 4-bit pages, in one pass: pools, lengths and q_out are bit for bit those of
+ * pd_rope_tokens followed by pd_kv_append_tokens / pd_kv_append_tokens_q4 (rotated keys are rounded to bf16 before they are
+ * quantised). positions NULL: every axis stands at the token's index in its sequence, ctx_lens[b] + i. A sequence whose append is
+ * skipped still gets its q_out. One token per sequence is q_indptr = 0, 1, 2, ... with max_q_len 1.
+ * PD_ERR_UNSUPPORTED: rot_dim not a multiple of 16; for _q4 also num_kv_heads * head_dim above 20480.
+ */
+int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,
+                   const void *k, void *q_out, void *k_out, int32_t total, void *stream);
+int pd_rope_append_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                          const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out,
+                          void *k_pages, void *v_pages, const int32_t *page_table, int32_t *ctx_lens, int32_t batch,
+                          int32_t max_q_len, uint32_t call_flags, void *stream);
+int pd_rope_append_tokens_q4(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                             const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out,
+                             void *kv4, const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
+                             uint32_t call_flags, void *stream);
+
 /* ---- Elastic KV pool on CUDA virtual memory management (Sec. 4.6: the intra-scale toggle keeps the
  * rollout process and swaps device state; Sec. 5: the KV cache is released when training begins and
  * restored when the GPU is available again). A pool is a device address range of `capacity` bytes whose

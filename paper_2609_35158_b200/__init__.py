@@ -31,6 +31,8 @@ EXPORTS = (
     "pd_makespan_coloc", "pd_makespan_disagg", "pd_feasible_disagg", "pd_decide", "pd_min_change_plan", "pd_toggle_gate",
     "pd_fit_decode_cost", "pd_plan_ranges", "pd_plan_walk",
     "pd_kv_quantize_pages", "pd_kv_append_fp8", "pd_decode_attn_fp8", "pd_decode_step_fp8", "pd_kv_gather_fp8", "pd_kv_scatter_fp8",
+    "pd_kv_append_q4", "pd_kv_append_tokens_q4", "pd_kv_dequantize_q4", "pd_decode_attn_q4", "pd_decode_step_q4",
+    "pd_rope_tokens", "pd_rope_append_tokens", "pd_rope_append_tokens_q4",
     "pd_pool_create", "pd_pool_resize", "pd_pool_base", "pd_pool_capacity", "pd_pool_chunk_bytes", "pd_pool_resident_bytes",
     "pd_pool_last_error", "pd_pool_destroy",
     "pd_set_profile_events", "pd_read_probe", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
@@ -54,6 +56,11 @@ class pd_cost_model(ctypes.Structure):
 class pd_target(ctypes.Structure):
     _fields_ = [("N_P", ctypes.c_int32), ("N_D", ctypes.c_int32), ("N_C", ctypes.c_int32),
                 ("makespan", ctypes.c_double)]
+
+
+class pd_rope_config(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("num_axes", ctypes.c_int32), ("adjacent", ctypes.c_int32),
+                ("magnitude", ctypes.c_float), ("axis_of_pair", ctypes.c_uint8 * 64), ("inv_freq", ctypes.c_float * 64)]
 
 
 class PdError(RuntimeError):
@@ -115,6 +122,15 @@ def _load() -> ctypes.CDLL:
     lib.pd_decode_step_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp]
     lib.pd_kv_gather_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.pd_kv_scatter_fp8.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+    pr = ctypes.POINTER(pd_rope_config)
+    lib.pd_kv_append_q4.argtypes = [vp, vp, vp, vp, vp, vp, i32, u32, vp]
+    lib.pd_kv_append_tokens_q4.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
+    lib.pd_kv_dequantize_q4.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+    lib.pd_decode_attn_q4.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp]
+    lib.pd_decode_step_q4.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp]
+    lib.pd_rope_tokens.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, i32, vp]
+    lib.pd_rope_append_tokens.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
+    lib.pd_rope_append_tokens_q4.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
     u64 = ctypes.c_uint64
     lib.pd_pool_create.argtypes = [i32, u64, u64, ctypes.POINTER(vp)]
     lib.pd_pool_resize.argtypes = [vp, u64, vp]
@@ -293,6 +309,89 @@ def pd_kv_scatter_fp8(ctx, packed, packed_page_offset, k8, v8, kv_scales, page_t
     _check(_lib.pd_kv_scatter_fp8(ctx, _ptr(packed), _ptr(packed_page_offset), _ptr(k8), _ptr(v8), _ptr(kv_scales),
                                   _ptr(page_table), _ptr(page_begin), _ptr(page_end), batch, _stream(stream)),
            "pd_kv_scatter_fp8", ctx)
+
+
+def pd_kv_append_q4(ctx, k_new, v_new, kv4, page_table, ctx_lens, batch=None, call_flags=0, stream=None):
+    batch = k_new.shape[0] if batch is None else batch
+    _check(_lib.pd_kv_append_q4(ctx, _ptr(k_new), _ptr(v_new), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens), batch, call_flags,
+                                _stream(stream)), "pd_kv_append_q4", ctx)
+
+
+def pd_kv_append_tokens_q4(ctx, k_new, v_new, q_indptr, kv4, page_table, ctx_lens, max_q_len, batch=None, call_flags=0,
+                           stream=None):
+    batch = q_indptr.shape[0] - 1 if batch is None else batch
+    _check(_lib.pd_kv_append_tokens_q4(ctx, _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(kv4), _ptr(page_table),
+                                       _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
+           "pd_kv_append_tokens_q4", ctx)
+
+
+def pd_kv_dequantize_q4(ctx, kv4, page_table, first_token, ctx_lens, k_pages, v_pages, dst_page_table, batch=None, stream=None):
+    """``first_token`` may be None (every sequence from its first token)."""
+    batch = ctx_lens.shape[0] if batch is None else batch
+    _check(_lib.pd_kv_dequantize_q4(ctx, _ptr(kv4), _ptr(page_table), _ptr(first_token), _ptr(ctx_lens), _ptr(k_pages),
+                                    _ptr(v_pages), _ptr(dst_page_table), batch, _stream(stream)), "pd_kv_dequantize_q4", ctx)
+
+
+def pd_decode_attn_q4(ctx, q, kv4, page_table, ctx_lens, out, lse=None, batch=None, sm_scale=1.0, split_pages=0, stream=None):
+    batch = q.shape[0] if batch is None else batch
+    _check(_lib.pd_decode_attn_q4(ctx, _ptr(q), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens), _ptr(out), _ptr(lse), batch,
+                                  sm_scale, split_pages, _stream(stream)), "pd_decode_attn_q4", ctx)
+
+
+def pd_decode_step_q4(ctx, q, k_new, v_new, kv4, page_table, ctx_lens, out, lse=None, batch=None, sm_scale=1.0, split_pages=0,
+                      stream=None):
+    batch = q.shape[0] if batch is None else batch
+    _check(_lib.pd_decode_step_q4(ctx, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens),
+                                  _ptr(out), _ptr(lse), batch, sm_scale, split_pages, _stream(stream)),
+           "pd_decode_step_q4", ctx)
+
+
+def rope_config(rot_dim: int, inv_freq, axis_of_pair=None, num_axes: int = 1, adjacent: bool = False,
+                magnitude: float = 1.0) -> pd_rope_config:
+    """A ``pd_rope_config`` from host sequences of rot_dim / 2 frequencies and (default: all 0) axis numbers."""
+    half = rot_dim // 2
+    inv_freq = [float(f) for f in inv_freq]
+    axis = [0] * half if axis_of_pair is None else [int(a) for a in axis_of_pair]
+    if not 0 < half <= 64 or len(inv_freq) != half or len(axis) != half or any(not 0 <= a < 256 for a in axis):
+        raise ValueError("rope_config: rot_dim / 2 (at most 64) frequencies and axis numbers are needed")
+    c = pd_rope_config(rot_dim, num_axes, int(adjacent), magnitude)
+    c.axis_of_pair[:half] = axis
+    c.inv_freq[:half] = inv_freq
+    return c
+
+
+def _position_stride(positions, rope) -> int:
+    if positions is None:
+        return 0
+    if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() < rope.num_axes * positions.shape[-1]:
+        raise ValueError("positions: a contiguous int32 tensor [num_axes, rows] (or [rows] for one axis)")
+    return positions.shape[-1]
+
+
+def pd_rope_tokens(ctx, rope, positions, q, k, q_out, k_out, total=None, stream=None):
+    """``positions``: int32 [num_axes, rows] (or [rows] for one axis), contiguous."""
+    total = q.shape[0] if total is None else total
+    _check(_lib.pd_rope_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q), _ptr(k),
+                               _ptr(q_out), _ptr(k_out), total, _stream(stream)), "pd_rope_tokens", ctx)
+
+
+def pd_rope_append_tokens(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out, k_pages, v_pages, page_table, ctx_lens,
+                          max_q_len, batch=None, call_flags=0, stream=None):
+    """``positions`` may be None: every axis stands at the token's index in its sequence."""
+    batch = q_indptr.shape[0] - 1 if batch is None else batch
+    _check(_lib.pd_rope_append_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
+                                      _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
+                                      _ptr(page_table), _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
+           "pd_rope_append_tokens", ctx)
+
+
+def pd_rope_append_tokens_q4(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out, kv4, page_table, ctx_lens, max_q_len,
+                             batch=None, call_flags=0, stream=None):
+    batch = q_indptr.shape[0] - 1 if batch is None else batch
+    _check(_lib.pd_rope_append_tokens_q4(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
+                                         _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(kv4), _ptr(page_table),
+                                         _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
+           "pd_rope_append_tokens_q4", ctx)
 
 
 def pd_pool_create(device: int, capacity_bytes: int, chunk_bytes: int = 0):

@@ -78,6 +78,7 @@ struct pd_ctx {
     cudaEvent_t ev_before = nullptr, ev_after = nullptr;  // optional timing hook around the split kernel
     bool prefill_ready = false;
     bool fp8_ready = false;
+    bool q4_ready = false;
     int64_t launches = 0;
     char last_error[256] = {0};
 };
@@ -662,6 +663,291 @@ int pd_decode_step_fp8(pd_ctx *ctx, const void *q, const void *k_new, const void
     if (int rc = fp8_attn_check_args(ctx, q, k8, v8, kv_scales, page_table, ctx_lens, out, batch, sm_scale, split_pages)) return rc;
     if (int rc = pd_kv_append_fp8(ctx, k_new, v_new, k8, v8, kv_scales, page_table, ctx_lens, batch, 0u, stream)) return rc;
     return decode_attn_fp8_impl(ctx, q, k8, v8, kv_scales, page_table, ctx_lens, out, lse, batch, sm_scale, split_pages, stream);
+}
+
+}  // extern "C"
+
+namespace {
+
+int q4_attn_check_args(pd_ctx *ctx, const char *who, const void *q, const void *kv4, const int32_t *page_table,
+                       const int32_t *ctx_lens, const void *out, int32_t batch, float sm_scale, int32_t split_pages) {
+    if (int rc = check_batch(ctx, batch)) return rc;
+    if (!aligned16(q) || !aligned16(kv4) || !aligned16(out) || page_table == nullptr || ctx_lens == nullptr) {
+        char msg[96];
+        std::snprintf(msg, sizeof msg, "%s: null or misaligned pointer", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
+    if (!(sm_scale > 0.f) || !(sm_scale < 3.0e38f)) return fail(ctx, PD_ERR_INVALID_ARG, "sm_scale must be finite and positive");
+    if (split_pages < 0) return fail(ctx, PD_ERR_INVALID_ARG, "split_pages must be >= 0");
+    return PD_OK;
+}
+
+int append_q4(pd_ctx *ctx, const char *who, const void *k_new, const void *v_new, const int32_t *q_indptr, void *kv4,
+              const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len, uint32_t call_flags, void *stream) {
+    if (int rc = check_batch(ctx, batch)) return rc;
+    char msg[96];
+    if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(kv4) || page_table == nullptr || ctx_lens == nullptr) {
+        std::snprintf(msg, sizeof msg, "%s: null or misaligned pointer", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
+    if (call_flags & ~PD_APPEND_NO_ADVANCE) {
+        std::snprintf(msg, sizeof msg, "%s: unknown call flag", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
+    if (max_q_len < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len must be >= 0");
+    if (batch == 0 || max_q_len == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    pd::AppendQ4Params p{};
+    p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
+    p.q_indptr = q_indptr;
+    p.kv4 = static_cast<uint8_t *>(kv4);
+    p.page_table = page_table;
+    p.ctx_lens = ctx_lens;
+    p.status = ctx->status;
+    p.B = batch;
+    p.Hkv = ctx->cfg.num_kv_heads;
+    p.D = ctx->cfg.head_dim;
+    p.MP = ctx->cfg.max_pages_per_seq;
+    p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.advance = (call_flags & PD_APPEND_NO_ADVANCE) ? 0 : 1;
+    p.pdl = ctx->pdl;
+    int launched = 0;
+    const cudaError_t err = pd::launch_kv_append_q4(p, max_q_len, ctx->num_sms, &launched, static_cast<cudaStream_t>(stream));
+    ctx->launches += launched;
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "kv_append_q4 launch", err);
+    return PD_OK;
+}
+
+int decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *page_table, const int32_t *ctx_lens, void *out,
+                   float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream) {
+    if (batch == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    if (!ctx->q4_ready) {
+        const cudaError_t e = pd::prepare_decode_attn_q4(ctx->cfg.head_dim);
+        if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "4-bit decode kernel attribute", e);
+        ctx->q4_ready = true;
+    }
+    pd::AttnParams p{};
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.kv4 = static_cast<const uint8_t *>(kv4);
+    p.page_table = page_table;
+    p.ctx_lens = ctx_lens;
+    p.out = static_cast<__nv_bfloat16 *>(out);
+    p.lse = lse;
+    p.part_o = ctx->part_o;
+    p.part_ml = ctx->part_ml;
+    p.cum_pages = ctx->cum_pages;
+    p.plan = ctx->plan;
+    p.status = ctx->status;
+    p.B = batch;
+    p.Hq = ctx->cfg.num_q_heads;
+    p.Hkv = ctx->cfg.num_kv_heads;
+    p.G = ctx->group;
+    p.MP = ctx->cfg.max_pages_per_seq;
+    p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.scale_log2 = sm_scale * 1.4426950408889634f;
+    p.split_pages = split_pages;
+    p.max_ranges = ctx->max_ranges;
+    p.min_pages_auto = ctx->min_pages_auto;
+    p.halving_levels = ctx->halving_levels;
+    p.tail_pages = ctx->tail_pages;
+    p.static_fair_max = kFp8StaticFairMax;
+    const bool hooked = ctx->ev_before != nullptr;
+    p.pdl = hooked ? 0 : ctx->pdl;
+    p.merge_rows = ctx->merge_rows;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (hooked) cudaEventRecord(ctx->ev_before, s);
+    cudaError_t err = pd::launch_decode_attn_q4(ctx->cfg.head_dim, p, ctx->num_ctas, s);
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "decode_attn_split_q4 launch", err);
+    if (hooked) {
+        cudaEventRecord(ctx->ev_after, s);
+        ctx->ev_before = nullptr;
+        ctx->ev_after = nullptr;
+    }
+    err = pd::launch_lse_merge(ctx->cfg.head_dim, p, s);
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "lse_merge launch", err);
+    ctx->launches += 2;
+    return PD_OK;
+}
+
+// Checks a rotation and lays it out for the kernels.
+int rope_params(pd_ctx *ctx, const pd_rope_config *rope, pd::RopeParams *p) {
+    if (rope == nullptr) return fail(ctx, PD_ERR_INVALID_ARG, "rope: null configuration");
+    if (rope->rot_dim < 16 || rope->rot_dim > ctx->cfg.head_dim || rope->num_axes < 1 || rope->num_axes > 4 ||
+        (rope->adjacent != 0 && rope->adjacent != 1) || !(rope->magnitude > -3.0e38f && rope->magnitude < 3.0e38f))
+        return fail(ctx, PD_ERR_INVALID_ARG, "rope: rot_dim, num_axes, adjacent or magnitude out of range");
+    if (rope->rot_dim % 16 != 0) return fail(ctx, PD_ERR_UNSUPPORTED, "rope: rot_dim must be a multiple of 16");
+    for (int i = 0; i < rope->rot_dim / 2; ++i) {
+        const double turns = static_cast<double>(rope->inv_freq[i]) * 0.15915494309189533577;  // 1 / (2 pi)
+        if (rope->axis_of_pair[i] >= rope->num_axes || !(turns > -64.0 && turns < 64.0))
+            return fail(ctx, PD_ERR_INVALID_ARG, "rope: axis or frequency of a pair out of range");
+        // two's complement carries the sign, and whole turns fall off the top; split in two so that the cast is exact
+        double frac = turns < 0.0 ? -turns : turns;
+        frac -= static_cast<double>(static_cast<int>(frac));
+        const uint64_t fixed = static_cast<uint64_t>(frac * 18446744073709551616.0);
+        p->freq[i] = turns < 0.0 ? 0ull - fixed : fixed;
+        p->axis_of_pair[i] = rope->axis_of_pair[i];
+    }
+    p->magnitude = rope->magnitude;
+    p->rot_dim = rope->rot_dim;
+    p->adjacent = rope->adjacent;
+    p->status = ctx->status;
+    p->Hq = ctx->cfg.num_q_heads;
+    p->Hkv = ctx->cfg.num_kv_heads;
+    p->D = ctx->cfg.head_dim;
+    p->MP = ctx->cfg.max_pages_per_seq;
+    p->num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p->pdl = ctx->pdl;
+    return PD_OK;
+}
+
+int rope_append(pd_ctx *ctx, const char *who, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out, void *k_pages,
+                void *v_pages, void *kv4, const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
+                uint32_t call_flags, void *stream) {
+    if (int rc = check_batch(ctx, batch)) return rc;
+    char msg[96];
+    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || q_indptr == nullptr ||
+        page_table == nullptr || ctx_lens == nullptr || (kv4 != nullptr ? !aligned16(kv4) : !aligned16(k_pages) || !aligned16(v_pages))) {
+        std::snprintf(msg, sizeof msg, "%s: null or misaligned pointer", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
+    if (call_flags & ~PD_APPEND_NO_ADVANCE) {
+        std::snprintf(msg, sizeof msg, "%s: unknown call flag", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
+    if (max_q_len < 0 || position_stride < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len and position_stride must be >= 0");
+    pd::RopeParams p{};
+    if (int rc = rope_params(ctx, rope, &p)) return rc;
+    if (kv4 != nullptr && ctx->cfg.num_kv_heads * ctx->cfg.head_dim > 20480)
+        return fail(ctx, PD_ERR_UNSUPPORTED, "pd_rope_append_tokens_q4: num_kv_heads * head_dim above 20480");
+    if (batch == 0 || max_q_len == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    p.positions = positions;
+    p.position_stride = position_stride;
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.k_new = static_cast<const __nv_bfloat16 *>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16 *>(v_new);
+    p.q_out = static_cast<__nv_bfloat16 *>(q_out);
+    p.q_indptr = q_indptr;
+    p.k_pages = static_cast<__nv_bfloat16 *>(k_pages);
+    p.v_pages = static_cast<__nv_bfloat16 *>(v_pages);
+    p.kv4 = static_cast<uint8_t *>(kv4);
+    p.page_table = page_table;
+    p.ctx_lens = ctx_lens;
+    p.B = batch;
+    p.advance = (call_flags & PD_APPEND_NO_ADVANCE) ? 0 : 1;
+    int launched = 0;
+    const cudaError_t err = pd::launch_rope(p, kv4 != nullptr ? 2 : 1, max_q_len, ctx->num_sms, &launched, static_cast<cudaStream_t>(stream));
+    ctx->launches += launched;
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "rope append launch", err);
+    return PD_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int pd_kv_append_q4(pd_ctx *ctx, const void *k_new, const void *v_new, void *kv4, const int32_t *page_table,
+                    int32_t *ctx_lens, int32_t batch, uint32_t call_flags, void *stream) {
+    return append_q4(ctx, "pd_kv_append_q4", k_new, v_new, nullptr, kv4, page_table, ctx_lens, batch, 1, call_flags, stream);
+}
+
+int pd_kv_append_tokens_q4(pd_ctx *ctx, const void *k_new, const void *v_new, const int32_t *q_indptr, void *kv4,
+                           const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
+                           uint32_t call_flags, void *stream) {
+    if (ctx != nullptr && q_indptr == nullptr) return fail(ctx, PD_ERR_INVALID_ARG, "pd_kv_append_tokens_q4: null q_indptr");
+    return append_q4(ctx, "pd_kv_append_tokens_q4", k_new, v_new, q_indptr, kv4, page_table, ctx_lens, batch, max_q_len, call_flags, stream);
+}
+
+int pd_kv_dequantize_q4(pd_ctx *ctx, const void *kv4, const int32_t *page_table, const int32_t *first_token,
+                        const int32_t *ctx_lens, void *k_pages, void *v_pages, const int32_t *dst_page_table, int32_t batch,
+                        void *stream) {
+    if (int rc = check_batch(ctx, batch)) return rc;
+    if (!aligned16(kv4) || !aligned16(k_pages) || !aligned16(v_pages) || page_table == nullptr || ctx_lens == nullptr ||
+        dst_page_table == nullptr)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_kv_dequantize_q4: null or misaligned pointer");
+    if (batch == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    pd::DequantizeQ4Params p{};
+    p.kv4 = static_cast<const uint8_t *>(kv4);
+    p.page_table = page_table;
+    p.dst_page_table = dst_page_table;
+    p.first_token = first_token;
+    p.ctx_lens = ctx_lens;
+    p.k_pages = static_cast<__nv_bfloat16 *>(k_pages);
+    p.v_pages = static_cast<__nv_bfloat16 *>(v_pages);
+    p.status = ctx->status;
+    p.B = batch;
+    p.Hkv = ctx->cfg.num_kv_heads;
+    p.D = ctx->cfg.head_dim;
+    p.MP = ctx->cfg.max_pages_per_seq;
+    p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.pdl = ctx->pdl;
+    const cudaError_t err = pd::launch_kv_dequantize_q4(p, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "kv_dequantize_q4 launch", err);
+    ctx->launches += 1;
+    return PD_OK;
+}
+
+int pd_decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *page_table, const int32_t *ctx_lens,
+                      void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream) {
+    if (int rc = q4_attn_check_args(ctx, "pd_decode_attn_q4", q, kv4, page_table, ctx_lens, out, batch, sm_scale, split_pages)) return rc;
+    return decode_attn_q4(ctx, q, kv4, page_table, ctx_lens, out, lse, batch, sm_scale, split_pages, stream);
+}
+
+int pd_decode_step_q4(pd_ctx *ctx, const void *q, const void *k_new, const void *v_new, void *kv4, const int32_t *page_table,
+                      int32_t *ctx_lens, void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream) {
+    if (int rc = q4_attn_check_args(ctx, "pd_decode_step_q4", q, kv4, page_table, ctx_lens, out, batch, sm_scale, split_pages)) return rc;
+    if (int rc = append_q4(ctx, "pd_decode_step_q4", k_new, v_new, nullptr, kv4, page_table, ctx_lens, batch, 1, 0u, stream)) return rc;
+    return decode_attn_q4(ctx, q, kv4, page_table, ctx_lens, out, lse, batch, sm_scale, split_pages, stream);
+}
+
+int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,
+                   const void *k, void *q_out, void *k_out, int32_t total, void *stream) {
+    if (ctx == nullptr) return PD_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || positions == nullptr)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_tokens: null or misaligned pointer");
+    if (total < 0 || position_stride < total) return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_tokens: negative total, or position_stride below it");
+    pd::RopeParams p{};
+    if (int rc = rope_params(ctx, rope, &p)) return rc;
+    if (total == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    p.positions = positions;
+    p.position_stride = position_stride;
+    p.q = static_cast<const __nv_bfloat16 *>(q);
+    p.k_new = static_cast<const __nv_bfloat16 *>(k);
+    p.q_out = static_cast<__nv_bfloat16 *>(q_out);
+    p.k_out = static_cast<__nv_bfloat16 *>(k_out);
+    p.total = total;
+    int launched = 0;
+    const cudaError_t err = pd::launch_rope(p, 0, total, ctx->num_sms, &launched, static_cast<cudaStream_t>(stream));
+    ctx->launches += launched;
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "rope launch", err);
+    return PD_OK;
+}
+
+int pd_rope_append_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                          const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out,
+                          void *k_pages, void *v_pages, const int32_t *page_table, int32_t *ctx_lens, int32_t batch,
+                          int32_t max_q_len, uint32_t call_flags, void *stream) {
+    return rope_append(ctx, "pd_rope_append_tokens", rope, positions, position_stride, q, k_new, v_new, q_indptr, q_out, k_pages,
+                       v_pages, nullptr, page_table, ctx_lens, batch, max_q_len, call_flags, stream);
+}
+
+int pd_rope_append_tokens_q4(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                             const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out,
+                             void *kv4, const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
+                             uint32_t call_flags, void *stream) {
+    if (ctx != nullptr && kv4 == nullptr) return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_append_tokens_q4: null kv4");
+    return rope_append(ctx, "pd_rope_append_tokens_q4", rope, positions, position_stride, q, k_new, v_new, q_indptr, q_out, nullptr,
+                       nullptr, kv4, page_table, ctx_lens, batch, max_q_len, call_flags, stream);
 }
 
 int pd_kv_append_tokens(pd_ctx *ctx, const void *k_new, const void *v_new, const int32_t *q_indptr, void *k_pages,

@@ -57,6 +57,7 @@ struct AttnParams {
     int32_t fused;
     // FP8 pages (null for bf16 pools): {k_scale, v_scale, 0, 0} fp32 per (page, KV head)
     const float *kv_scales;
+    const uint8_t *kv4;         // 4-bit pages (null otherwise): [num_pages][Hkv][18 D] bytes
     int32_t merge_rows;         // rows per CTA of the merge kernel, 0 = chosen from the row count
     // Host-visible result (null / 0 otherwise): the merge kernel delivers every final row to out_host, the
     // device alias of a pinned host buffer [B][Hq][D] (rows the split kernel wrote to `out` are forwarded), and
@@ -147,6 +148,47 @@ struct AppendFp8Params {
     int32_t B, Hkv, D, MP, num_pages, advance, pdl;
 };
 
+// Packed new tokens into 4-bit pages; q_indptr = null: one token per sequence.
+struct AppendQ4Params {
+    const __nv_bfloat16 *k_new, *v_new;  // [total][Hkv][D]
+    const int32_t *q_indptr;             // [B+1] or null
+    uint8_t *kv4;
+    const int32_t *page_table;
+    int32_t *ctx_lens;
+    int32_t *status;
+    int32_t B, Hkv, D, MP, num_pages, advance, pdl;
+};
+
+// Tokens [first_token[b], ctx_lens[b]) of 4-bit pages into bf16 pages.
+struct DequantizeQ4Params {
+    const uint8_t *kv4;
+    const int32_t *page_table, *dst_page_table;  // [B][MP] each
+    const int32_t *first_token;                  // [B] or null (0)
+    const int32_t *ctx_lens;
+    __nv_bfloat16 *k_pages, *v_pages;
+    int32_t *status;
+    int32_t B, Hkv, D, MP, num_pages, pdl;
+};
+
+// Rotary positions, alone (total tokens, k_out) or with the append of packed new tokens to bf16 or 4-bit pages.
+struct RopeParams {
+    unsigned long long freq[64];   // turns per position, 64-bit fixed point
+    uint8_t axis_of_pair[64];
+    float magnitude;
+    int32_t rot_dim, adjacent;
+    const int32_t *positions;      // [axes][position_stride] or null: the token's index in its sequence
+    long long position_stride;
+    const __nv_bfloat16 *q, *k_new, *v_new;
+    __nv_bfloat16 *q_out, *k_out;
+    const int32_t *q_indptr;
+    __nv_bfloat16 *k_pages, *v_pages;
+    uint8_t *kv4;
+    const int32_t *page_table;
+    int32_t *ctx_lens;
+    int32_t *status;
+    int32_t B, Hq, Hkv, D, MP, num_pages, total, advance, tile, pdl;
+};
+
 struct AttnVariant {
     int head_dim, warps, stages, hilo;
 };
@@ -186,6 +228,15 @@ cudaError_t prepare_prefill_attn(int head_dim);  // opt-in shared memory, once
 cudaError_t launch_prefill_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const PrefillParams &p,
                                 int max_q_len, cudaStream_t stream);
 cudaError_t launch_kv_append_tokens(const AppendTokensParams &p, int max_q_len, cudaStream_t stream);
+// ctx_lens[b] += q_indptr[b + 1] - q_indptr[b] where the table row has room (the second half of a multi-token append)
+cudaError_t launch_advance_lens(const AppendTokensParams &p, cudaStream_t stream);
+// 4-bit pages; the split kernel writes the same partials and plan, so launch_lse_merge follows it
+cudaError_t prepare_decode_attn_q4(int head_dim);
+cudaError_t launch_decode_attn_q4(int head_dim, const AttnParams &p, int num_ctas, cudaStream_t stream);
+cudaError_t launch_kv_append_q4(const AppendQ4Params &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
+cudaError_t launch_kv_dequantize_q4(const DequantizeQ4Params &p, int num_sms, cudaStream_t stream);
+// *launched: kernels enqueued. append: 0 = rotate only, 1 = into bf16 pages, 2 = into 4-bit pages
+cudaError_t launch_rope(const RopeParams &p, int append, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_transfer(const TransferParams &p, bool scatter, int num_sms, cudaStream_t stream);
 
 }  // namespace pd

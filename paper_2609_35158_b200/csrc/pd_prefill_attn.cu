@@ -525,6 +525,10 @@ cudaError_t launch_kv_append_tokens(const AppendTokensParams &p, int max_q_len, 
     const dim3 grid(max_q_len < 64 ? max_q_len : 64, p.B);
     cudaError_t err = launch_pdl(kv_append_tokens_kernel, grid, dim3(256), 0, stream, p.pdl != 0, p);
     if (err != cudaSuccess) return err;
+    return launch_advance_lens(p, stream);
+}
+
+cudaError_t launch_advance_lens(const AppendTokensParams &p, cudaStream_t stream) {
     return launch_pdl(advance_lens_kernel, dim3((p.B + 127) / 128), dim3(128), 0, stream, p.pdl != 0, p);
 }
 
