@@ -3,20 +3,27 @@
 // With K_t = sk_t k_t + mk_t and V_t = sv_t v_t + mv_t (codes k, v in 0..15, one scale and minimum per token and group
 // of 64 values) the two products fall apart into products of codes and rank-one terms:
 //   S_t = sum_groups sk_t (q . k_t) + mk_t sum(q)          O = sum_t (p_t sv_t) v_t + sum_t p_t mv_t
-// so the codes go to the tensor core as they are and scales and minima stay in fp32 registers.
+// so the codes go to the tensor core as they are and scales and minima stay beside them.
 //
-// Same plan of ranges, worker warps, partial format and merge kernel as the other split kernels. What differs:
-//   * a (page, KV head) block is one piece of 18 D bytes: one untiled bulk copy on one barrier per stage;
+// Same plan of ranges, partial format and merge kernel as the other split kernels. What differs:
+//   * a (page, KV head) block is one piece of 18 D bytes: one untiled bulk copy per page. A tile is TP pages of one
+//     segment on one barrier, issued by TP lanes of the worker that will read it. (One producer warp for the CTA, lane i
+//     for worker i, measured 145 against XXX us on 64 contexts of 2K-16K: copies of different lanes are issued one after
+//     the other, about 120 cycles each, and a stage waited 5200 cycles for its turn.);
 //   * codes become fp16 without a conversion: a nibble in the low bits of a 16-bit half IS the fp16 subnormal
-//     code * 2^-24, exactly, and mma.sync takes subnormals. So (w & 0x000f000f) is an operand register, and so are
-//     (w & 0x00f000f0), 16 times larger, and the two of w >> 8: five integer instructions for eight values. The factor
-//     16 is taken out of Q beforehand for K, and out of the output rows at the end for V;
+//     code * 2^-24, exactly, and mma.sync takes subnormals. For K, (w & 0x000f000f) is an operand register, and so are
+//     (w & 0x00f000f0), 16 times larger, and the two of w >> 8; the factor 16 is taken out of Q beforehand. For V, bytes
+//     are operands as well (two codes u + 16 v below 1024 are still a subnormal) and v's row of O is recovered at the
+//     end as (O_byte - O_u) / 16, which saves the shift;
 //   * Q is scaled per head by a power of two so that its largest value lies in [2^14, 2^15): fp16 then holds every
 //     bf16 q down to 2^-24 of the largest exactly, whatever q's magnitude;
-//   * P * sv goes to the tensor core in fp16 relative to a per-head power of two `f` that keeps the largest weight of
-//     the segment between 2^2 and 2^15: weights below 2^-16 of the largest start to lose bits, which is under 2^-27 of
-//     the largest for each. Tracking the product and not sv alone keeps a token of huge scale and vanishing
-//     probability from pushing the others out of range.
+//   * mk_t sum(q) is one bf16 mma: mk is a bf16, sum(q) the sum of three. Its accumulator starts at -r, r being the
+//     reference of the exponentials, so exp2 takes what the products leave;
+//   * r is chosen per head so that the largest weight p_t sv_t of the segment lies in [2^2, 2^15]: the weights go to the
+//     tensor core in fp16, of which weights below 2^-16 of the largest start to lose bits (under 2^-27 of the largest
+//     for each). Taking the product and not p or sv alone keeps a token of huge scale and vanishing probability from
+//     pushing the others out of range. The check in the loop is conservative (p and sv against caps whose product is
+//     2^15) and the exact one runs only when it fires.
 // Sums, statistics, O and the rank-one terms are fp32.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
@@ -35,23 +42,53 @@ __device__ __forceinline__ uint32_t half2_bits(float lo, float hi) {
 }
 __device__ __forceinline__ float pow2_int(int e) { return __int_as_float((e + 127) << 23); }  // -126 <= e <= 127
 __device__ __forceinline__ int exponent_of(float x) { return static_cast<int>((__float_as_uint(x) >> 23) & 255u) - 127; }
+// Free to be scheduled among one another, unlike the volatile forms of pd_ptx.cuh: four independent chains of products are
+// in flight here, and in program order each would wait for the one before.
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The first of a chain, without registers to clear beforehand.
+__device__ __forceinline__ void mma_f16_from_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// C (16x8) = A (16x8, bf16, in the low half of a 16x16) * B + {from, from}: rows g and g + 8 start at the same two values.
+__device__ __forceinline__ void mma_bf16_from(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0, float from_a, float from_b) {
+    asm("mma.sync.aligned.m16n8k8.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5}, {%6}, {%7,%8,%7,%8};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(b0), "f"(from_a), "f"(from_b));
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
+    uint32_t d;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(a));
+    return d;
+}
 
 constexpr uint32_t kNib0 = 0x000f000fu, kNib1 = 0x00f000f0u;
-constexpr float kWeightMax = 32768.f;
 
-template <int D, int WARPS, int STAGES>
+template <int D, int WARPS, int STAGES, int TP>
 __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(const AttnParams p) {
     static_assert(D == 64 || D == 128, "head_dim 64 or 128");
     constexpr int THREADS = WARPS * 32;
     constexpr int BLOCK = q4_block_bytes<D>();
+    constexpr int STAGE = TP * BLOCK;
     constexpr int PIECES = D / 32;       // 16-byte pieces of a row
     constexpr int GROUPS = D / kQ4Group;
+    constexpr int WINDOW = 32 / TP * TP;  // page ids held one per lane, whole tiles of them
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring0 = (raw + 127u) & ~127u;
     uint8_t *aligned = smem_raw + (ring0 - raw);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + WARPS * STAGES * BLOCK);
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + WARPS * STAGES * STAGE);
     Plan *plan_s = reinterpret_cast<Plan *>(bars + WARPS * STAGES);
     int32_t *stage_range = reinterpret_cast<int32_t *>(plan_s + 1);
     int32_t *warp_sums = stage_range + WARPS * STAGES;
@@ -89,282 +126,350 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     }
 
     const int worker = blockIdx.x * WARPS + warp;
-    const uint32_t ring = ring0 + warp * STAGES * BLOCK;
-    const uint32_t bar0 = smem_u32(bars + warp * STAGES);
+    const uint32_t ring = ring0 + warp * STAGES * STAGE;
+    const uint32_t full = smem_u32(bars + warp * STAGES);
     int32_t *my_stage_range = stage_range + warp * STAGES;
-    const int quad_row = lane >> 2, quad_t = lane & 3, quad_col = quad_t * 2;
-    const int G = p.G;
-    // ldmatrix source rows: matrices 0 / 1 = slots 0-7 / 8-15 of a piece, 2 / 3 = the same of the next piece
-    const int mat = lane >> 3, ld_slot = (mat & 1) * 8 + (lane & 7), ld_piece = mat >> 1;
-    const uint32_t ld_row = ld_slot * (D / 2);
 
-    PageIdCache pt;
-    pt.b = -1; pt.blk = -1; pt.val = -1; pt.nval = -1;
+    // ---- issuing side: walks STAGES tiles ahead of the reading side
     Cursor prod;
     prod.b = 0; prod.kvh = 0; prod.page = 0; prod.np = 1;
-    int p_rid = -1, p_left = 0;
+    int p_rid = worker, p_left = 0, p_stage = 0, inflight = 0;
+    int ids = 0, ids_next = 0, window = 0;  // page ids [window, window + 32) of the open segment, one per lane, and those from window + WINDOW on
     bool p_first = true, p_done = false, have_next = false;
     int next_raw = 0;
-    uint32_t p_stage = 0;
-    int inflight = 0;
-
-    auto issue_next = [&]() -> bool {
+    const uint8_t *blocks = p.kv4;  // page 0 of the open KV head
+    const uint32_t page_bytes = static_cast<uint32_t>(p.Hkv) * BLOCK;
+    auto load_ids = [&](int page) {
+        return page + lane < prod.np ? __ldg(p.page_table + static_cast<size_t>(prod.b) * p.MP + page + lane) : 0;
+    };
+    auto issue_next = [&]() {
         if (p_left == 0) {
-            if (p_done) return false;
-            int rid;
-            if (p_first) {
-                rid = worker;
-                p_first = false;
-            } else {
+            if (p_done) return;
+            if (!p_first) {
                 if (!have_next && lane == 0) next_raw = atomicAdd(p.status + kSchedNext, 1);
-                rid = n_workers + __shfl_sync(0xffffffffu, next_raw, 0);
+                p_rid = n_workers + __shfl_sync(0xffffffffu, next_raw, 0);
                 have_next = false;
             }
-            if (rid >= pl.n_ranges) {
+            p_first = false;
+            if (p_rid >= pl.n_ranges) {
                 p_done = true;
-                return false;
+                return;
             }
             long long start;
-            range_bounds(pl, rid, start, p_left);
+            range_bounds(pl, p_rid, start, p_left);
             prod = locate(cum, p.B, p.Hkv, start);
-            p_rid = rid;
+            blocks = p.kv4 + prod.kvh * BLOCK;
+            window = prod.page;
+            ids = load_ids(window);
+            ids_next = load_ids(window + WINDOW);
         }
-        int pid = page_id(pt, p, prod.b, prod.page, lane);
-        if (pid < 0 || pid >= p.num_pages) {
-            if (lane == 0) latch_status(p.status, kDevBadPage, prod.b, pid);
-            pid = 0;
-        }
+        const int n = min(TP, min(p_left, prod.np - prod.page));
+        int pid = __shfl_sync(0xffffffffu, ids, (prod.page - window + lane) & 31);
         if (lane == 0) {
             my_stage_range[p_stage] = p_rid;
-            const uint32_t bar = bar0 + p_stage * 8;
-            mbar_arrive_expect_tx(bar, BLOCK);
-            bulk_load(ring + p_stage * BLOCK, p.kv4 + (static_cast<size_t>(pid) * p.Hkv + prod.kvh) * BLOCK, BLOCK, bar);
+            mbar_arrive_expect_tx(full + p_stage * 8, n * BLOCK);
         }
-        advance(prod, cum, p.B, p.Hkv);
-        --p_left;
-        if (p_left <= kClaimAhead && !have_next && !p_first) {
+        __syncwarp();
+        if (lane < n) {
+            if (static_cast<uint32_t>(pid) >= static_cast<uint32_t>(p.num_pages)) {
+                latch_status(p.status, kDevBadPage, prod.b, pid);
+                pid = 0;
+            }
+            bulk_load(ring + p_stage * STAGE + lane * BLOCK, blocks + static_cast<uint64_t>(static_cast<uint32_t>(pid)) * page_bytes, BLOCK,
+                      full + p_stage * 8);
+        }
+        p_left -= n;
+        prod.page += n;
+        if (prod.page == prod.np) {
+            prod.page -= 1;
+            advance(prod, cum, p.B, p.Hkv);
+            if (p_left > 0) {
+                blocks = p.kv4 + prod.kvh * BLOCK;
+                window = 0;
+                ids = load_ids(0);
+                ids_next = load_ids(WINDOW);
+            }
+        } else if (prod.page - window == WINDOW) {
+            window += WINDOW;
+            ids = ids_next;
+            ids_next = load_ids(window + WINDOW);
+        }
+        if (p_left <= kClaimAhead * TP && !have_next) {
             if (lane == 0) next_raw = atomicAdd(p.status + kSchedNext, 1);
             have_next = true;
         }
         if (++p_stage == STAGES) p_stage = 0;
         ++inflight;
-        __syncwarp();
-        return true;
     };
+    for (int s = 0; s < STAGES; ++s) issue_next();
 
-    while (inflight < STAGES && issue_next()) {}
+    // ---- reading side
+    const int quad_row = lane >> 2, quad_t = lane & 3, quad_col = quad_t * 2;
+    const int G = p.G;
+    // ldmatrix source rows: matrices 0 / 1 = slots 0-7 / 8-15 of a piece, 2 / 3 = the same of the next piece
+    const int ld_slot = ((lane >> 3) & 1) * 8 + (lane & 7), ld_piece = lane >> 4;
+    uint32_t ld_off[GROUPS];
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) ld_off[g] = ld_slot * (D / 2) + q4_piece_pos<D>(2 * g + ld_piece, ld_slot) * 16;
+    const uint32_t rec_off = 16 * D + quad_row * (D / 8);
+    int stage = 0;
+    uint32_t parity = 0;
+    bool alive = true;
 
-    Cursor cons;
-    cons.b = 0; cons.kvh = 0; cons.page = 0; cons.np = 1;
-    int c_rid = -1, c_left = 0;
-    uint32_t stage = 0, parity = 0;
-    bool alive = true, seg_open = false;
-    int seg_page0 = 0, L = 0;
-    // Q^T as the fp16 B operand, head quad_row: register j of piece c holds d = 32 c + 8 t + j and + 4 (odd j: / 16)
-    uint32_t qb[PIECES][4];
-    // heads quad_col and quad_col + 1 (a, b): unit of the code products in log2 logits, and scale_log2 * sum(q) by group
-    float unit_a = 0.f, unit_b = 0.f, qs_a[GROUPS], qs_b[GROUPS];
-    // O^T, piece c, j: rows d = 32 c + 4 g + 2 j (registers 0, 1 for heads a, b) and + 1 (registers 2, 3, 16 times larger)
-    float O[PIECES][2][4];
-    float Ma[GROUPS], Mb[GROUPS];  // this lane's slots' share of sum p * v_min
-    float m_a = -INFINITY, m_b = -INFINITY, l_a = 0.f, l_b = 0.f;
-    float f_a = 1.f, f_b = 1.f;    // weights go to the tensor core as p * v_scale * f
+    while (alive && inflight > 0) {
+        const int rid = my_stage_range[stage];
+        long long start;
+        int range_left;
+        range_bounds(pl, rid, start, range_left);
+        Cursor cur = locate(cum, p.B, p.Hkv, start);
 
-    while (inflight > 0) {
-        if (c_left == 0) {
-            c_rid = my_stage_range[stage];
-            long long start;
-            range_bounds(pl, c_rid, start, c_left);
-            cons = locate(cum, p.B, p.Hkv, start);
-        }
-        if (!seg_open) {
-            seg_open = true;
-            seg_page0 = cons.page;
-            L = clamp_len(__ldg(p.ctx_lens + cons.b), p.MP);
-            const __nv_bfloat16 *qrow = p.q + (static_cast<size_t>(cons.b) * p.Hq + cons.kvh * G + quad_row) * D;
-            uint4 x[PIECES];
-            float amax = 0.f, sum[GROUPS];
+        while (range_left > 0 && alive) {  // one segment: the range's pages of one (sequence, KV head)
+            const int page0 = cur.page, pages = min(range_left, cur.np - page0);
+            const int L = clamp_len(__ldg(p.ctx_lens + cur.b), p.MP);
+            int rem = min(L - page0 * kPageSize, pages * kPageSize);  // tokens of the segment still to come
+
+            // Q^T as the fp16 B operand, head quad_row: register j of piece c holds d = 32 c + 8 t + j and + 4 (odd j: / 16)
+            uint32_t qb[PIECES][4];
+            uint32_t qsum;  // B operand of the minima: sum(q) by group in three bf16 parts, part t in lane t
+            float unit_a, unit_b;
+            {
+                const __nv_bfloat16 *qrow = p.q + (static_cast<size_t>(cur.b) * p.Hq + cur.kvh * G + quad_row) * D;
+                uint4 x[PIECES];
+                float amax = 0.f, sum[GROUPS];
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) sum[g] = 0.f;
+                for (int g = 0; g < GROUPS; ++g) sum[g] = 0.f;
 #pragma unroll
-            for (int c = 0; c < PIECES; ++c) {
-                x[c] = make_uint4(0u, 0u, 0u, 0u);
-                if (quad_row < G) x[c] = __ldg(reinterpret_cast<const uint4 *>(qrow + c * 32 + quad_t * 8));
-                const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
+                for (int c = 0; c < PIECES; ++c) {
+                    x[c] = make_uint4(0u, 0u, 0u, 0u);
+                    if (quad_row < G) x[c] = __ldg(reinterpret_cast<const uint4 *>(qrow + c * 32 + quad_t * 8));
+                    const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float lo = bf16_lo(w[i]), hi = bf16_hi(w[i]);
-                    amax = fmaxf(amax, fmaxf(fabsf(lo), fabsf(hi)));
-                    sum[c * GROUPS / PIECES] += lo + hi;
+                    for (int i = 0; i < 4; ++i) {
+                        const float lo = bf16_lo(w[i]), hi = bf16_hi(w[i]);
+                        amax = fmaxf(amax, fmaxf(fabsf(lo), fabsf(hi)));
+                        sum[c * GROUPS / PIECES] += lo + hi;
+                    }
                 }
-            }
 #pragma unroll
-            for (int o = 1; o < 4; o <<= 1) {
-                amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
+                for (int o = 1; o < 4; o <<= 1) {
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, o));
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], o);
-            }
-            const int e = max(-100, min(100, 14 - exponent_of(amax)));
-            const float up = pow2_int(e), up16 = pow2_int(e - 4);
+                    for (int g = 0; g < GROUPS; ++g) sum[g] += __shfl_xor_sync(0xffffffffu, sum[g], o);
+                }
+                const int e = max(-100, min(100, 14 - exponent_of(amax)));
+                const float up = pow2_int(e), up16 = pow2_int(e - 4);
 #pragma unroll
-            for (int c = 0; c < PIECES; ++c) {
-                qb[c][0] = half2_bits(bf16_lo(x[c].x) * up, bf16_lo(x[c].z) * up);
-                qb[c][1] = half2_bits(bf16_hi(x[c].x) * up16, bf16_hi(x[c].z) * up16);
-                qb[c][2] = half2_bits(bf16_lo(x[c].y) * up, bf16_lo(x[c].w) * up);
-                qb[c][3] = half2_bits(bf16_hi(x[c].y) * up16, bf16_hi(x[c].w) * up16);
-            }
-            // what belongs to a head is wanted by the lanes whose accumulator columns it is
-            const int e_a = __shfl_sync(0xffffffffu, e, quad_col * 4), e_b = __shfl_sync(0xffffffffu, e, quad_col * 4 + 4);
-            unit_a = p.scale_log2 * pow2_int(24 - e_a);
-            unit_b = p.scale_log2 * pow2_int(24 - e_b);
+                for (int c = 0; c < PIECES; ++c) {
+                    qb[c][0] = half2_bits(bf16_lo(x[c].x) * up, bf16_lo(x[c].z) * up);
+                    qb[c][1] = half2_bits(bf16_hi(x[c].x) * up16, bf16_hi(x[c].z) * up16);
+                    qb[c][2] = half2_bits(bf16_lo(x[c].y) * up, bf16_lo(x[c].w) * up);
+                    qb[c][3] = half2_bits(bf16_hi(x[c].y) * up16, bf16_hi(x[c].w) * up16);
+                }
+                // the scale of a head is wanted by the lanes whose accumulator columns it is
+                unit_a = p.scale_log2 * pow2_int(24 - __shfl_sync(0xffffffffu, e, quad_col * 4));
+                unit_b = p.scale_log2 * pow2_int(24 - __shfl_sync(0xffffffffu, e, quad_col * 4 + 4));
+                float part[2] = {0.f, 0.f};
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) {
-                qs_a[g] = p.scale_log2 * __shfl_sync(0xffffffffu, sum[g], quad_col * 4);
-                qs_b[g] = p.scale_log2 * __shfl_sync(0xffffffffu, sum[g], quad_col * 4 + 4);
-                Ma[g] = 0.f;
-                Mb[g] = 0.f;
+                for (int g = 0; g < GROUPS; ++g) {
+                    const float s = sum[g] * p.scale_log2;
+                    const float hi = __bfloat162float(__float2bfloat16(s));
+                    const float mid = __bfloat162float(__float2bfloat16(s - hi));
+                    part[g] = quad_t == 0 ? hi : (quad_t == 1 ? mid : (quad_t == 2 ? s - hi - mid : 0.f));
+                }
+                qsum = pack_bf16x2(part[0], part[1]);
             }
+            // O^T, piece c, j: rows d = 32 c + 4 g + 2 j (registers 0, 1 for heads a, b); registers 2, 3: that plus 16 times d + 1
+            float O[PIECES][2][4], Ma[GROUPS], Mb[GROUPS];
 #pragma unroll
             for (int c = 0; c < PIECES; ++c)
 #pragma unroll
                 for (int j = 0; j < 2; ++j) { O[c][j][0] = 0.f; O[c][j][1] = 0.f; O[c][j][2] = 0.f; O[c][j][3] = 0.f; }
-            m_a = -INFINITY; m_b = -INFINITY;
-            l_a = 0.f; l_b = 0.f;
-            f_a = 1.f; f_b = 1.f;
-        }
+#pragma unroll
+            for (int g = 0; g < GROUPS; ++g) { Ma[g] = 0.f; Mb[g] = 0.f; }
+            float l_a = 0.f, l_b = 0.f, nr_a = 0.f, nr_b = 0.f;  // nr = -r
+            float cap_x = -INFINITY, cap_v = -1.f;  // nothing passes before the first tile has set them
 
-        const uint32_t kbase = ring + stage * BLOCK, vbase = kbase + 8 * D;
-        const int valid = L - cons.page * kPageSize;
-        if (!__all_sync(0xffffffffu, mbar_wait(bar0 + stage * 8, parity))) { alive = false; break; }
+            for (int pg = 0; pg < pages; pg += TP, rem -= TP * kPageSize) {
+                if (!__all_sync(0xffffffffu, mbar_wait(full + stage * 8, parity))) { alive = false; break; }
+                const uint32_t base = ring + stage * STAGE;
+                const uint8_t *recs = aligned + (base - ring0) + rec_off;
 
-        // records of slots g and g + 8: per group {k_scale, k_min}, {v_scale, v_min}
-        float ks0[GROUPS], km0[GROUPS], vs0[GROUPS], vm0[GROUPS], ks1[GROUPS], km1[GROUPS], vs1[GROUPS], vm1[GROUPS];
-        const uint8_t *recs = aligned + (kbase - ring0) + 16 * D;
+                // records of slots g (i = 0) and g + 8 (i = 1): words {k_scale, k_min}, {v_scale, v_min} by group
+                uint32_t rk[TP][2][GROUPS], rv[TP][2][GROUPS];
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const uint2 r0 = *reinterpret_cast<const uint2 *>(recs + quad_row * (D / 8) + g * 8);
-            const uint2 r1 = *reinterpret_cast<const uint2 *>(recs + (quad_row + 8) * (D / 8) + g * 8);
-            ks0[g] = bf16_lo(r0.x); km0[g] = bf16_hi(r0.x); vs0[g] = bf16_lo(r0.y); vm0[g] = bf16_hi(r0.y);
-            ks1[g] = bf16_lo(r1.x); km1[g] = bf16_hi(r1.x); vs1[g] = bf16_lo(r1.y); vm1[g] = bf16_hi(r1.y);
-        }
+                for (int t = 0; t < TP; ++t)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint8_t *at = recs + t * BLOCK + i * D;  // 8 slots of D / 8 bytes
+                        if (GROUPS == 2) {
+                            const uint4 w = *reinterpret_cast<const uint4 *>(at);
+                            rk[t][i][0] = w.x; rv[t][i][0] = w.y; rk[t][i][GROUPS - 1] = w.z; rv[t][i][GROUPS - 1] = w.w;
+                        } else {
+                            const uint2 w = *reinterpret_cast<const uint2 *>(at);
+                            rk[t][i][0] = w.x; rv[t][i][0] = w.y;
+                        }
+                    }
 
-        // code products K Q^T by group; the accumulators of a group hold the sum over its 64 values
-        float s0 = 0.f, s1 = 0.f, s2 = 0.f, s3 = 0.f, r0s = 0.f, r1s = 0.f, r2s = 0.f, r3s = 0.f;
+                // x = S - r in log2 units, [slot g: heads a, b; slot g + 8: heads a, b]
+                float x[TP][4];
+                {
+                    uint32_t w[TP][GROUPS][4];  // (slots 0-7, 8-15) of piece 2 g, then of piece 2 g + 1
+                    float acc[TP][4], A[TP][GROUPS][4];
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            uint32_t w[4];  // (slots 0-7, 8-15) of piece 2 g, then of piece 2 g + 1
-            ldmatrix_x4(w[0], w[1], w[2], w[3], kbase + ld_row + q4_piece_pos<D>(2 * g + ld_piece, ld_slot) * 16);
-            float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f};
-            mma_f16_16816(A, w[0] & kNib0, w[1] & kNib0, w[0] & kNib1, w[1] & kNib1, qb[2 * g][0], qb[2 * g][1]);
-            mma_f16_16816(B, w[2] & kNib0, w[3] & kNib0, w[2] & kNib1, w[3] & kNib1, qb[2 * g + 1][0], qb[2 * g + 1][1]);
+                    for (int t = 0; t < TP; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) w[i] >>= 8;
-            mma_f16_16816(A, w[0] & kNib0, w[1] & kNib0, w[0] & kNib1, w[1] & kNib1, qb[2 * g][2], qb[2 * g][3]);
-            mma_f16_16816(B, w[2] & kNib0, w[3] & kNib0, w[2] & kNib1, w[3] & kNib1, qb[2 * g + 1][2], qb[2 * g + 1][3]);
-            s0 += (A[0] + B[0]) * ks0[g]; s1 += (A[1] + B[1]) * ks0[g];
-            s2 += (A[2] + B[2]) * ks1[g]; s3 += (A[3] + B[3]) * ks1[g];
-            r0s += km0[g] * qs_a[g]; r1s += km0[g] * qs_b[g];
-            r2s += km1[g] * qs_a[g]; r3s += km1[g] * qs_b[g];
-        }
-        s0 = s0 * unit_a + r0s; s1 = s1 * unit_b + r1s;
-        s2 = s2 * unit_a + r2s; s3 = s3 * unit_b + r3s;
-        if (valid < kPageSize) {  // codes of empty slots are harmless numbers, their records may be anything
-            if (quad_row >= valid) {
-                s0 = -INFINITY; s1 = -INFINITY;
+                        for (int g = 0; g < GROUPS; ++g) {
+                            ldmatrix_x4(w[t][g][0], w[t][g][1], w[t][g][2], w[t][g][3], base + t * BLOCK + ld_off[g]);
+                        }
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) { vs0[g] = 0.f; vm0[g] = 0.f; }
-            }
-            if (quad_row + 8 >= valid) {
-                s2 = -INFINITY; s3 = -INFINITY;
+                    for (int t = 0; t < TP; ++t) {
+                        if (GROUPS == 2)
+                            mma_bf16_from(acc[t], __byte_perm(rk[t][0][0], rk[t][0][GROUPS - 1], 0x7632),
+                                          __byte_perm(rk[t][1][0], rk[t][1][GROUPS - 1], 0x7632), qsum, nr_a, nr_b);
+                        else
+                            mma_bf16_from(acc[t], rk[t][0][0] >> 16, rk[t][1][0] >> 16, qsum, nr_a, nr_b);
+                    }
 #pragma unroll
-                for (int g = 0; g < GROUPS; ++g) { vs1[g] = 0.f; vm1[g] = 0.f; }
-            }
-        }
-
-        float mx_a = fmaxf(s0, s2), mx_b = fmaxf(s1, s3);
-        float alpha_a = 1.f, alpha_b = 1.f;
-        const bool raise = __any_sync(0xffffffffu, mx_a > m_a + kRescaleSlack || mx_b > m_b + kRescaleSlack);
-        if (raise) {
+                    for (int h = 0; h < 4; ++h)  // piece 2 g + h / 2, its even (h = 0, 2) and odd bytes
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-                mx_a = fmaxf(mx_a, __shfl_xor_sync(0xffffffffu, mx_a, o));
-                mx_b = fmaxf(mx_b, __shfl_xor_sync(0xffffffffu, mx_b, o));
-            }
-            const float new_a = fmaxf(m_a, mx_a), new_b = fmaxf(m_b, mx_b);
-            alpha_a = fast_exp2(m_a - new_a);
-            alpha_b = fast_exp2(m_b - new_b);
-            l_a *= alpha_a;
-            l_b *= alpha_b;
+                        for (int t = 0; t < TP; ++t)
 #pragma unroll
-            for (int g = 0; g < GROUPS; ++g) { Ma[g] *= alpha_a; Mb[g] *= alpha_b; }
-            m_a = new_a;
-            m_b = new_b;
-        }
-        const float p0 = fast_exp2(s0 - m_a), p1 = fast_exp2(s1 - m_b);
-        const float p2 = fast_exp2(s2 - m_a), p3 = fast_exp2(s3 - m_b);
-        l_a += p0 + p2;
-        l_b += p1 + p3;
-        float w_a = 0.f, w_b = 0.f;  // largest weight of this lane's slots
+                            for (int g = 0; g < GROUPS; ++g) {
+                                const uint32_t u = w[t][g][h & 2] >> (8 * (h & 1)), v = w[t][g][(h & 2) + 1] >> (8 * (h & 1));
+                                const uint32_t b0 = qb[2 * g + (h >> 1)][2 * (h & 1)], b1 = qb[2 * g + (h >> 1)][2 * (h & 1) + 1];
+                                if (h == 0) mma_f16_from_zero(A[t][g], u & kNib0, v & kNib0, u & kNib1, v & kNib1, b0, b1);
+                                else mma_f16(A[t][g], u & kNib0, v & kNib0, u & kNib1, v & kNib1, b0, b1);
+                            }
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            Ma[g] += p0 * vm0[g] + p2 * vm1[g];
-            Mb[g] += p1 * vm0[g] + p3 * vm1[g];
-            w_a = fmaxf(w_a, fmaxf(p0 * vs0[g], p2 * vs1[g]));
-            w_b = fmaxf(w_b, fmaxf(p1 * vs0[g], p3 * vs1[g]));
-        }
-        if (__any_sync(0xffffffffu, raise || w_a * f_a > kWeightMax || w_b * f_b > kWeightMax)) {
+                    for (int t = 0; t < TP; ++t) {
+                        float sum[4];
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
-                w_a = fmaxf(w_a, __shfl_xor_sync(0xffffffffu, w_a, o));
-                w_b = fmaxf(w_b, __shfl_xor_sync(0xffffffffu, w_b, o));
-            }
-            // this page's largest weight to [2^2, 2^3), unless older weights, shrunk by alpha, are larger: O never grows
-            auto retarget = [](float w, float alpha, float &f, float &scale_o) {
-                float nf = pow2_int(max(-100, min(100, 2 - exponent_of(w))));
-                const float keep = f / alpha;  // alpha = 0 (first page, or nothing left of the past): +inf
-                int ke = exponent_of(keep);
-                if (ke < 100 && pow2_int(max(ke, -126)) < nf) nf = pow2_int(max(ke, -100));
-                scale_o = alpha * (nf / f);
-                if (!(alpha > 0.f)) scale_o = 0.f;
-                f = nf;
-            };
-            float so_a, so_b;
-            retarget(w_a, alpha_a, f_a, so_a);
-            retarget(w_b, alpha_b, f_b, so_b);
-#pragma unroll
-            for (int c = 0; c < PIECES; ++c)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    O[c][j][0] *= so_a; O[c][j][2] *= so_a;
-                    O[c][j][1] *= so_b; O[c][j][3] *= so_b;
+                        for (int g = 0; g < GROUPS; ++g) {
+                            const float s0 = bf16_lo(rk[t][0][g]), s1 = bf16_lo(rk[t][1][g]);
+                            sum[0] = g == 0 ? A[t][g][0] * s0 : fmaf(A[t][g][0], s0, sum[0]);
+                            sum[1] = g == 0 ? A[t][g][1] * s0 : fmaf(A[t][g][1], s0, sum[1]);
+                            sum[2] = g == 0 ? A[t][g][2] * s1 : fmaf(A[t][g][2], s1, sum[2]);
+                            sum[3] = g == 0 ? A[t][g][3] * s1 : fmaf(A[t][g][3], s1, sum[3]);
+                        }
+                        x[t][0] = fmaf(sum[0], unit_a, acc[t][0]);
+                        x[t][1] = fmaf(sum[1], unit_b, acc[t][1]);
+                        x[t][2] = fmaf(sum[2], unit_a, acc[t][2]);
+                        x[t][3] = fmaf(sum[3], unit_b, acc[t][3]);
+                    }
                 }
-        }
+                if (rem < TP * kPageSize) {  // codes of empty slots are harmless numbers, their records may be anything
+#pragma unroll
+                    for (int t = 0; t < TP; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if (t * kPageSize + i * 8 + quad_row >= rem) {
+                                x[t][2 * i] = -INFINITY;
+                                x[t][2 * i + 1] = -INFINITY;
+#pragma unroll
+                                for (int g = 0; g < GROUPS; ++g) rv[t][i][g] = 0u;
+                            }
+                }
 
-        // O^T += V^T (P v_scale f)^T; the weights differ by group
-        const float p0f = p0 * f_a, p1f = p1 * f_b, p2f = p2 * f_a, p3f = p3 * f_b;
+                float xm_a = x[0][0], xm_b = x[0][1], vm = 0.f;
 #pragma unroll
-        for (int g = 0; g < GROUPS; ++g) {
-            const uint32_t pb0 = movmatrix_trans(half2_bits(p0f * vs0[g], p1f * vs0[g]));
-            const uint32_t pb1 = movmatrix_trans(half2_bits(p2f * vs1[g], p3f * vs1[g]));
-            uint32_t w[4];
-            ldmatrix_x4_trans(w[0], w[1], w[2], w[3], vbase + ld_row + q4_piece_pos<D>(2 * g + ld_piece, ld_slot) * 16);
+                for (int t = 0; t < TP; ++t) {
+                    xm_a = max3(xm_a, x[t][0], x[t][2]);
+                    xm_b = max3(xm_b, x[t][1], x[t][3]);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                uint32_t x = w[2 * h], y = w[2 * h + 1];  // slots 2t, 2t+1 and 2t+8, 2t+9; four consecutive d each
-                mma_f16_16816(O[2 * g + h][0], x & kNib0, x & kNib1, y & kNib0, y & kNib1, pb0, pb1);
-                x >>= 8;
-                y >>= 8;
-                mma_f16_16816(O[2 * g + h][1], x & kNib0, x & kNib1, y & kNib0, y & kNib1, pb0, pb1);
+                    for (int g = 0; g < GROUPS; ++g) vm = max3(vm, bf16_lo(rv[t][0][g]), bf16_lo(rv[t][1][g]));
+                }
+                if (__any_sync(0xffffffffu, xm_a > cap_x || xm_b > cap_x || vm > cap_v)) {
+                    // largest weight of this tile by head: p * v_scale; a minimum 2^24 times the scale counts like the scale
+                    // (the codes no longer matter then), and p itself stays below 2^100
+                    float w_a = xm_a - 100.f, w_b = xm_b - 100.f;
+#pragma unroll
+                    for (int t = 0; t < TP; ++t)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i) {
+                            float v = 0.f;
+#pragma unroll
+                            for (int g = 0; g < GROUPS; ++g)
+                                v = fmaxf(v, fmaxf(bf16_lo(rv[t][i][g]), fabsf(bf16_hi(rv[t][i][g])) * 5.9604645e-8f));
+                            const float lv = __log2f(v);  // v = 0: -inf
+                            w_a = fmaxf(w_a, x[t][2 * i] + lv);
+                            w_b = fmaxf(w_b, x[t][2 * i + 1] + lv);
+                        }
+#pragma unroll
+                    for (int o = 4; o < 32; o <<= 1) {
+                        w_a = fmaxf(w_a, __shfl_xor_sync(0xffffffffu, w_a, o));
+                        w_b = fmaxf(w_b, __shfl_xor_sync(0xffffffffu, w_b, o));
+                    }
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) vm = fmaxf(vm, __shfl_xor_sync(0xffffffffu, vm, o));
+                    // the first tile puts its largest weight at 2^2; later ones only ever raise r
+                    const bool fresh = cap_v < 0.f;
+                    const float up_a = fresh ? w_a - 2.f : fmaxf(w_a - 2.f, 0.f), up_b = fresh ? w_b - 2.f : fmaxf(w_b - 2.f, 0.f);
+                    const float f_a = fresh ? 0.f : fast_exp2(-up_a), f_b = fresh ? 0.f : fast_exp2(-up_b);
+                    nr_a -= up_a;
+                    nr_b -= up_b;
+                    l_a *= f_a;
+                    l_b *= f_b;
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) { Ma[g] *= f_a; Mb[g] *= f_b; }
+#pragma unroll
+                    for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            O[c][j][0] *= f_a; O[c][j][2] *= f_a;
+                            O[c][j][1] *= f_b; O[c][j][3] *= f_b;
+                        }
+#pragma unroll
+                    for (int t = 0; t < TP; ++t) {
+                        x[t][0] -= up_a; x[t][2] -= up_a;
+                        x[t][1] -= up_b; x[t][3] -= up_b;
+                    }
+                    // caps with cap_v 2^cap_x <= 2^15; v_scale may grow eightfold before the next look
+                    const int ev = max(-110, min(100, exponent_of(fmaxf(vm, cap_v * 0.125f)) + 1));
+                    cap_v = pow2_int(ev + 3);
+                    cap_x = static_cast<float>(min(15 - (ev + 3), 100));
+                }
+
+                // weights, their sums, and the fp16 B operands: P^T transposed from (slot x head) to (head x slot)
+                uint32_t pb[TP][GROUPS][2];
+#pragma unroll
+                for (int t = 0; t < TP; ++t) {
+                    const float p0 = fast_exp2(x[t][0]), p1 = fast_exp2(x[t][1]), p2 = fast_exp2(x[t][2]), p3 = fast_exp2(x[t][3]);
+                    l_a += p0 + p2;
+                    l_b += p1 + p3;
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g) {
+                        const float v0 = bf16_lo(rv[t][0][g]), v1 = bf16_lo(rv[t][1][g]), m0 = bf16_hi(rv[t][0][g]), m1 = bf16_hi(rv[t][1][g]);
+                        Ma[g] = fmaf(p0, m0, fmaf(p2, m1, Ma[g]));
+                        Mb[g] = fmaf(p1, m0, fmaf(p3, m1, Mb[g]));
+                        pb[t][g][0] = transpose8x8(half2_bits(p0 * v0, p1 * v0));
+                        pb[t][g][1] = transpose8x8(half2_bits(p2 * v1, p3 * v1));
+                    }
+                }
+                // O^T += V^T P^T; with V's codes in registers the stage goes back to the copies
+                uint32_t w[TP][GROUPS][4];
+#pragma unroll
+                for (int t = 0; t < TP; ++t)
+#pragma unroll
+                    for (int g = 0; g < GROUPS; ++g)
+                        ldmatrix_x4_trans(w[t][g][0], w[t][g][1], w[t][g][2], w[t][g][3], base + t * BLOCK + 8 * D + ld_off[g]);
+                __syncwarp();
+                --inflight;
+                issue_next();
+#pragma unroll
+                for (int t = 0; t < TP; ++t)
+#pragma unroll
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int g = 0; g < GROUPS; ++g) {
+                            const uint32_t u = w[t][g][h & 2], v = w[t][g][(h & 2) + 1];  // slots 2t, 2t+1 and 2t+8, 2t+9; four consecutive d each
+                            const uint32_t pick = (h & 1) ? 0x4341u : 0x4240u;            // d + 2, d + 3 or d, d + 1
+                            const uint32_t ub = __byte_perm(u, 0u, pick), vb = __byte_perm(v, 0u, pick);
+                            mma_f16(O[2 * g + (h >> 1)][h & 1], ub & kNib0, ub, vb & kNib0, vb, pb[t][g][0], pb[t][g][1]);
+                        }
+                if (++stage == STAGES) { stage = 0; parity ^= 1u; }
             }
-        }
-        __syncwarp();
-        --inflight;
-        issue_next();
-        if (++stage == STAGES) { stage = 0; parity ^= 1u; }
+            if (!alive) break;
 
-        --c_left;
-        const bool pair_end = cons.page + 1 == cons.np;
-        if (c_left == 0 || pair_end) {
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) {
                 l_a += __shfl_xor_sync(0xffffffffu, l_a, o);
@@ -375,54 +480,57 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                     Mb[g] += __shfl_xor_sync(0xffffffffu, Mb[g], o);
                 }
             }
-            const size_t row0 = static_cast<size_t>(cons.b) * p.Hq + cons.kvh * G + quad_col;
+            const size_t row0 = static_cast<size_t>(cur.b) * p.Hq + cur.kvh * G + quad_col;
             const bool has_a = quad_col < G, has_b = quad_col + 1 < G;
-            // codes came in as code * 2^-24 (and 16 times that in registers 2, 3)
-            const float ka = 16777216.f / f_a, kb = 16777216.f / f_b;
-            if (seg_page0 == 0 && pair_end) {
-                const float inv_a = 1.f / l_a, inv_b = 1.f / l_b;
+            const bool whole = page0 == 0 && pages == cur.np;
+            // Final rows are divided by the sum of weights. Partials carry (reference, sum) with the sum in [1, 2), so that the
+            // merge compares references that mean the same thing whatever this segment's scales were.
+            const int el_a = max(-126, min(126, exponent_of(l_a))), el_b = max(-126, min(126, exponent_of(l_b)));
+            const float da = whole ? 1.f / l_a : pow2_int(-el_a), db = whole ? 1.f / l_b : pow2_int(-el_b);
+            // codes came in as code * 2^-24; registers 2, 3 hold the even row plus 16 times the odd one
+            float ya[PIECES][4], yb[PIECES][4];
+#pragma unroll
+            for (int c = 0; c < PIECES; ++c) {
+                const float ma = Ma[c * GROUPS / PIECES], mb = Mb[c * GROUPS / PIECES];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    ya[c][2 * j] = (O[c][j][0] * 16777216.f + ma) * da;
+                    ya[c][2 * j + 1] = ((O[c][j][2] - O[c][j][0]) * 1048576.f + ma) * da;
+                    yb[c][2 * j] = (O[c][j][1] * 16777216.f + mb) * db;
+                    yb[c][2 * j + 1] = ((O[c][j][3] - O[c][j][1]) * 1048576.f + mb) * db;
+                }
+            }
+            if (whole) {
                 __nv_bfloat16 *oa = p.out + row0 * D + 4 * quad_row, *ob = oa + D;
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
-                    const float ma = Ma[c * GROUPS / PIECES], mb = Mb[c * GROUPS / PIECES];
-                    const float *x = O[c][0], *y = O[c][1];
                     if (has_a)
-                        *reinterpret_cast<uint2 *>(oa + 32 * c) =
-                            make_uint2(pack_bf16x2((x[0] * ka + ma) * inv_a, (x[2] * (ka * 0.0625f) + ma) * inv_a),
-                                       pack_bf16x2((y[0] * ka + ma) * inv_a, (y[2] * (ka * 0.0625f) + ma) * inv_a));
+                        *reinterpret_cast<uint2 *>(oa + 32 * c) = make_uint2(pack_bf16x2(ya[c][0], ya[c][1]), pack_bf16x2(ya[c][2], ya[c][3]));
                     if (has_b)
-                        *reinterpret_cast<uint2 *>(ob + 32 * c) =
-                            make_uint2(pack_bf16x2((x[1] * kb + mb) * inv_b, (x[3] * (kb * 0.0625f) + mb) * inv_b),
-                                       pack_bf16x2((y[1] * kb + mb) * inv_b, (y[3] * (kb * 0.0625f) + mb) * inv_b));
+                        *reinterpret_cast<uint2 *>(ob + 32 * c) = make_uint2(pack_bf16x2(yb[c][0], yb[c][1]), pack_bf16x2(yb[c][2], yb[c][3]));
                 }
                 if (p.lse != nullptr && quad_row == 0) {
-                    if (has_a) p.lse[row0] = (m_a + log2f(l_a)) * kLn2;
-                    if (has_b) p.lse[row0 + 1] = (m_b + log2f(l_b)) * kLn2;
+                    if (has_a) p.lse[row0] = (log2f(l_a) - nr_a) * kLn2;
+                    if (has_b) p.lse[row0 + 1] = (log2f(l_b) - nr_b) * kLn2;
                 }
             } else {
-                const size_t slot = static_cast<size_t>(c_rid) + static_cast<size_t>(cons.b) * p.Hkv + cons.kvh;
+                const size_t slot = static_cast<size_t>(rid) + static_cast<size_t>(cur.b) * p.Hkv + cur.kvh;
                 float *oa = p.part_o + (slot * G + quad_col) * D + 4 * quad_row, *ob = oa + D;
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
-                    const float ma = Ma[c * GROUPS / PIECES], mb = Mb[c * GROUPS / PIECES];
-                    const float *x = O[c][0], *y = O[c][1];
-                    if (has_a)
-                        *reinterpret_cast<float4 *>(oa + 32 * c) = make_float4(x[0] * ka + ma, x[2] * (ka * 0.0625f) + ma,
-                                                                              y[0] * ka + ma, y[2] * (ka * 0.0625f) + ma);
-                    if (has_b)
-                        *reinterpret_cast<float4 *>(ob + 32 * c) = make_float4(x[1] * kb + mb, x[3] * (kb * 0.0625f) + mb,
-                                                                              y[1] * kb + mb, y[3] * (kb * 0.0625f) + mb);
+                    if (has_a) *reinterpret_cast<float4 *>(oa + 32 * c) = make_float4(ya[c][0], ya[c][1], ya[c][2], ya[c][3]);
+                    if (has_b) *reinterpret_cast<float4 *>(ob + 32 * c) = make_float4(yb[c][0], yb[c][1], yb[c][2], yb[c][3]);
                 }
                 if (quad_row == 0) {
-                    if (has_a) p.part_ml[slot * G + quad_col] = make_float2(m_a, l_a);
-                    if (has_b) p.part_ml[slot * G + quad_col + 1] = make_float2(m_b, l_b);
+                    if (has_a) p.part_ml[slot * G + quad_col] = make_float2(el_a - nr_a, l_a * da);
+                    if (has_b) p.part_ml[slot * G + quad_col + 1] = make_float2(el_b - nr_b, l_b * db);
                 }
             }
-            seg_open = false;
+            range_left -= pages;
+            cur.page += pages - 1;
+            advance(cur, cum, p.B, p.Hkv);
         }
-        advance(cons, cum, p.B, p.Hkv);
     }
-
     if (lane == 0) {
         if (!alive) latch_status(p.status, kDevTimeout, -1, worker);
         if (atomicAdd(p.status + kSchedDone, 1) == n_workers - 1) {  // the last worker re-arms the claim counter
@@ -432,16 +540,35 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     }
 }
 
-template <int D, int WARPS, int STAGES>
+template <int D, int WARPS, int STAGES, int TP>
 constexpr size_t q4_smem_bytes() {
-    return static_cast<size_t>(WARPS) * STAGES * q4_block_bytes<D>() + 128 + WARPS * STAGES * 8 + sizeof(Plan) +
+    return static_cast<size_t>(WARPS) * STAGES * TP * q4_block_bytes<D>() + 128 + WARPS * STAGES * 8 + sizeof(Plan) +
            WARPS * STAGES * 4 + 32 * 4 + (kMaxBatch + 1) * 4;
 }
 
+#ifndef PD_Q4_W128
+#define PD_Q4_W128 12
+#endif
+#ifndef PD_Q4_S128
+#define PD_Q4_S128 1
+#endif
+#ifndef PD_Q4_T128
+#define PD_Q4_T128 4
+#endif
+#ifndef PD_Q4_W64
+#define PD_Q4_W64 16
+#endif
+#ifndef PD_Q4_S64
+#define PD_Q4_S64 2
+#endif
+#ifndef PD_Q4_T64
+#define PD_Q4_T64 4
+#endif
 template <typename F>
 cudaError_t with_q4_kernel(int head_dim, F &&f) {
-    if (head_dim == 64) return f(decode_attn_split_q4_kernel<64, 16, 10>, q4_smem_bytes<64, 16, 10>(), 16);
-    return f(decode_attn_split_q4_kernel<128, 16, 5>, q4_smem_bytes<128, 16, 5>(), 16);
+    if (head_dim == 64)
+        return f(decode_attn_split_q4_kernel<64, PD_Q4_W64, PD_Q4_S64, PD_Q4_T64>, q4_smem_bytes<64, PD_Q4_W64, PD_Q4_S64, PD_Q4_T64>(), PD_Q4_W64);
+    return f(decode_attn_split_q4_kernel<128, PD_Q4_W128, PD_Q4_S128, PD_Q4_T128>, q4_smem_bytes<128, PD_Q4_W128, PD_Q4_S128, PD_Q4_T128>(), PD_Q4_W128);
 }
 
 }  // namespace
