@@ -754,6 +754,8 @@ int decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *p
     p.min_pages_auto = ctx->min_pages_auto;
     p.halving_levels = ctx->halving_levels;
     p.tail_pages = ctx->tail_pages;
+    // One equal range per worker as long as the FP8 kernel takes it: claiming short ranges late measured 168 against 145 us on
+    // 64 contexts of 2K-16K (32/8 heads) and 128 against 88 us on 64 lognormal ones (32/4 heads).
     p.static_fair_max = kFp8StaticFairMax;
     const bool hooked = ctx->ev_before != nullptr;
     p.pdl = hooked ? 0 : ctx->pdl;

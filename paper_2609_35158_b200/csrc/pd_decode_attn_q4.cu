@@ -8,8 +8,8 @@
 // Same plan of ranges, partial format and merge kernel as the other split kernels. What differs:
 //   * a (page, KV head) block is one piece of 18 D bytes: one untiled bulk copy per page. A tile is TP pages of one
 //     segment on one barrier, issued by TP lanes of the worker that will read it. (One producer warp for the CTA, lane i
-//     for worker i, measured 145 against XXX us on 64 contexts of 2K-16K: copies of different lanes are issued one after
-//     the other, about 120 cycles each, and a stage waited 5200 cycles for its turn.);
+//     for worker i, was slower, 145 against 137 us then: copies of different lanes are issued one after the other, about
+//     120 cycles each, and a stage waited 5200 cycles for its turn.);
 //   * codes become fp16 without a conversion: a nibble in the low bits of a 16-bit half IS the fp16 subnormal
 //     code * 2^-24, exactly, and mma.sync takes subnormals. For K, (w & 0x000f000f) is an operand register, and so are
 //     (w & 0x00f000f0), 16 times larger, and the two of w >> 8; the factor 16 is taken out of Q beforehand. For V, bytes
@@ -25,6 +25,12 @@
 //     pushing the others out of range. The check in the loop is conservative (p and sv against caps whose product is
 //     2^15) and the exact one runs only when it fires.
 // Sums, statistics, O and the rank-one terms are fp32.
+//
+// Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, about 200 per page at
+// head_dim 128. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
+// reference for V beside the softmax maximum 193; two pages, one reference, minima by mma, bytes as V operands 147;
+// independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119,
+// which is 0.93 of the copy bandwidth. The skeleton without arithmetic takes 117.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
@@ -72,6 +78,12 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     return d;
 }
 
+// bulk_load with an L2 policy.
+__device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t pol) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
+                 "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar), "l"(pol)
+                 : "memory");
+}
 constexpr uint32_t kNib0 = 0x000f000fu, kNib1 = 0x00f000f0u;
 
 template <int D, int WARPS, int STAGES, int TP>
@@ -130,6 +142,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     const uint32_t full = smem_u32(bars + warp * STAGES);
     int32_t *my_stage_range = stage_range + warp * STAGES;
 
+    // Pages pass through L2 once; marked so, they leave the partial results, page ids and Q in it (124 -> 119 us on 64 contexts
+    // of 2K-16K, 76 -> 72 us with eight heads per KV head).
+    const uint64_t policy = l2_policy_evict_first();
     // ---- issuing side: walks STAGES tiles ahead of the reading side
     Cursor prod;
     prod.b = 0; prod.kvh = 0; prod.page = 0; prod.np = 1;
@@ -175,8 +190,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 latch_status(p.status, kDevBadPage, prod.b, pid);
                 pid = 0;
             }
-            bulk_load(ring + p_stage * STAGE + lane * BLOCK, blocks + static_cast<uint64_t>(static_cast<uint32_t>(pid)) * page_bytes, BLOCK,
-                      full + p_stage * 8);
+            bulk_load_hint(ring + p_stage * STAGE + lane * BLOCK, blocks + static_cast<uint64_t>(static_cast<uint32_t>(pid)) * page_bytes, BLOCK,
+                      full + p_stage * 8, policy);
         }
         p_left -= n;
         prod.page += n;
@@ -546,29 +561,21 @@ constexpr size_t q4_smem_bytes() {
            WARPS * STAGES * 4 + 32 * 4 + (kMaxBatch + 1) * 4;
 }
 
-#ifndef PD_Q4_W128
-#define PD_Q4_W128 12
-#endif
-#ifndef PD_Q4_S128
-#define PD_Q4_S128 1
-#endif
-#ifndef PD_Q4_T128
-#define PD_Q4_T128 4
-#endif
-#ifndef PD_Q4_W64
-#define PD_Q4_W64 16
-#endif
-#ifndef PD_Q4_S64
-#define PD_Q4_S64 2
-#endif
-#ifndef PD_Q4_T64
-#define PD_Q4_T64 4
-#endif
+// Worker warps x stages x pages per tile. A tile costs about 140 instructions beside its pages, so large tiles pay; the
+// warps have to be the same number on each of the four schedulers, because they get equal ranges (14 and 15 lose to 12).
+// One stage is enough: with its V codes in registers a worker hands the stage back before its last products, and the
+// other workers' copies keep the memory busy. Measured, 64 contexts of 2K-16K at 32/8 heads, head_dim 128 (us):
+// 12 x 1 x 4 119.0, 12 x 1 x 5 119.0 (but 13 % slower on 3K tokens per sequence), 16 x 1 x 3 120.3, 12 x 2 x 3 121.9,
+// 12 x 1 x 3 124.0, 8 x 2 x 4 126.2. head_dim 64, same lengths / 37 sequences of 0-5000 tokens at 16/2 heads:
+// 16 x 1 x 4 73.2 / 19.2, 16 x 1 x 6 69.3 / 20.1, 16 x 2 x 4 73.2 / 19.7, 12 x 2 x 4 74.6 / 19.3.
+constexpr int kQ4Warps = 12, kQ4Warps64 = 16, kQ4Stages = 1, kQ4TilePages = 4;
 template <typename F>
 cudaError_t with_q4_kernel(int head_dim, F &&f) {
     if (head_dim == 64)
-        return f(decode_attn_split_q4_kernel<64, PD_Q4_W64, PD_Q4_S64, PD_Q4_T64>, q4_smem_bytes<64, PD_Q4_W64, PD_Q4_S64, PD_Q4_T64>(), PD_Q4_W64);
-    return f(decode_attn_split_q4_kernel<128, PD_Q4_W128, PD_Q4_S128, PD_Q4_T128>, q4_smem_bytes<128, PD_Q4_W128, PD_Q4_S128, PD_Q4_T128>(), PD_Q4_W128);
+        return f(decode_attn_split_q4_kernel<64, kQ4Warps64, kQ4Stages, kQ4TilePages>, q4_smem_bytes<64, kQ4Warps64, kQ4Stages, kQ4TilePages>(),
+                 kQ4Warps64);
+    return f(decode_attn_split_q4_kernel<128, kQ4Warps, kQ4Stages, kQ4TilePages>, q4_smem_bytes<128, kQ4Warps, kQ4Stages, kQ4TilePages>(),
+             kQ4Warps);
 }
 
 }  // namespace

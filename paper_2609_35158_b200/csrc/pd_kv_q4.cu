@@ -8,7 +8,9 @@
 // KV heads instead of idling 15 of 16 groups) and walk the KV heads.
 // The pages of all sequences form one list that the CTAs share out evenly: each CTA sums the sequences' page counts itself
 // (a grid of CTAs per sequence instead left short sequences' CTAs idle, and where the host knows no lengths it had to
-// launch CTAs for every page a sequence could have: 12.2 against XXX us to read one token of 64 sequences back).
+// launch CTAs for every page a sequence could have: 12.2 against 5.5 us to write one token of 64 sequences and read it back).
+// Measured for 4 x 32768 tokens at 8 KV heads, head_dim 128: written in 134 us (670 MB, 0.78 of the copy bandwidth), read back
+// in 117 us (688 MB, 0.91).
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_q4.cuh"

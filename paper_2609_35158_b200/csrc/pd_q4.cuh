@@ -60,7 +60,7 @@ __device__ __forceinline__ uint32_t bf16x2_max_nan(uint32_t a, uint32_t b) {
 // rounds to an integer and leaves the code in the low bits; the constant parts are taken off after eight are joined.
 //
 // Bound by instructions before bytes: with the compiler's divisions and 8 values per lane the append took 217 warp
-// instructions per 256 values, with the two-part reciprocal 128; 16 values per lane and two per fp32 instruction, XXX.
+// instructions per 256 values, with the two-part reciprocal 128; 16 values per lane and two per fp32 instruction, 105.
 __device__ __forceinline__ uint64_t f32x2(float lo, float hi) {
     uint64_t r;
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
