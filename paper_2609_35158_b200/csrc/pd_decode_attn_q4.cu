@@ -30,7 +30,9 @@
 // head_dim 128. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
 // reference for V beside the softmax maximum 193; two pages, one reference, minima by mma, bytes as V operands 147;
 // independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119,
-// which is 0.93 of the copy bandwidth. The skeleton without arithmetic takes 117.
+// which is 0.93 of the copy bandwidth (126, 0.88, when it runs for long and the power limit takes the SM clock to about
+// 1.8 GHz). The skeleton without arithmetic takes 117. Pages fetched four at a time by a TMA gather instead of four bulk
+// copies: 1 % slower at head_dim 128. Partial results merged inside this kernel instead of by the next one: 2 us slower.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
@@ -137,7 +139,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
         }
     }
 
-    const int worker = blockIdx.x * WARPS + warp;
+    const int worker = warp * gridDim.x + blockIdx.x;  // a few ranges spread over all SMs (11.4 against 12.3 us for one sequence of 4096 tokens)
     const uint32_t ring = ring0 + warp * STAGES * STAGE;
     const uint32_t full = smem_u32(bars + warp * STAGES);
     int32_t *my_stage_range = stage_range + warp * STAGES;
