@@ -444,8 +444,9 @@ int pd_kv_scatter_fp8(pd_ctx *ctx, const void *packed, const int64_t *packed_pag
 
 /*
  * Append of one token per sequence (pd_kv_append_q4: k_new / v_new [batch][num_kv_heads][head_dim]) and of packed new
- * tokens (pd_kv_append_tokens_q4: rows as in pd_kv_append_tokens), quantised as they are written. Positions, skipping and error reporting as
- * pd_kv_append and pd_kv_append_tokens. PD_APPEND_NO_ADVANCE leaves ctx_lens as it is, for the layers of a model that
+ * tokens (pd_kv_append_tokens_q4: rows as in pd_kv_append_tokens), quantised as they are written. Positions, skipping and
+ * error reporting as pd_kv_append and pd_kv_append_tokens; a sequence that brings more than one token although max_q_len
+ * is 1 is skipped and latched. PD_APPEND_NO_ADVANCE leaves ctx_lens as it is, for the layers of a model that
  * share one length array.
  */
 int pd_kv_append_q4(pd_ctx *ctx, const void *k_new, const void *v_new, void *kv4, const int32_t *page_table,
@@ -505,7 +506,7 @@ typedef struct pd_rope_config {
  * pd_rope_tokens followed by pd_kv_append_tokens / pd_kv_append_tokens_q4 (rotated keys are rounded to bf16 before they are
  * quantised). positions NULL: every axis stands at the token's index in its sequence, ctx_lens[b] + i. A sequence whose append is
  * skipped still gets its q_out. One token per sequence is q_indptr = 0, 1, 2, ... with max_q_len 1.
- * PD_ERR_UNSUPPORTED: rot_dim not a multiple of 16; for _q4 also num_kv_heads * head_dim above 20480.
+ * PD_ERR_UNSUPPORTED: rot_dim not a multiple of 16; for _q4 also num_kv_heads * head_dim above 14336.
  */
 int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,
                    const void *k, void *q_out, void *k_out, int32_t total, void *stream);

@@ -824,8 +824,8 @@ int rope_append(pd_ctx *ctx, const char *who, const pd_rope_config *rope, const 
     if (max_q_len < 0 || position_stride < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len and position_stride must be >= 0");
     pd::RopeParams p{};
     if (int rc = rope_params(ctx, rope, &p)) return rc;
-    if (kv4 != nullptr && ctx->cfg.num_kv_heads * ctx->cfg.head_dim > 20480)
-        return fail(ctx, PD_ERR_UNSUPPORTED, "pd_rope_append_tokens_q4: num_kv_heads * head_dim above 20480");
+    if (kv4 != nullptr && ctx->cfg.num_kv_heads * ctx->cfg.head_dim > 14336)
+        return fail(ctx, PD_ERR_UNSUPPORTED, "pd_rope_append_tokens_q4: num_kv_heads * head_dim above 14336");
     if (batch == 0 || max_q_len == 0) return PD_OK;
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");

@@ -405,6 +405,79 @@ def test_step_is_append_then_attention_and_can_be_captured():
         check_attention(out_b, lse_b, ref)
 
 
+def test_an_empty_batch_and_rows_behind_the_last_sequence():
+    """All contexts empty; and a batch argument below the tensors' rows leaves the others as they were."""
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv, d = 8, 2, 64
+    lens = np.array([0, 0, 40], np.int32)
+    kv4, table, NP = random_cache(lens, Hkv, d, 140)
+    q = wl.random_bf16((3, Hq, d), 141, DEV)
+    out = torch.full((3, Hq, d), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((3, Hq), 5.0, device=DEV)
+    with Ctx(Hq, Hkv, d, 3, table.shape[1], NP) as ctx:
+        pd.pd_decode_attn_q4(ctx.h, q, dev(kv4), dev(table), dev(lens), out, lse, batch=2, sm_scale=0.1)
+        torch.cuda.synchronize()
+        assert (out[:2] == 0).all() and torch.isneginf(lse[:2]).all() and (out[2] == 5).all() and (lse[2] == 5).all()
+        pool, L = torch.zeros((NP, Hkv, 18 * d), dtype=torch.uint8, device=DEV), dev(np.array([3, 0, 8], np.int32))
+        rows = dev(np.array([[0], [1], [2]], np.int32).repeat(table.shape[1], 1))
+        kn = wl.random_bf16((3, Hkv, d), 142, DEV)
+        pd.pd_kv_append_q4(ctx.h, kn, kn, pool, rows, L, batch=2)
+        torch.cuda.synchronize()
+        assert pd.pd_device_status(ctx.h)[0] == 0
+        assert L.cpu().tolist() == [4, 1, 8] and pool.flatten(1).any(1).cpu().tolist()[:3] == [True, True, False]
+
+
+def test_more_tokens_than_announced_are_refused_on_the_device():
+    import paper_2609_35158_b200 as pd
+
+    Hkv, d = 2, 128
+    kn = wl.random_bf16((3, Hkv, d), 150, DEV)
+    pool, L = torch.zeros((2, Hkv, 18 * d), dtype=torch.uint8, device=DEV), dev(np.zeros(2, np.int32))
+    with Ctx(Hkv, Hkv, d, 2, 1, 2) as ctx:
+        pd.pd_kv_append_tokens_q4(ctx.h, kn, kn, dev(np.array([0, 2, 3], np.int32)), pool, dev(np.array([[0], [1]], np.int32)), L, 1)
+        assert pd.pd_device_status(ctx.h)[:2] == (pd.PD_ERR_DEVICE_FAULT, 0)
+        assert L.cpu().tolist() == [0, 1] and pool.flatten(1).any(1).cpu().tolist() == [False, True]
+
+
+def test_two_contexts_on_two_streams_at_once():
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv, d = 32, 8, 128
+    runs = []
+    for seed, lens in ((160, [3000, 17, 900]), (170, [1, 5000, 0, 64])):
+        lens = np.array(lens, np.int32)
+        kv4, table, NP = random_cache(lens, Hkv, d, seed)
+        q = wl.random_bf16((len(lens), Hq, d), seed + 1, DEV)
+        runs.append((q, kv4, table, lens, NP, *attend(pd, Hq, Hkv, d, q, kv4, table, lens, NP, 0.09)))
+    streams = [torch.cuda.Stream() for _ in runs]
+    with Ctx(Hq, Hkv, d, 4, runs[0][2].shape[1], runs[0][4]) as a, Ctx(Hq, Hkv, d, 4, runs[1][2].shape[1], runs[1][4]) as b:
+        inputs = [(r[0], dev(r[1]), dev(r[2]), dev(r[3]), torch.empty_like(r[5]), torch.empty_like(r[6])) for r in runs]
+        torch.cuda.synchronize()
+        for _ in range(20):
+            for ctx, s, (q, kv, t, L, out, lse) in zip((a, b), streams, inputs):
+                pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, out, lse, sm_scale=0.09, stream=s)
+        torch.cuda.synchronize()
+        for r, x in zip(runs, inputs):
+            assert torch.equal(r[5].view(torch.int16), x[4].view(torch.int16)) and torch.equal(r[6], x[5])
+
+
+@pytest.mark.parametrize("seed", range(10))
+def test_attention_random_cases(seed):
+    import paper_2609_35158_b200 as pd
+
+    rng = np.random.default_rng(1000 + seed)
+    d, Hkv = int(rng.choice([64, 128])), int(rng.choice([1, 2, 3, 5]))
+    Hq = Hkv * int(rng.choice([1, 2, 4, 8]))
+    lens = np.minimum(np.exp(rng.uniform(0, 7.5, int(rng.integers(1, 9)))).astype(np.int32) * rng.integers(0, 2, 1)[0] + rng.integers(0, 70), 2000).astype(np.int32)
+    kv4, table, NP = random_cache(lens, Hkv, d, 1100 + seed, scale_k=float(10 ** rng.uniform(-3, 1)), scale_v=float(10 ** rng.uniform(-3, 3)))
+    q = wl.random_bf16((len(lens), Hq, d), 1200 + seed, "cpu")
+    scale = float(rng.uniform(0.02, 0.3))
+    ref = q4.decode_attn(oracle.bf16_bits(q), kv4, table, lens, scale)
+    out, lse = attend(pd, Hq, Hkv, d, q.to(DEV), kv4, table, lens, NP, scale, int(rng.choice([0, 0, 2, 7])))
+    check_attention(out, lse, ref, f"seed {seed}: {Hq}/{Hkv} d={d} {lens.tolist()}")
+
+
 def test_blocks_past_four_gigabytes():
     """Pages at the far end of a pool of 5 GB: block offsets need 64 bits."""
     import paper_2609_35158_b200 as pd

@@ -76,13 +76,13 @@ def packed(before, new, seed, Hq, Hkv, d, axes):
             wl.random_bf16((total, Hkv, d), seed + 3, DEV))
 
 
-@pytest.mark.parametrize("d,rot,adjacent,Hkv", [(128, 128, False, 8), (64, 32, True, 2), (128, 64, False, 1), (64, 64, False, 40)])
-@pytest.mark.parametrize("new", [[1] * 7, [0, 70, 1, 16, 3, 33, 5], [0, 0, 0, 0, 0, 0, 300]])
+@pytest.mark.parametrize("d,rot,adjacent,Hkv", [(128, 128, False, 8), (64, 32, True, 2), (128, 64, False, 1), (64, 64, False, 40), (128, 128, False, 112)])
+@pytest.mark.parametrize("new", [[1] * 7, [1, 0, 1, 1, 0, 0, 1], [0, 70, 1, 16, 3, 33, 5], [0, 0, 0, 0, 0, 0, 300]])
 @pytest.mark.parametrize("with_positions", [True, False])
 def test_fused_appends_are_the_two_calls(d, rot, adjacent, Hkv, new, with_positions):
     import paper_2609_35158_b200 as pd
 
-    Hq = 2 * Hkv
+    Hq = Hkv if Hkv > 100 else 2 * Hkv
     before, new = np.array([0, 5, 16, 31, 47, 3, 8], np.int32), np.array(new, np.int32)
     after = before + new
     indptr, pos, q, k, v = packed(before, new, 20, Hq, Hkv, d, 3)
@@ -156,7 +156,7 @@ def test_refusals():
     nan_freq.inv_freq[3] = float("nan")
     axis9.axis_of_pair[15] = 1
     far.inv_freq[0] = 403.0
-    with Ctx(4, 2, 64, 2, 4, 8) as ctx, Ctx(256, 256, 128, 1, 1, 1) as wide:
+    with Ctx(4, 2, 64, 2, 4, 8) as ctx, Ctx(113, 113, 128, 1, 1, 1) as wide:
         h = ctx.h
         n0 = pd.pd_launch_count(h)
         for c in (cfg(rot_dim=0), cfg(rot_dim=80), cfg(num_axes=0), cfg(num_axes=5), cfg(adjacent=2), cfg(magnitude=float("inf")),
