@@ -3,11 +3,11 @@
 //
 // Both kernels are a pass over the tokens bound by their bytes: a token of one KV head is 4 D bytes of bf16 (K and V)
 // and 9 D / 8 bytes of 4-bit page. Writing, four lanes carry a group of 64 values (16 each: what a group costs beside its
-// values is paid once per 16); reading back, eight do (8 each: one 16-byte store, whole 32-byte sectors per warp). A CTA takes the
-// tokens of one page: lane groups sit on its slots (rounded up to a power of two, so that a single token spreads over the
-// KV heads instead of idling 15 of 16 groups) and walk the KV heads.
-// The pages of all sequences form one list that the CTAs share out evenly: each CTA sums the sequences' page counts itself
-// (a grid of CTAs per sequence instead left short sequences' CTAs idle, and where the host knows no lengths it had to
+// values is paid once per 16); reading back, eight do (8 each: one 16-byte store, whole 32-byte sectors per warp). A CTA takes 16
+// packed tokens, or the tokens of one page: lane groups sit on them (rounded up to a power of two, so that a single token
+// spreads over the KV heads instead of idling 15 of 16 groups) and walk the KV heads.
+// The work forms one list that the CTAs share out evenly. Writing, that is the packed tokens; reading back, the pages of all
+// sequences, whose counts each CTA sums itself (a grid of CTAs per sequence instead left short sequences' CTAs idle, and where the host knows no lengths it had to
 // launch CTAs for every page a sequence could have: 12.2 against 5.5 us to write one token of 64 sequences and read it back).
 // Measured for 4 x 32768 tokens at 8 KV heads, head_dim 128: written in 134 us (670 MB, 0.78 of the copy bandwidth), read back
 // in 117 us (688 MB, 0.91).
@@ -36,6 +36,16 @@ struct PageShare {
 __device__ __forceinline__ PageShare share_page(int nt, int groups) {
     const int shift = nt <= 1 ? 0 : 32 - __clz(nt - 1);
     return {shift, groups >> shift};
+}
+
+// The sequence whose part of a list holds entry x: the last one that begins at or before it (starts[0] <= x).
+__device__ __forceinline__ int owner(const int32_t *starts, int B, int x) {
+    int lo = 0, hi = B - 1;
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (starts[mid] <= x) lo = mid; else hi = mid - 1;
+    }
+    return lo;
 }
 
 // Exclusive prefix sums of count(b), b < B, into cum[0 .. B] (shared memory); every thread of the CTA takes part.
@@ -67,80 +77,77 @@ __device__ void prefix_sums(int B, int32_t *cum, int32_t *warp_sums, Count count
     __syncthreads();
 }
 
-// The sequence whose part of the list holds entry x < cum[B].
-__device__ __forceinline__ int owner(const int32_t *cum, int B, int x) {
-    int lo = 0, hi = B - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (cum[mid] <= x) lo = mid; else hi = mid - 1;
-    }
-    return lo;
-}
-
-// SINGLE: one token per sequence and one CTA each, which also advances the length; otherwise packed tokens.
+// SINGLE: one token per sequence and one CTA each, which also advances the length; otherwise CTAs take 16 packed tokens at a
+// time. Where a token's values lie follows from its row alone, so they are on their way while its sequence is looked for.
 template <int D, bool SINGLE>
-__global__ void __launch_bounds__(kThreads) kv_append_q4_kernel(const AppendQ4Params p) {
+__global__ void __launch_bounds__(kThreads, 5) kv_append_q4_kernel(const AppendQ4Params p) {
     constexpr int LANES = D / 16;  // lanes per row
-    __shared__ int32_t cum[SINGLE ? 1 : kMaxBatch + 1], warp_sums[kThreads / 32];
+    static_assert(kThreads / LANES >= 2 * kPageSize, "K and V of 16 tokens side by side: the hop below is at least one");
     const int j = threadIdx.x % LANES, sub = threadIdx.x / LANES;
     grid_dependency_wait();
     launch_dependents();
-    if (!SINGLE) {
-        prefix_sums(p.B, cum, warp_sums, [&](int b) {
-            const int n = p.q_indptr[b + 1] - p.q_indptr[b], L = p.ctx_lens[b];
-            if (n <= 0) return 0;
-            if (L < 0 || L > p.MP * kPageSize - n) {
-                if (blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);
-                return 0;
-            }
-            return (L + n - 1) / kPageSize - L / kPageSize + 1;
-        });
-    }
-    const int total = SINGLE ? p.B : cum[p.B];
-    for (int x = blockIdx.x; x < total; x += gridDim.x) {
-        const int b = SINGLE ? x : owner(cum, p.B, x);
-        const int r0 = p.q_indptr != nullptr ? p.q_indptr[b] : b, n = p.q_indptr != nullptr ? p.q_indptr[b + 1] - r0 : 1;
-        const int L = p.ctx_lens[b];
-        if (SINGLE) {
-            __syncthreads();  // everyone has read the length before thread 0 advances it
-            if (n <= 0) continue;
-            if (n != 1 || L < 0 || L >= p.MP * kPageSize) {
-                if (threadIdx.x == 0) latch(p.status, kDevBadLength, b, L);
-                continue;
-            }
-        }
-        const int pg = L / kPageSize + (SINGLE ? 0 : x - cum[b]);
-        const int page = p.page_table[static_cast<size_t>(b) * p.MP + pg];
-        const bool ok = page >= 0 && page < p.num_pages;
-        if (!ok && threadIdx.x == 0) latch(p.status, kDevBadPage, b, page);
-        // the length of a packed token with a bad page grows all the same, as in the bf16 append
-        if (SINGLE && p.advance && threadIdx.x == 0 && (ok || p.q_indptr != nullptr)) p.ctx_lens[b] = L + 1;
-        if (!ok) continue;
-        const int t0 = max(pg * kPageSize, L), nt = min(pg * kPageSize + kPageSize, L + n) - t0;
+    const int begin = SINGLE ? 0 : p.q_indptr[0], end = SINGLE ? p.B : p.q_indptr[p.B];
+    constexpr int TILE = SINGLE ? 1 : kPageSize;
+    for (int t0 = begin + static_cast<int>(blockIdx.x) * TILE; t0 < end; t0 += static_cast<int>(gridDim.x) * TILE) {
+        const int nt = min(TILE, end - t0);
         const PageShare sh = share_page(nt, kThreads / LANES);
-        const int t = sub & ((1 << sh.shift) - 1), slot = (t0 + min(t, nt - 1)) % kPageSize;
-        const size_t row = static_cast<size_t>(r0 + t0 - L + min(t, nt - 1)) * p.Hkv;
-        // items: K and V of the KV heads in turn. Lanes without an item of their own follow along on another's: the shuffles
-        // want whole warps. The next item's values are on their way while one is worked on.
+        const int t = min(sub & ((1 << sh.shift) - 1), nt - 1);
+        const size_t row = static_cast<size_t>(SINGLE && p.q_indptr != nullptr ? p.q_indptr[t0] : t0 + t) * p.Hkv;
+        // Items: K and V of the KV heads in turn. The step is even, so a lane stays with K or with V. Lanes without an item of their
+        // own follow along on another's: the shuffles want whole warps. The next item's values are on their way while one is
+        // worked on.
+        const int item = sub >> sh.shift, which = item & 1, hop = sh.step >> 1;
+        const __nv_bfloat16 *first = (which ? p.v_new : p.k_new) + row * D + j * 16;
+        const __nv_bfloat16 *src = first + static_cast<size_t>(item >> 1) * D;
         uint4 x0, x1;
-        auto load = [&](int i) {
-            const int item = min(i, 2 * p.Hkv - 1);
-            const uint4 *src = reinterpret_cast<const uint4 *>(((item & 1) ? p.v_new : p.k_new) + (row + (item >> 1)) * D + j * 16);
-            x0 = __ldg(src);
-            x1 = __ldg(src + 1);
+        auto load = [&](bool live) {
+            const uint4 *from = reinterpret_cast<const uint4 *>(live ? src : first);
+            x0 = __ldg(from);
+            x1 = __ldg(from + 1);
         };
-        int i = sub >> sh.shift;
-        load(i);
-        for (int i0 = 0; i0 < 2 * p.Hkv; i0 += sh.step, i += sh.step) {
+        int h = item >> 1;
+        if (!SINGLE) load(h < p.Hkv);
+
+        int b = t0, n = 1;
+        if (!SINGLE) {
+            b = owner(p.q_indptr, p.B, t0 + t);
+            n = p.q_indptr[b + 1] - p.q_indptr[b];
+        } else if (p.q_indptr != nullptr) {
+            n = p.q_indptr[b + 1] - p.q_indptr[b];
+        }
+        const int L = p.ctx_lens[b];
+        if (SINGLE) __syncthreads();  // everyone has read the length before thread 0 advances it
+        if (SINGLE && n <= 0) continue;
+        const int pos = SINGLE ? L : L + (t0 + t - p.q_indptr[b]);
+        const bool room = L >= 0 && L <= p.MP * kPageSize - n && pos >= 0 && pos < p.MP * kPageSize && (!SINGLE || n == 1);
+        int page = -1;
+        if (room) page = p.page_table[static_cast<size_t>(b) * p.MP + pos / kPageSize];
+        const bool ok = page >= 0 && page < p.num_pages;
+        if (!ok && j == 0) latch(p.status, room ? kDevBadPage : kDevBadLength, b, room ? page : L);
+        // the length of a packed token with a bad page grows all the same, as in the bf16 append
+        if (SINGLE && p.advance && threadIdx.x == 0 && room && (ok || p.q_indptr != nullptr)) p.ctx_lens[b] = L + 1;
+        if (SINGLE && !ok) continue;
+        if (SINGLE) load(h < p.Hkv);
+
+        const bool mine = ok && (sub & ((1 << sh.shift) - 1)) < nt;
+        const int slot = pos & (kPageSize - 1);
+        uint8_t *block = p.kv4 + (static_cast<size_t>(ok ? page : 0) * p.Hkv + (item >> 1)) * q4_block_bytes<D>();
+        uint2 *codes_at = reinterpret_cast<uint2 *>(q4_codes_at<D>(block, which, slot, 2 * j));
+        uint32_t *rec_at = q4_record_at<D>(block, which, slot, 2 * j);
+        for (int h0 = 0; h0 < p.Hkv; h0 += hop) {
             const uint4 y0 = x0, y1 = x1;
-            if (i0 + sh.step < 2 * p.Hkv) load(i + sh.step);
+            const bool live = mine && h < p.Hkv;
+            h += hop;
+            src += static_cast<size_t>(hop) * D;
+            if (h0 + hop < p.Hkv) load(h < p.Hkv);
             uint32_t rec;
             const uint2 codes = q4_quantize16(y0, y1, rec);
-            if (t < nt && i < 2 * p.Hkv) {
-                uint8_t *block = p.kv4 + (static_cast<size_t>(page) * p.Hkv + (i >> 1)) * q4_block_bytes<D>();
-                *reinterpret_cast<uint2 *>(q4_codes_at<D>(block, i & 1, slot, 2 * j)) = codes;
-                if ((j & 3) == 0) *q4_record_at<D>(block, i & 1, slot, 2 * j) = rec;
+            if (live) {
+                *codes_at = codes;
+                if ((j & 3) == 0) *rec_at = rec;
             }
+            codes_at += static_cast<size_t>(hop) * (q4_block_bytes<D>() / 8);
+            rec_at += static_cast<size_t>(hop) * (q4_block_bytes<D>() / 4);
         }
     }
 }
@@ -197,8 +204,7 @@ cudaError_t launch_kv_append_q4(const AppendQ4Params &p, int max_q_len, int num_
     if (p.B == 0 || max_q_len <= 0) return cudaSuccess;
     auto go = [&](auto *k, int grid) { return launch_pdl(k, dim3(grid), dim3(kThreads), 0, stream, p.pdl != 0, p); };
     const bool single = max_q_len == 1;
-    // max_q_len tokens that start inside a page touch one page more than they fill
-    const int grid = single ? p.B : ctas(static_cast<int64_t>(p.B) * ((max_q_len + kPageSize - 2) / kPageSize + 1), num_sms * 40);
+    const int grid = single ? p.B : ctas((static_cast<int64_t>(p.B) * max_q_len + kPageSize - 1) / kPageSize, num_sms * 40);
     const cudaError_t err = single ? (p.D == 128 ? go(kv_append_q4_kernel<128, true>, grid) : go(kv_append_q4_kernel<64, true>, grid))
                                    : (p.D == 128 ? go(kv_append_q4_kernel<128, false>, grid) : go(kv_append_q4_kernel<64, false>, grid));
     if (err != cudaSuccess) return err;

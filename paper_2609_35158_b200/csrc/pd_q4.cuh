@@ -88,11 +88,10 @@ __device__ __forceinline__ uint2 q4_quantize16(const uint4 &x0, const uint4 &x1,
     rec = (__float_as_uint(s) >> 16) | (bad ? 0u : __float_as_uint(lo) & 0xffff0000u);
     uint32_t out[2];
     if (s <= 18446744073709551616.f) {
-        float inv = 0.f, inv_lo = 0.f;  // scale 0: codes 0
-        if (s > 0.f) {
-            asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
-            inv_lo = __fmul_rn(__fmaf_rn(-s, inv, 1.f), inv);
-        }
+        float inv;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+        inv = s > 0.f ? inv : 0.f;  // scale 0: codes 0
+        const float inv_lo = __fmul_rn(__fmaf_rn(-s, inv, 1.f), inv);
         const uint64_t base2 = f32x2(-lo, -lo), inv2 = f32x2(inv, inv), lo2 = f32x2(inv_lo, inv_lo), round2 = f32x2(12582912.f, 12582912.f);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
