@@ -726,7 +726,7 @@ int decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *p
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
     if (!ctx->q4_ready) {
-        const cudaError_t e = pd::prepare_decode_attn_q4(ctx->cfg.head_dim);
+        const cudaError_t e = pd::prepare_decode_attn_q4(ctx->cfg.head_dim, ctx->group);
         if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "4-bit decode kernel attribute", e);
         ctx->q4_ready = true;
     }

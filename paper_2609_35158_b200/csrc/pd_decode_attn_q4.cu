@@ -23,11 +23,15 @@
 //     tensor core in fp16, of which weights below 2^-16 of the largest start to lose bits (under 2^-27 of the largest
 //     for each). Taking the product and not p or sv alone keeps a token of huge scale and vanishing probability from
 //     pushing the others out of range. The check in the loop is conservative (p and sv against caps whose product is
-//     2^15) and the exact one runs only when it fires.
+//     2^15) and the exact one runs only when it fires;
+//   * with at most four query heads per KV head (PACK = 2) the eight columns of a product are four heads of one page and the same
+//     four of the next: both pages' products go into one accumulator, each with zeros in the other's columns, and the
+//     softmax between the products costs two pages what it cost one. O has both pages' sums apart and adds them at the end
+//     (134 -> 130 us on 64 contexts of 2K-16K at 32/8 heads, 79 -> 73 us at head_dim 64; both under the power limit).
 // Sums, statistics, O and the rank-one terms are fp32.
 //
-// Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, about 200 per page at
-// head_dim 128. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
+// Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, 187 per page at head_dim 128 and four
+// heads, 205 at eight. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
 // reference for V beside the softmax maximum 193; two pages, one reference, minima by mma, bytes as V operands 147;
 // independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119,
 // which is 0.93 of the copy bandwidth (126, 0.88, when it runs for long and the power limit takes the SM clock to about
@@ -69,6 +73,12 @@ __device__ __forceinline__ void mma_bf16_from(float (&c)[4], uint32_t a0, uint32
         : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
         : "r"(a0), "r"(a1), "r"(b0), "f"(from_a), "f"(from_b));
 }
+// The same with 16 columns of A, the second eight those of the first again.
+__device__ __forceinline__ void mma_bf16_from_twice(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t b0, uint32_t b1, float from_a, float from_b) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%4,%5}, {%6,%7}, {%8,%9,%8,%9};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(b0), "r"(b1), "f"(from_a), "f"(from_b));
+}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
@@ -88,7 +98,9 @@ __device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void *src, ui
 }
 constexpr uint32_t kNib0 = 0x000f000fu, kNib1 = 0x00f000f0u;
 
-template <int D, int WARPS, int STAGES, int TP>
+// PACK = 2 (groups of at most four heads): the eight columns of the products are four heads of one page and the same four of the
+// next, see the top of the file.
+template <int D, int WARPS, int STAGES, int TP, int PACK>
 __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(const AttnParams p) {
     static_assert(D == 64 || D == 128, "head_dim 64 or 128");
     constexpr int THREADS = WARPS * 32;
@@ -96,6 +108,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     constexpr int STAGE = TP * BLOCK;
     constexpr int PIECES = D / 32;       // 16-byte pieces of a row
     constexpr int GROUPS = D / kQ4Group;
+    constexpr int SETS = TP / PACK;      // pages, or pairs of pages, whose softmax is worked on together
+    constexpr int COLS = 8 / PACK;       // heads per page among the columns
+    constexpr int HEAD_LANES = COLS / 2;  // lanes of a quad that hold different heads
     constexpr int WINDOW = 32 / TP * TP;  // page ids held one per lane, whole tiles of them
 
     extern __shared__ uint8_t smem_raw[];
@@ -221,14 +236,19 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     for (int s = 0; s < STAGES; ++s) issue_next();
 
     // ---- reading side
-    const int quad_row = lane >> 2, quad_t = lane & 3, quad_col = quad_t * 2;
+    const int quad_row = lane >> 2, quad_t = lane & 3;
+    // columns 2 t and 2 t + 1 of the accumulators: heads quad_col (a) and quad_col + 1 (b) of a set's page my_page
+    const int quad_col = quad_t * 2 % COLS, my_page = quad_t * 2 / COLS;
+    // column g of a B operand: head b_head of the set's page b_page
+    const int b_head = quad_row % COLS, b_page = quad_row / COLS;
     const int G = p.G;
     // ldmatrix source rows: matrices 0 / 1 = slots 0-7 / 8-15 of a piece, 2 / 3 = the same of the next piece
     const int ld_slot = ((lane >> 3) & 1) * 8 + (lane & 7), ld_piece = lane >> 4;
     uint32_t ld_off[GROUPS];
 #pragma unroll
     for (int g = 0; g < GROUPS; ++g) ld_off[g] = ld_slot * (D / 2) + q4_piece_pos<D>(2 * g + ld_piece, ld_slot) * 16;
-    const uint32_t rec_off = 16 * D + quad_row * (D / 8);
+    const uint32_t rec_off = my_page * BLOCK + 16 * D + quad_row * (D / 8);
+    const uint32_t first_page = b_page == 0 ? 0xffffffffu : 0u;
     int stage = 0;
     uint32_t parity = 0;
     bool alive = true;
@@ -245,12 +265,15 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
             const int L = clamp_len(__ldg(p.ctx_lens + cur.b), p.MP);
             int rem = min(L - page0 * kPageSize, pages * kPageSize);  // tokens of the segment still to come
 
-            // Q^T as the fp16 B operand, head quad_row: register j of piece c holds d = 32 c + 8 t + j and + 4 (odd j: / 16)
-            uint32_t qb[PIECES][4];
-            uint32_t qsum;  // B operand of the minima: sum(q) by group in three bf16 parts, part t in lane t
+            // Q^T as the fp16 B operand for each page of a set (zero in the other page's columns), head b_head: register j of
+            // piece c holds d = 32 c + 8 t + j and + 4 (odd j: / 16)
+            uint32_t qb[PACK][PIECES][4];
+            // B operand of the minima: sum(q) by group in three bf16 parts, for PACK = 1 part t in lane t. For two pages lanes
+            // 0, 1 meet the first page's minima and 2, 3 the second's, with two rows each: parts 0 and 1, part 2 and 0.
+            uint32_t qsum[PACK];
             float unit_a, unit_b;
             {
-                const __nv_bfloat16 *qrow = p.q + (static_cast<size_t>(cur.b) * p.Hq + cur.kvh * G + quad_row) * D;
+                const __nv_bfloat16 *qrow = p.q + (static_cast<size_t>(cur.b) * p.Hq + cur.kvh * G + b_head) * D;
                 uint4 x[PIECES];
                 float amax = 0.f, sum[GROUPS];
 #pragma unroll
@@ -258,7 +281,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
                     x[c] = make_uint4(0u, 0u, 0u, 0u);
-                    if (quad_row < G) x[c] = __ldg(reinterpret_cast<const uint4 *>(qrow + c * 32 + quad_t * 8));
+                    if (b_head < G) x[c] = __ldg(reinterpret_cast<const uint4 *>(qrow + c * 32 + quad_t * 8));
                     const uint32_t w[4] = {x[c].x, x[c].y, x[c].z, x[c].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
@@ -277,23 +300,32 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 const float up = pow2_int(e), up16 = pow2_int(e - 4);
 #pragma unroll
                 for (int c = 0; c < PIECES; ++c) {
-                    qb[c][0] = half2_bits(bf16_lo(x[c].x) * up, bf16_lo(x[c].z) * up);
-                    qb[c][1] = half2_bits(bf16_hi(x[c].x) * up16, bf16_hi(x[c].z) * up16);
-                    qb[c][2] = half2_bits(bf16_lo(x[c].y) * up, bf16_lo(x[c].w) * up);
-                    qb[c][3] = half2_bits(bf16_hi(x[c].y) * up16, bf16_hi(x[c].w) * up16);
+                    const uint32_t r[4] = {half2_bits(bf16_lo(x[c].x) * up, bf16_lo(x[c].z) * up), half2_bits(bf16_hi(x[c].x) * up16, bf16_hi(x[c].z) * up16),
+                                           half2_bits(bf16_lo(x[c].y) * up, bf16_lo(x[c].w) * up), half2_bits(bf16_hi(x[c].y) * up16, bf16_hi(x[c].w) * up16)};
+#pragma unroll
+                    for (int k = 0; k < PACK; ++k)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) qb[k][c][i] = PACK == 1 || b_page == k ? r[i] : 0u;
                 }
                 // the scale of a head is wanted by the lanes whose accumulator columns it is
                 unit_a = p.scale_log2 * pow2_int(24 - __shfl_sync(0xffffffffu, e, quad_col * 4));
                 unit_b = p.scale_log2 * pow2_int(24 - __shfl_sync(0xffffffffu, e, quad_col * 4 + 4));
-                float part[2] = {0.f, 0.f};
+                float part[3][2] = {{0.f, 0.f}, {0.f, 0.f}, {0.f, 0.f}};
 #pragma unroll
                 for (int g = 0; g < GROUPS; ++g) {
                     const float s = sum[g] * p.scale_log2;
-                    const float hi = __bfloat162float(__float2bfloat16(s));
-                    const float mid = __bfloat162float(__float2bfloat16(s - hi));
-                    part[g] = quad_t == 0 ? hi : (quad_t == 1 ? mid : (quad_t == 2 ? s - hi - mid : 0.f));
+                    part[0][g] = __bfloat162float(__float2bfloat16(s));
+                    part[1][g] = __bfloat162float(__float2bfloat16(s - part[0][g]));
+                    part[2][g] = s - part[0][g] - part[1][g];
                 }
-                qsum = pack_bf16x2(part[0], part[1]);
+                const uint32_t parts[3] = {pack_bf16x2(part[0][0], part[0][1]), pack_bf16x2(part[1][0], part[1][1]), pack_bf16x2(part[2][0], part[2][1])};
+                if (PACK == 1) {
+                    qsum[0] = quad_t == 0 ? parts[0] : (quad_t == 1 ? parts[1] : (quad_t == 2 ? parts[2] : 0u));
+                } else {
+                    const bool own = quad_t >> 1 == b_page;
+                    qsum[0] = own ? (quad_t & 1 ? parts[2] : parts[0]) : 0u;
+                    qsum[PACK - 1] = own && !(quad_t & 1) ? parts[1] : 0u;
+                }
             }
             // O^T, piece c, j: rows d = 32 c + 4 g + 2 j (registers 0, 1 for heads a, b); registers 2, 3: that plus 16 times d + 1
             float O[PIECES][2][4], Ma[GROUPS], Mb[GROUPS];
@@ -311,85 +343,99 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 const uint32_t base = ring + stage * STAGE;
                 const uint8_t *recs = aligned + (base - ring0) + rec_off;
 
-                // records of slots g (i = 0) and g + 8 (i = 1): words {k_scale, k_min}, {v_scale, v_min} by group
-                uint32_t rk[TP][2][GROUPS], rv[TP][2][GROUPS];
+                // records of slots g (i = 0) and g + 8 (i = 1) of this lane's page: {k_scale, k_min}, {v_scale, v_min} by group
+                uint32_t rk[SETS][2][GROUPS], rv[SETS][2][GROUPS];
 #pragma unroll
-                for (int t = 0; t < TP; ++t)
+                for (int u = 0; u < SETS; ++u)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        const uint8_t *at = recs + t * BLOCK + i * D;  // 8 slots of D / 8 bytes
+                        const uint8_t *at = recs + u * PACK * BLOCK + i * D;  // 8 slots of D / 8 bytes
                         if (GROUPS == 2) {
                             const uint4 w = *reinterpret_cast<const uint4 *>(at);
-                            rk[t][i][0] = w.x; rv[t][i][0] = w.y; rk[t][i][GROUPS - 1] = w.z; rv[t][i][GROUPS - 1] = w.w;
+                            rk[u][i][0] = w.x; rv[u][i][0] = w.y; rk[u][i][GROUPS - 1] = w.z; rv[u][i][GROUPS - 1] = w.w;
                         } else {
                             const uint2 w = *reinterpret_cast<const uint2 *>(at);
-                            rk[t][i][0] = w.x; rv[t][i][0] = w.y;
+                            rk[u][i][0] = w.x; rv[u][i][0] = w.y;
                         }
                     }
+                const bool tail = rem < TP * kPageSize;
+                // Codes of empty slots are harmless numbers, their records may be anything. What a slot's own columns make of them is
+                // overwritten below, but the minima of one page of a pair also meet the other's columns, with a factor of 0.
+                if (PACK > 1 && tail) {
+#pragma unroll
+                    for (int u = 0; u < SETS; ++u)
+#pragma unroll
+                        for (int i = 0; i < 2; ++i)
+                            if ((u * PACK + my_page) * kPageSize + i * 8 + quad_row >= rem) {
+#pragma unroll
+                                for (int g = 0; g < GROUPS; ++g) rk[u][i][g] = 0u;
+                            }
+                }
 
                 // x = S - r in log2 units, [slot g: heads a, b; slot g + 8: heads a, b]
-                float x[TP][4];
+                float x[SETS][4];
                 {
                     uint32_t w[TP][GROUPS][4];  // (slots 0-7, 8-15) of piece 2 g, then of piece 2 g + 1
-                    float acc[TP][4], A[TP][GROUPS][4];
+                    float acc[SETS][4], A[SETS][GROUPS][4];
 #pragma unroll
                     for (int t = 0; t < TP; ++t)
 #pragma unroll
-                        for (int g = 0; g < GROUPS; ++g) {
+                        for (int g = 0; g < GROUPS; ++g)
                             ldmatrix_x4(w[t][g][0], w[t][g][1], w[t][g][2], w[t][g][3], base + t * BLOCK + ld_off[g]);
-                        }
 #pragma unroll
-                    for (int t = 0; t < TP; ++t) {
-                        if (GROUPS == 2)
-                            mma_bf16_from(acc[t], __byte_perm(rk[t][0][0], rk[t][0][GROUPS - 1], 0x7632),
-                                          __byte_perm(rk[t][1][0], rk[t][1][GROUPS - 1], 0x7632), qsum, nr_a, nr_b);
-                        else
-                            mma_bf16_from(acc[t], rk[t][0][0] >> 16, rk[t][1][0] >> 16, qsum, nr_a, nr_b);
+                    for (int u = 0; u < SETS; ++u) {
+                        const uint32_t k0 = GROUPS == 2 ? __byte_perm(rk[u][0][0], rk[u][0][GROUPS - 1], 0x7632) : rk[u][0][0] >> 16;
+                        const uint32_t k1 = GROUPS == 2 ? __byte_perm(rk[u][1][0], rk[u][1][GROUPS - 1], 0x7632) : rk[u][1][0] >> 16;
+                        if (PACK == 1) mma_bf16_from(acc[u], k0, k1, qsum[0], nr_a, nr_b);
+                        else mma_bf16_from_twice(acc[u], k0, k1, qsum[0], qsum[PACK - 1], nr_a, nr_b);
                     }
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)  // piece 2 g + h / 2, its even (h = 0, 2) and odd bytes
+                    for (int k = 0; k < PACK; ++k)
 #pragma unroll
-                        for (int t = 0; t < TP; ++t)
+                        for (int h = 0; h < 4; ++h)  // piece 2 g + h / 2, its even (h = 0, 2) and odd bytes
 #pragma unroll
-                            for (int g = 0; g < GROUPS; ++g) {
-                                const uint32_t u = w[t][g][h & 2] >> (8 * (h & 1)), v = w[t][g][(h & 2) + 1] >> (8 * (h & 1));
-                                const uint32_t b0 = qb[2 * g + (h >> 1)][2 * (h & 1)], b1 = qb[2 * g + (h >> 1)][2 * (h & 1) + 1];
-                                if (h == 0) mma_f16_from_zero(A[t][g], u & kNib0, v & kNib0, u & kNib1, v & kNib1, b0, b1);
-                                else mma_f16(A[t][g], u & kNib0, v & kNib0, u & kNib1, v & kNib1, b0, b1);
-                            }
+                            for (int u = 0; u < SETS; ++u)
 #pragma unroll
-                    for (int t = 0; t < TP; ++t) {
+                                for (int g = 0; g < GROUPS; ++g) {
+                                    const int t = u * PACK + k, c = 2 * g + (h >> 1);
+                                    const uint32_t lo = w[t][g][h & 2] >> (8 * (h & 1)), hi = w[t][g][(h & 2) + 1] >> (8 * (h & 1));
+                                    const uint32_t b0 = qb[k][c][2 * (h & 1)], b1 = qb[k][c][2 * (h & 1) + 1];
+                                    if (h == 0 && k == 0) mma_f16_from_zero(A[u][g], lo & kNib0, hi & kNib0, lo & kNib1, hi & kNib1, b0, b1);
+                                    else mma_f16(A[u][g], lo & kNib0, hi & kNib0, lo & kNib1, hi & kNib1, b0, b1);
+                                }
+#pragma unroll
+                    for (int u = 0; u < SETS; ++u) {
                         float sum[4];
 #pragma unroll
                         for (int g = 0; g < GROUPS; ++g) {
-                            const float s0 = bf16_lo(rk[t][0][g]), s1 = bf16_lo(rk[t][1][g]);
-                            sum[0] = g == 0 ? A[t][g][0] * s0 : fmaf(A[t][g][0], s0, sum[0]);
-                            sum[1] = g == 0 ? A[t][g][1] * s0 : fmaf(A[t][g][1], s0, sum[1]);
-                            sum[2] = g == 0 ? A[t][g][2] * s1 : fmaf(A[t][g][2], s1, sum[2]);
-                            sum[3] = g == 0 ? A[t][g][3] * s1 : fmaf(A[t][g][3], s1, sum[3]);
+                            const float s0 = bf16_lo(rk[u][0][g]), s1 = bf16_lo(rk[u][1][g]);
+                            sum[0] = g == 0 ? A[u][g][0] * s0 : fmaf(A[u][g][0], s0, sum[0]);
+                            sum[1] = g == 0 ? A[u][g][1] * s0 : fmaf(A[u][g][1], s0, sum[1]);
+                            sum[2] = g == 0 ? A[u][g][2] * s1 : fmaf(A[u][g][2], s1, sum[2]);
+                            sum[3] = g == 0 ? A[u][g][3] * s1 : fmaf(A[u][g][3], s1, sum[3]);
                         }
-                        x[t][0] = fmaf(sum[0], unit_a, acc[t][0]);
-                        x[t][1] = fmaf(sum[1], unit_b, acc[t][1]);
-                        x[t][2] = fmaf(sum[2], unit_a, acc[t][2]);
-                        x[t][3] = fmaf(sum[3], unit_b, acc[t][3]);
+                        x[u][0] = fmaf(sum[0], unit_a, acc[u][0]);
+                        x[u][1] = fmaf(sum[1], unit_b, acc[u][1]);
+                        x[u][2] = fmaf(sum[2], unit_a, acc[u][2]);
+                        x[u][3] = fmaf(sum[3], unit_b, acc[u][3]);
                     }
                 }
-                if (rem < TP * kPageSize) {  // codes of empty slots are harmless numbers, their records may be anything
+                if (tail) {
 #pragma unroll
-                    for (int t = 0; t < TP; ++t)
+                    for (int u = 0; u < SETS; ++u)
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
-                            if (t * kPageSize + i * 8 + quad_row >= rem) {
-                                x[t][2 * i] = -INFINITY;
-                                x[t][2 * i + 1] = -INFINITY;
+                            if ((u * PACK + my_page) * kPageSize + i * 8 + quad_row >= rem) {
+                                x[u][2 * i] = -INFINITY;
+                                x[u][2 * i + 1] = -INFINITY;
 #pragma unroll
-                                for (int g = 0; g < GROUPS; ++g) rv[t][i][g] = 0u;
+                                for (int g = 0; g < GROUPS; ++g) rv[u][i][g] = 0u;
                             }
                 }
 
                 float xm_a = x[0][0], xm_b = x[0][1], vm = 0.f;
 #pragma unroll
-                for (int t = 0; t < TP; ++t) {
+                for (int t = 0; t < SETS; ++t) {
                     xm_a = max3(xm_a, x[t][0], x[t][2]);
                     xm_b = max3(xm_b, x[t][1], x[t][3]);
 #pragma unroll
@@ -400,7 +446,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                     // (the codes no longer matter then), and p itself stays below 2^100
                     float w_a = xm_a - 100.f, w_b = xm_b - 100.f;
 #pragma unroll
-                    for (int t = 0; t < TP; ++t)
+                    for (int t = 0; t < SETS; ++t)
 #pragma unroll
                         for (int i = 0; i < 2; ++i) {
                             float v = 0.f;
@@ -412,7 +458,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                             w_b = fmaxf(w_b, x[t][2 * i + 1] + lv);
                         }
 #pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) {
+                    for (int o = HEAD_LANES; o < 32; o <<= 1) {  // the lanes that hold the same heads
                         w_a = fmaxf(w_a, __shfl_xor_sync(0xffffffffu, w_a, o));
                         w_b = fmaxf(w_b, __shfl_xor_sync(0xffffffffu, w_b, o));
                     }
@@ -436,7 +482,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                             O[c][j][1] *= f_b; O[c][j][3] *= f_b;
                         }
 #pragma unroll
-                    for (int t = 0; t < TP; ++t) {
+                    for (int t = 0; t < SETS; ++t) {
                         x[t][0] -= up_a; x[t][2] -= up_a;
                         x[t][1] -= up_b; x[t][3] -= up_b;
                     }
@@ -447,9 +493,9 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 }
 
                 // weights, their sums, and the fp16 B operands: P^T transposed from (slot x head) to (head x slot)
-                uint32_t pb[TP][GROUPS][2];
+                uint32_t pb[SETS][GROUPS][2];
 #pragma unroll
-                for (int t = 0; t < TP; ++t) {
+                for (int t = 0; t < SETS; ++t) {
                     const float p0 = fast_exp2(x[t][0]), p1 = fast_exp2(x[t][1]), p2 = fast_exp2(x[t][2]), p3 = fast_exp2(x[t][3]);
                     l_a += p0 + p2;
                     l_b += p1 + p3;
@@ -473,22 +519,40 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 --inflight;
                 issue_next();
 #pragma unroll
-                for (int t = 0; t < TP; ++t)
+                for (int u = 0; u < SETS; ++u)
 #pragma unroll
-                    for (int h = 0; h < 4; ++h)
+                    for (int k = 0; k < PACK; ++k) {
+                        // of a pair's weights, those of page k: the other page's columns must add nothing
+                        uint32_t pk[GROUPS][2];
 #pragma unroll
-                        for (int g = 0; g < GROUPS; ++g) {
-                            const uint32_t u = w[t][g][h & 2], v = w[t][g][(h & 2) + 1];  // slots 2t, 2t+1 and 2t+8, 2t+9; four consecutive d each
-                            const uint32_t pick = (h & 1) ? 0x4341u : 0x4240u;            // d + 2, d + 3 or d, d + 1
-                            const uint32_t ub = __byte_perm(u, 0u, pick), vb = __byte_perm(v, 0u, pick);
-                            mma_f16(O[2 * g + (h >> 1)][h & 1], ub & kNib0, ub, vb & kNib0, vb, pb[t][g][0], pb[t][g][1]);
-                        }
+                        for (int g = 0; g < GROUPS; ++g)
+#pragma unroll
+                            for (int i = 0; i < 2; ++i) pk[g][i] = PACK == 1 ? pb[u][g][i] : pb[u][g][i] & (k == 0 ? first_page : ~first_page);
+#pragma unroll
+                        for (int h = 0; h < 4; ++h)
+#pragma unroll
+                            for (int g = 0; g < GROUPS; ++g) {
+                                const int t = u * PACK + k;
+                                const uint32_t lo = w[t][g][h & 2], hi = w[t][g][(h & 2) + 1];  // slots 2t, 2t+1 and 2t+8, 2t+9; four consecutive d each
+                                const uint32_t pick = (h & 1) ? 0x4341u : 0x4240u;              // d + 2, d + 3 or d, d + 1
+                                const uint32_t lb = __byte_perm(lo, 0u, pick), hb = __byte_perm(hi, 0u, pick);
+                                mma_f16(O[2 * g + (h >> 1)][h & 1], lb & kNib0, lb, hb & kNib0, hb, pk[g][0], pk[g][1]);
+                            }
+                    }
                 if (++stage == STAGES) { stage = 0; parity ^= 1u; }
             }
             if (!alive) break;
 
+            if (PACK > 1) {  // a pair's pages have summed the same heads in different lanes
 #pragma unroll
-            for (int o = 4; o < 32; o <<= 1) {
+                for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) O[c][j][i] += __shfl_xor_sync(0xffffffffu, O[c][j][i], HEAD_LANES);
+            }
+#pragma unroll
+            for (int o = HEAD_LANES; o < 32; o <<= 1) {
                 l_a += __shfl_xor_sync(0xffffffffu, l_a, o);
                 l_b += __shfl_xor_sync(0xffffffffu, l_b, o);
 #pragma unroll
@@ -498,7 +562,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 }
             }
             const size_t row0 = static_cast<size_t>(cur.b) * p.Hq + cur.kvh * G + quad_col;
-            const bool has_a = quad_col < G, has_b = quad_col + 1 < G;
+            const bool has_a = my_page == 0 && quad_col < G, has_b = my_page == 0 && quad_col + 1 < G;
             const bool whole = page0 == 0 && pages == cur.np;
             // Final rows are divided by the sum of weights. Partials carry (reference, sum) with the sum in [1, 2), so that the
             // merge compares references that mean the same thing whatever this segment's scales were.
@@ -571,29 +635,31 @@ constexpr size_t q4_smem_bytes() {
 // 12 x 1 x 3 124.0, 8 x 2 x 4 126.2. head_dim 64, same lengths / 37 sequences of 0-5000 tokens at 16/2 heads:
 // 16 x 1 x 4 73.2 / 19.2, 16 x 1 x 6 69.3 / 20.1, 16 x 2 x 4 73.2 / 19.7, 12 x 2 x 4 74.6 / 19.3.
 constexpr int kQ4Warps = 12, kQ4Warps64 = 16, kQ4Stages = 1, kQ4TilePages = 4;
+template <int D, int WARPS, typename F>
+cudaError_t with_q4_pack(int group, F &&f) {
+    constexpr size_t bytes = q4_smem_bytes<D, WARPS, kQ4Stages, kQ4TilePages>();
+    return group <= 4 ? f(decode_attn_split_q4_kernel<D, WARPS, kQ4Stages, kQ4TilePages, 2>, bytes, WARPS)
+                      : f(decode_attn_split_q4_kernel<D, WARPS, kQ4Stages, kQ4TilePages, 1>, bytes, WARPS);
+}
 template <typename F>
-cudaError_t with_q4_kernel(int head_dim, F &&f) {
-    if (head_dim == 64)
-        return f(decode_attn_split_q4_kernel<64, kQ4Warps64, kQ4Stages, kQ4TilePages>, q4_smem_bytes<64, kQ4Warps64, kQ4Stages, kQ4TilePages>(),
-                 kQ4Warps64);
-    return f(decode_attn_split_q4_kernel<128, kQ4Warps, kQ4Stages, kQ4TilePages>, q4_smem_bytes<128, kQ4Warps, kQ4Stages, kQ4TilePages>(),
-             kQ4Warps);
+cudaError_t with_q4_kernel(int head_dim, int group, F &&f) {
+    return head_dim == 64 ? with_q4_pack<64, kQ4Warps64>(group, f) : with_q4_pack<128, kQ4Warps>(group, f);
 }
 
 }  // namespace
 
-cudaError_t prepare_decode_attn_q4(int head_dim) {
+cudaError_t prepare_decode_attn_q4(int head_dim, int group) {
     auto set = [](auto *k, size_t bytes, int) {
         return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(bytes));
     };
-    return with_q4_kernel(head_dim, set);
+    return with_q4_kernel(head_dim, group, set);
 }
 
 cudaError_t launch_decode_attn_q4(int head_dim, const AttnParams &p, int num_ctas, cudaStream_t stream) {
     auto go = [&](auto *k, size_t bytes, int warps) {
         return launch_pdl(k, dim3(num_ctas), dim3(warps * 32), bytes, stream, p.pdl != 0, p);
     };
-    return with_q4_kernel(head_dim, go);
+    return with_q4_kernel(head_dim, p.G, go);
 }
 
 }  // namespace pd

@@ -231,7 +231,7 @@ cudaError_t launch_kv_append_tokens(const AppendTokensParams &p, int max_q_len, 
 // ctx_lens[b] += q_indptr[b + 1] - q_indptr[b] where the table row has room (the second half of a multi-token append)
 cudaError_t launch_advance_lens(const AppendTokensParams &p, cudaStream_t stream);
 // 4-bit pages; the split kernel writes the same partials and plan, so launch_lse_merge follows it
-cudaError_t prepare_decode_attn_q4(int head_dim);
+cudaError_t prepare_decode_attn_q4(int head_dim, int group);
 cudaError_t launch_decode_attn_q4(int head_dim, const AttnParams &p, int num_ctas, cudaStream_t stream);
 cudaError_t launch_kv_append_q4(const AppendQ4Params &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_dequantize_q4(const DequantizeQ4Params &p, int num_sms, cudaStream_t stream);
