@@ -61,6 +61,7 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ void prefetch_l1(const void *at) { asm volatile("prefetch.global.L1 [%0];" ::"l"(at)); }
 // The first of a chain, without registers to clear beforehand.
 __device__ __forceinline__ void mma_f16_from_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
@@ -169,6 +170,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     int ids = 0, ids_next = 0, window = 0;  // page ids [window, window + 32) of the open segment, one per lane, and those from window + WINDOW on
     bool p_first = true, p_done = false, have_next = false;
     int next_raw = 0;
+    // With one range per worker at most nothing is ever claimed: no traffic on the counters then (all workers of a small batch
+    // at once cost 1.5 us).
+    const bool claims = pl.n_ranges > n_workers;
+    const int G = p.G;
     const uint8_t *blocks = p.kv4;  // page 0 of the open KV head
     const uint32_t page_bytes = static_cast<uint32_t>(p.Hkv) * BLOCK;
     auto load_ids = [&](int page) {
@@ -177,16 +182,16 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     auto issue_next = [&]() {
         if (p_left == 0) {
             if (p_done) return;
-            if (!p_first) {
+            if (!p_first && claims) {
                 if (!have_next && lane == 0) next_raw = atomicAdd(p.status + kSchedNext, 1);
                 p_rid = n_workers + __shfl_sync(0xffffffffu, next_raw, 0);
                 have_next = false;
             }
-            p_first = false;
-            if (p_rid >= pl.n_ranges) {
+            if (p_rid >= pl.n_ranges || (!p_first && !claims)) {
                 p_done = true;
                 return;
             }
+            p_first = false;
             long long start;
             range_bounds(pl, p_rid, start, p_left);
             prod = locate(cum, p.B, p.Hkv, start);
@@ -194,6 +199,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
             window = prod.page;
             ids = load_ids(window);
             ids_next = load_ids(window + WINDOW);
+            // the queries, wanted when the first tile has come: 0.8 us if they are only asked for then
+            if (lane < G * D / 64) prefetch_l1(p.q + (static_cast<size_t>(prod.b) * p.Hq + prod.kvh * G) * D + lane * 64);
         }
         const int n = min(TP, min(p_left, prod.np - prod.page));
         int pid = __shfl_sync(0xffffffffu, ids, (prod.page - window + lane) & 31);
@@ -226,7 +233,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
             ids = ids_next;
             ids_next = load_ids(window + WINDOW);
         }
-        if (p_left <= kClaimAhead * TP && !have_next) {
+        if (claims && p_left <= kClaimAhead * TP && !have_next) {
             if (lane == 0) next_raw = atomicAdd(p.status + kSchedNext, 1);
             have_next = true;
         }
@@ -241,7 +248,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     const int quad_col = quad_t * 2 % COLS, my_page = quad_t * 2 / COLS;
     // column g of a B operand: head b_head of the set's page b_page
     const int b_head = quad_row % COLS, b_page = quad_row / COLS;
-    const int G = p.G;
     // ldmatrix source rows: matrices 0 / 1 = slots 0-7 / 8-15 of a piece, 2 / 3 = the same of the next piece
     const int ld_slot = ((lane >> 3) & 1) * 8 + (lane & 7), ld_piece = lane >> 4;
     uint32_t ld_off[GROUPS];
@@ -614,7 +620,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     }
     if (lane == 0) {
         if (!alive) latch_status(p.status, kDevTimeout, -1, worker);
-        if (atomicAdd(p.status + kSchedDone, 1) == n_workers - 1) {  // the last worker re-arms the claim counter
+        if (claims && atomicAdd(p.status + kSchedDone, 1) == n_workers - 1) {  // the last worker re-arms the claim counter
             p.status[kSchedNext] = 0;
             p.status[kSchedDone] = 0;
         }

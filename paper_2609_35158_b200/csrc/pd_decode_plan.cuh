@@ -57,7 +57,9 @@ __device__ void scan_pages(const AttnParams &p, int32_t *cum, int32_t *warp_sums
     for (int i = begin; i < end; ++i) {
         const int L = __ldg(p.ctx_lens + i) + p.fused;
         if (L < p.fused || L > p.MP * kPageSize) latch_status(p.status, kDevBadLength, i, L - p.fused);
-        sum += (clamp_len(L, p.MP) + kPageSize - 1) / kPageSize;
+        const int pages = (clamp_len(L, p.MP) + kPageSize - 1) / kPageSize;
+        cum[i] = pages;  // this thread's own entries, turned into sums below
+        sum += pages;
     }
     int incl = sum;
 #pragma unroll
@@ -71,11 +73,17 @@ __device__ void scan_pages(const AttnParams &p, int32_t *cum, int32_t *warp_sums
     for (int w = 0; w < (tid >> 5); ++w) base += warp_sums[w];
     int run = base + incl - sum;
     for (int i = begin; i < end; ++i) {
+        const int pages = cum[i];
         cum[i] = run;
-        run += (clamp_len(__ldg(p.ctx_lens + i) + p.fused, p.MP) + kPageSize - 1) / kPageSize;
+        run += pages;
     }
     if (tid == THREADS - 1) cum[p.B] = run;
     __syncthreads();
+}
+
+// a / b for a >= 0, b > 0; 64-bit division is a long routine on the device, and most operands fit 32 bits.
+__host__ __device__ __forceinline__ long long div_positive(long long a, long long b) {
+    return ((a | b) >> 32) == 0 ? static_cast<long long>(static_cast<uint32_t>(a) / static_cast<uint32_t>(b)) : a / b;
 }
 
 // The plan is a pure function of (total, workers, parameters): every CTA and the
@@ -86,12 +94,12 @@ __host__ __device__ inline void make_plan(Plan &pl, long long total, int n_worke
     long long pos = 0;
     if (p.split_pages > 0) {
         long long size = p.split_pages;
-        if ((total + size - 1) / size > p.max_ranges) size = (total + p.max_ranges - 1) / p.max_ranges;
+        if (div_positive(total + size - 1, size) > p.max_ranges) size = div_positive(total + p.max_ranges - 1, p.max_ranges);
         pl.lv[0].start = 0; pl.lv[0].size = static_cast<int>(size); pl.lv[0].first = 0;
-        first = static_cast<int>((total + size - 1) / size);
+        first = static_cast<int>(div_positive(total + size - 1, size));
         nl = 1;
     } else {
-        long long fair = (total + n_workers - 1) / n_workers;
+        long long fair = div_positive(total + n_workers - 1, n_workers);
         // a kernel whose workers all run at the same speed (the FP8 one: bound by its own instruction stream, not by
         // the memory system) gains nothing from claiming small ranges late and pays for every extra range
         const int levels = fair <= p.static_fair_max ? 0 : p.halving_levels;
@@ -99,7 +107,7 @@ __host__ __device__ inline void make_plan(Plan &pl, long long total, int n_worke
                                               min(static_cast<long long>(p.tail_pages), fair)));
         for (int l = 0; l < levels && nl < kMaxLevels - 1; ++l) {
             const long long rem = total - pos;
-            const long long size = (rem + 2ll * n_workers - 1) / (2ll * n_workers);
+            const long long size = div_positive(rem + 2ll * n_workers - 1, 2ll * n_workers);
             if (size < 2ll * tail || first + 2 * n_workers > p.max_ranges) break;
             pl.lv[nl].start = pos; pl.lv[nl].size = static_cast<int>(size); pl.lv[nl].first = first;
             pos += size * n_workers;
@@ -110,10 +118,10 @@ __host__ __device__ inline void make_plan(Plan &pl, long long total, int n_worke
         if (rem > 0 || nl == 0) {
             long long size = levels > 0 ? tail : max(fair, static_cast<long long>(p.min_pages_auto));
             const long long room = max(1, p.max_ranges - first);
-            if ((rem + size - 1) / size > room) size = (rem + room - 1) / room;
+            if (div_positive(rem + size - 1, size) > room) size = div_positive(rem + room - 1, room);
             if (size < 1) size = 1;
             pl.lv[nl].start = pos; pl.lv[nl].size = static_cast<int>(size); pl.lv[nl].first = first;
-            first += static_cast<int>((rem + size - 1) / size);
+            first += static_cast<int>(div_positive(rem + size - 1, size));
             ++nl;
         }
     }
@@ -130,7 +138,7 @@ __host__ __device__ __forceinline__ void range_bounds(const Plan &pl, int rid, l
 }
 
 __host__ __device__ __forceinline__ Cursor locate(const int32_t *cum, int B, int Hkv, long long x) {
-    const int y = static_cast<int>(x / Hkv);  // largest b with cum[b] <= y owns unit x
+    const int y = static_cast<int>(div_positive(x, Hkv));  // largest b with cum[b] <= y owns unit x
     int lo = 0, hi = B - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
