@@ -61,7 +61,6 @@ __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1,
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ void prefetch_l1(const void *at) { asm volatile("prefetch.global.L1 [%0];" ::"l"(at)); }
 // The first of a chain, without registers to clear beforehand.
 __device__ __forceinline__ void mma_f16_from_zero(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
@@ -199,8 +198,6 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
             window = prod.page;
             ids = load_ids(window);
             ids_next = load_ids(window + WINDOW);
-            // the queries, wanted when the first tile has come: 0.8 us if they are only asked for then
-            if (lane < G * D / 64) prefetch_l1(p.q + (static_cast<size_t>(prod.b) * p.Hq + prod.kvh * G) * D + lane * 64);
         }
         const int n = min(TP, min(p_left, prod.np - prod.page));
         int pid = __shfl_sync(0xffffffffu, ids, (prod.page - window + lane) & 31);
