@@ -9,8 +9,8 @@
 // The work forms one list that the CTAs share out evenly. Writing, that is the packed tokens; reading back, the pages of all
 // sequences, whose counts each CTA sums itself (a grid of CTAs per sequence instead left short sequences' CTAs idle, and where the host knows no lengths it had to
 // launch CTAs for every page a sequence could have: 12.2 against 5.5 us to write one token of 64 sequences and read it back).
-// Measured for 4 x 32768 tokens at 8 KV heads, head_dim 128: written in 134 us (670 MB, 0.78 of the copy bandwidth), read back
-// in 117 us (688 MB, 0.91).
+// Measured for 4 x 32768 tokens at 8 KV heads, head_dim 128: written in 119 us (670 MB), read back in
+// 123 us (688 MB), each 0.87 of the copy bandwidth.
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_q4.cuh"
@@ -194,7 +194,7 @@ __global__ void __launch_bounds__(kThreads) kv_dequantize_q4_kernel(const Dequan
 }
 
 // CTAs to launch: some waves of them, because the SMs differ in speed and the hardware hands late CTAs to the fast ones
-// (131072 tokens written: 134 us with 20 per SM, 152 us with 5, all resident), but no more than there can be pages. How many
+// (131072 tokens written, in an earlier form: 134 us with 20 per SM, 152 us with 5, all resident), but no more than there can be pages. How many
 // pages a read-back has the host does not know, and every CTA costs about 0.1 us per SM even if it finds none: 16.
 int ctas(int64_t pages_most, int most) { return static_cast<int>(pages_most < most ? (pages_most < 1 ? 1 : pages_most) : most); }
 
