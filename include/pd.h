@@ -484,7 +484,7 @@ int pd_decode_step_q4(pd_ctx *ctx, const void *q, const void *k_new, const void 
  *
  * The first rot_dim values of a head form rot_dim / 2 pairs: (i, i + rot_dim / 2), or (2i, 2i + 1) with `adjacent`.
  * Pair i turns by position[axis_of_pair[i]] * inv_freq[i] radians: (a, b) -> magnitude * (a cos - b sin, a sin + b cos).
- * Values past rot_dim are copied. The angle is exact to 2^-32 turns at every int32 position; sums are fp32, results are
+ * Values past rot_dim are copied. The angle is off by less than 2^-31 turns at every int32 position, then rounded to fp32; sums are fp32, results are
  * rounded once to bf16. The structure lies in HOST memory and is read during the call. */
 typedef struct pd_rope_config {
     int32_t rot_dim;          /* multiple of 16, 16 .. head_dim                                          */

@@ -4,6 +4,7 @@
 #include "../../include/pd_debug.h"
 
 #include <chrono>
+#include <cmath>
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
@@ -775,6 +776,20 @@ int decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *p
     return PD_OK;
 }
 
+// f radians per position as a 64-bit fixed-point fraction of a turn, |f| < 402. f is an integer of 24 bits times 2^exp, and
+// its product with 1 / (2 pi), given to 128 bits, is formed in integers: off by less than 2^-64 turns, so by 2^-33 at any
+// int32 position. (A product in fp64 is off by 2^-53 of itself: 2^-16 turns far out at the largest frequencies.)
+uint64_t turns_fixed(float f) {
+    constexpr uint64_t inv_hi = 0x28be60db9391054aull, inv_lo = 0x7f09d5f47d4d3770ull;
+    int exp = 0;
+    const uint64_t m = static_cast<uint64_t>(std::ldexp(std::frexp(std::fabs(static_cast<double>(f)), &exp), 24));
+    const int shift = 24 - exp;  // at least 15: |f| < 2^9
+    const unsigned __int128 product = static_cast<unsigned __int128>(m) * inv_hi + ((static_cast<unsigned __int128>(m) * inv_lo) >> 64);
+    // whole turns fall off the top; two's complement carries the sign
+    const uint64_t fixed = shift >= 128 ? 0ull : static_cast<uint64_t>(product >> shift);
+    return f < 0.f ? 0ull - fixed : fixed;
+}
+
 // Checks a rotation and lays it out for the kernels.
 int rope_params(pd_ctx *ctx, const pd_rope_config *rope, pd::RopeParams *p) {
     if (rope == nullptr) return fail(ctx, PD_ERR_INVALID_ARG, "rope: null configuration");
@@ -786,11 +801,7 @@ int rope_params(pd_ctx *ctx, const pd_rope_config *rope, pd::RopeParams *p) {
         const double turns = static_cast<double>(rope->inv_freq[i]) * 0.15915494309189533577;  // 1 / (2 pi)
         if (rope->axis_of_pair[i] >= rope->num_axes || !(turns > -64.0 && turns < 64.0))
             return fail(ctx, PD_ERR_INVALID_ARG, "rope: axis or frequency of a pair out of range");
-        // two's complement carries the sign, and whole turns fall off the top; split in two so that the cast is exact
-        double frac = turns < 0.0 ? -turns : turns;
-        frac -= static_cast<double>(static_cast<int>(frac));
-        const uint64_t fixed = static_cast<uint64_t>(frac * 18446744073709551616.0);
-        p->freq[i] = turns < 0.0 ? 0ull - fixed : fixed;
+        p->freq[i] = turns_fixed(rope->inv_freq[i]);
         p->axis_of_pair[i] = rope->axis_of_pair[i];
     }
     p->magnitude = rope->magnitude;

@@ -67,6 +67,52 @@ def test_far_and_negative_positions_keep_their_angle():
         check_rotated(qo, q, pos, freq, [0] * 64, d, False)
 
 
+def inv_two_pi(bits):
+    """floor(2^bits / (2 pi)) by Machin's formula in integers."""
+    n = bits + 64
+
+    def atan_inverse(x):
+        term = (1 << n) // x
+        total, k, sign = term, 1, -1
+        while term:
+            term //= x * x
+            k += 2
+            total, sign = total + sign * (term // k), -sign
+        return total
+
+    return (1 << (n + bits)) // (8 * (4 * atan_inverse(5) - atan_inverse(239)))
+
+
+def test_the_largest_frequencies_keep_their_angle_at_far_positions():
+    """Rotating (1, 0) gives cosine and sine alone; where one of them is near 0, bf16 shows its absolute error. The tolerance:
+    2^-31 turns and the rounding of the angle to fp32 (2^-26 turns) are below 2^-23 radians, sine and cosine of CUDA
+    are within 2 units of 2^-24; together below 2^-21. Then one rounding to bf16."""
+    import paper_2609_35158_b200 as pd
+
+    d, n, bits = 64, 500, 320
+    rng = np.random.default_rng(5)
+    freq = rng.uniform(50, 400, d // 2).astype(np.float32) * rng.choice([-1, 1], d // 2).astype(np.float32)
+    pos = rng.integers(-2 ** 31, 2 ** 31, (1, n)).astype(np.int32)
+    unit = inv_two_pi(bits)
+    want = np.empty((n, d))
+    for i, f in enumerate(freq):
+        num, den = float(f).as_integer_ratio()
+        for t in range(n):
+            whole = den << bits
+            turn = (num * unit * int(pos[0, t])) % whole
+            angle = 2 * np.pi * (((turn << 60) // whole) / 2.0 ** 60 - (turn * 2 >= whole))
+            want[t, i], want[t, i + d // 2] = np.cos(angle), np.sin(angle)
+    assert (np.abs(want) < 1e-3).sum() > 10
+    q = torch.zeros((n, 1, d), dtype=torch.bfloat16, device=DEV)
+    q[..., :d // 2] = 1
+    qo, ko = torch.empty_like(q), torch.empty_like(q)
+    with Ctx(1, 1, d, 1, 1, 1) as ctx:
+        pd.pd_rope_tokens(ctx.h, pd.rope_config(d, freq), dev(pos), q, q, qo, ko)
+        torch.cuda.synchronize()
+    got = qo[:, 0].float().cpu().numpy().astype(np.float64)
+    assert np.all(np.abs(got - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -21)
+
+
 def packed(before, new, seed, Hq, Hkv, d, axes):
     rng = np.random.default_rng(seed)
     total = int(new.sum())
