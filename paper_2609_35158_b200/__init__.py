@@ -360,7 +360,7 @@ def rope_config(rot_dim: int, inv_freq, axis_of_pair=None, num_axes: int = 1, ad
     return c
 
 
-def _position_stride(positions, rope, rows=0) -> int:
+def _position_stride(positions, rope, rows) -> int:
     if positions is None:
         return 0
     if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() < rope.num_axes * positions.shape[-1]:
@@ -373,7 +373,7 @@ def _position_stride(positions, rope, rows=0) -> int:
 def pd_rope_tokens(ctx, rope, positions, q, k, q_out, k_out, total=None, stream=None):
     """``positions``: int32 [num_axes, rows] (or [rows] for one axis), contiguous."""
     total = q.shape[0] if total is None else total
-    _check(_lib.pd_rope_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q), _ptr(k),
+    _check(_lib.pd_rope_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope, total), _ptr(q), _ptr(k),
                                _ptr(q_out), _ptr(k_out), total, _stream(stream)), "pd_rope_tokens", ctx)
 
 
