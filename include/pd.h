@@ -497,7 +497,6 @@ typedef struct pd_rope_config {
 
 /*
  * positions: int32 DEVICE array [num_axes][position_stride]; entry [axis][row] belongs to packed row `row`.
- * There are as many entries per axis as packed rows (q_indptr[batch], which the host does not see, in the appends).
  *
  * pd_rope_tokens rotates rows [0, total) of q ([total][num_q_heads][head_dim] bf16) into q_out and of k
  * ([total][num_kv_heads][head_dim]) into k_out. q_out may be q and k_out may be k (other overlaps are not allowed).

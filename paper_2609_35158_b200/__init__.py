@@ -360,20 +360,18 @@ def rope_config(rot_dim: int, inv_freq, axis_of_pair=None, num_axes: int = 1, ad
     return c
 
 
-def _position_stride(positions, rope, rows) -> int:
+def _position_stride(positions, rope) -> int:
     if positions is None:
         return 0
     if positions.dtype != torch.int32 or not positions.is_contiguous() or positions.numel() < rope.num_axes * positions.shape[-1]:
         raise ValueError("positions: a contiguous int32 tensor [num_axes, rows] (or [rows] for one axis)")
-    if positions.shape[-1] < rows:
-        raise ValueError("positions: fewer rows than q")
     return positions.shape[-1]
 
 
 def pd_rope_tokens(ctx, rope, positions, q, k, q_out, k_out, total=None, stream=None):
     """``positions``: int32 [num_axes, rows] (or [rows] for one axis), contiguous."""
     total = q.shape[0] if total is None else total
-    _check(_lib.pd_rope_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope, total), _ptr(q), _ptr(k),
+    _check(_lib.pd_rope_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q), _ptr(k),
                                _ptr(q_out), _ptr(k_out), total, _stream(stream)), "pd_rope_tokens", ctx)
 
 
@@ -381,7 +379,7 @@ def pd_rope_append_tokens(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out
                           max_q_len, batch=None, call_flags=0, stream=None):
     """``positions`` may be None: every axis stands at the token's index in its sequence."""
     batch = q_indptr.shape[0] - 1 if batch is None else batch
-    _check(_lib.pd_rope_append_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope, q.shape[0]), _ptr(q),
+    _check(_lib.pd_rope_append_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
                                       _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
                                       _ptr(page_table), _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
            "pd_rope_append_tokens", ctx)
@@ -390,7 +388,7 @@ def pd_rope_append_tokens(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out
 def pd_rope_append_tokens_q4(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out, kv4, page_table, ctx_lens, max_q_len,
                              batch=None, call_flags=0, stream=None):
     batch = q_indptr.shape[0] - 1 if batch is None else batch
-    _check(_lib.pd_rope_append_tokens_q4(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope, q.shape[0]), _ptr(q),
+    _check(_lib.pd_rope_append_tokens_q4(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
                                          _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(kv4), _ptr(page_table),
                                          _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
            "pd_rope_append_tokens_q4", ctx)
