@@ -833,6 +833,10 @@ int rope_append(pd_ctx *ctx, const char *who, const pd_rope_config *rope, const 
         return fail(ctx, PD_ERR_INVALID_ARG, msg);
     }
     if (max_q_len < 0 || position_stride < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len and position_stride must be >= 0");
+    if (positions != nullptr && position_stride == 0 && batch > 0 && max_q_len > 0) {
+        std::snprintf(msg, sizeof msg, "%s: no positions (position_stride 0)", who);
+        return fail(ctx, PD_ERR_INVALID_ARG, msg);
+    }
     pd::RopeParams p{};
     if (int rc = rope_params(ctx, rope, &p)) return rc;
     if (kv4 != nullptr && ctx->cfg.num_kv_heads * ctx->cfg.head_dim > 14336)

@@ -124,6 +124,7 @@ struct AppendTokensParams {
     int32_t B, Hkv, D, MP;
     int32_t num_pages;
     int32_t pdl;
+    long long row_limit;                 // advance_lens: sequences with rows from here on stay as they are (0 = no limit)
 };
 
 // Shape of one compiled variant of the split kernel.

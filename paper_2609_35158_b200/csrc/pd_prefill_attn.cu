@@ -486,6 +486,7 @@ __global__ void advance_lens_kernel(const AppendTokensParams p) {
     if (b >= p.B) return;
     const int n = p.q_indptr[b + 1] - p.q_indptr[b];
     const int L = p.ctx_lens[b];
+    if (p.row_limit > 0 && p.q_indptr[b + 1] > p.row_limit) return;
     if (n > 0 && L >= 0 && (L + n + kPageSize - 1) / kPageSize <= p.MP) p.ctx_lens[b] = L + n;
 }
 

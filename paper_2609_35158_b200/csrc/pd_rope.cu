@@ -120,6 +120,10 @@ __global__ void __launch_bounds__(kThreads, 5) rope_kernel(const __grid_constant
         n = p.q_indptr[b + 1] - r0;
         L = p.ctx_lens[b];
         if (n <= 0) return;
+        if (p.positions != nullptr && r0 + n > p.position_stride) {  // some of its positions would lie past the array
+            if (tid == 0 && blockIdx.x == 0) latch(p.status, kDevBadLength, b, r0 + n);
+            return;
+        }
     }
     const bool room = APPEND != kNoAppend && L >= 0 && L <= p.MP * kPageSize - n;
     if (APPEND != kNoAppend && !room && tid == 0 && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);
@@ -247,6 +251,7 @@ cudaError_t launch_rope(const RopeParams &base, int append, int max_q_len, int n
     a.B = p.B;
     a.MP = p.MP;
     a.pdl = p.pdl;
+    a.row_limit = p.positions != nullptr ? p.position_stride : 0;
     *launched = 2;
     return launch_advance_lens(a, stream);
 }

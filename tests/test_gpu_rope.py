@@ -186,6 +186,48 @@ def test_fused_append_reports_and_skips():
             check_rotated(qo, q, pos, freq, [0] * 64, d, False)  # queries are rotated all the same
 
 
+@pytest.mark.parametrize("new", [[1, 1, 1], [40, 30, 30], [0, 3, 2]])
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("rows_short", [0, 1])
+def test_fused_append_leaves_out_sequences_without_positions(new, four, rows_short):
+    """Positions for all rows but the last: the sequence that holds it keeps its pages, length and queries."""
+    import paper_2609_35158_b200 as pd
+
+    d, Hq, Hkv, axes = 128, 4, 2, 2
+    before, new = np.array([3, 0, 7], np.int32), np.array(new, np.int32)
+    table = np.arange(15, dtype=np.int32).reshape(3, 5)
+    indptr, pos, q, k, v = packed(before, new, 60, Hq, Hkv, d, axes)
+    held = int(indptr[3]) - rows_short
+    freq, axis = frequencies(d), [i % axes for i in range(d // 2)]
+    rope = pd.rope_config(d, freq, axis, num_axes=axes)
+    with Ctx(Hq, Hkv, d, 3, 5, 15) as ctx:
+        L, qo, given = dev(before), torch.full_like(q, float("nan")), dev(pos[:, :held].copy())
+        if four:
+            kv = torch.zeros((15, Hkv, 18 * d), dtype=torch.uint8, device=DEV)
+            pd.pd_rope_append_tokens_q4(ctx.h, rope, given, q, k, v, dev(indptr), qo, kv, dev(table), L, int(new.max()))
+            touched = kv.flatten(1).any(1)
+        else:
+            kp, vp = (torch.zeros((15, Hkv, P, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            pd.pd_rope_append_tokens(ctx.h, rope, given, q, k, v, dev(indptr), qo, kp, vp, dev(table), L, int(new.max()))
+            touched = (kp != 0).flatten(1).any(1) & (vp != 0).flatten(1).any(1)
+        if rows_short:
+            assert pd.pd_device_status(ctx.h) == (pd.PD_ERR_DEVICE_FAULT, 2, int(indptr[3]))
+        else:
+            assert pd.pd_device_status(ctx.h)[0] == 0
+        served = 2 if rows_short else 3
+        after = before.copy()
+        after[:served] += new[:served]
+        assert L.cpu().tolist() == after.tolist()
+        want = np.zeros(15, bool)
+        for b in range(served):
+            for t in range(int(before[b]), int(after[b])):
+                want[table[b, t // P]] = True
+        assert touched.cpu().tolist() == want.tolist()
+        n = int(indptr[served])
+        check_rotated(qo[:n], q[:n], pos[:, :n], freq, axis, d, False)
+        assert torch.isnan(qo[n:].float()).all()
+
+
 def test_refusals():
     import paper_2609_35158_b200 as pd
 
