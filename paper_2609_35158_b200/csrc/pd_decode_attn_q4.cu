@@ -436,14 +436,21 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                             }
                 }
 
-                float xm_a = x[0][0], xm_b = x[0][1], vm = 0.f;
+                // The caps are about the largest V scale, vm, and a minimum counts with 2^-24 of itself, as below: behind a tile whose V
+                // has tiny scales or none, p * minimum could leave fp32. (A record as a float is its minimum but for bits below bf16's;
+                // the check costs 0.5 % on the long batches.)
+                float xm_a = x[0][0], xm_b = x[0][1], vm = 0.f, mm = 0.f;
 #pragma unroll
                 for (int t = 0; t < SETS; ++t) {
                     xm_a = max3(xm_a, x[t][0], x[t][2]);
                     xm_b = max3(xm_b, x[t][1], x[t][3]);
 #pragma unroll
-                    for (int g = 0; g < GROUPS; ++g) vm = max3(vm, bf16_lo(rv[t][0][g]), bf16_lo(rv[t][1][g]));
+                    for (int g = 0; g < GROUPS; ++g) {
+                        vm = max3(vm, bf16_lo(rv[t][0][g]), bf16_lo(rv[t][1][g]));
+                        mm = max3(mm, fabsf(__uint_as_float(rv[t][0][g])), fabsf(__uint_as_float(rv[t][1][g])));
+                    }
                 }
+                vm = fmaxf(vm, mm * 5.9604645e-8f);
                 if (__any_sync(0xffffffffu, xm_a > cap_x || xm_b > cap_x || vm > cap_v)) {
                     // largest weight of this tile by head: p * v_scale; a minimum 2^24 times the scale counts like the scale
                     // (the codes no longer matter then), and p itself stays below 2^100
@@ -470,19 +477,23 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                     // the first tile puts its largest weight at 2^2; later ones only ever raise r
                     const bool fresh = cap_v < 0.f;
                     const float up_a = fresh ? w_a - 2.f : fmaxf(w_a - 2.f, 0.f), up_b = fresh ? w_b - 2.f : fmaxf(w_b - 2.f, 0.f);
-                    const float f_a = fresh ? 0.f : fast_exp2(-up_a), f_b = fresh ? 0.f : fast_exp2(-up_b);
+                    // 2^-up in two factors: where a reference set by tiny scales meets large ones up passes 126, and the sums of
+                    // weights, up to 2^100, still count
+                    const float f_a = fresh ? 0.f : fast_exp2(-fminf(up_a, 100.f)), f_b = fresh ? 0.f : fast_exp2(-fminf(up_b, 100.f));
+                    const float f2_a = fast_exp2(fminf(100.f - up_a, 0.f)), f2_b = fast_exp2(fminf(100.f - up_b, 0.f));
+                    const float fo_a = f_a * f2_a, fo_b = f_b * f2_b;
                     nr_a -= up_a;
                     nr_b -= up_b;
-                    l_a *= f_a;
-                    l_b *= f_b;
+                    l_a = l_a * f_a * f2_a;
+                    l_b = l_b * f_b * f2_b;
 #pragma unroll
-                    for (int g = 0; g < GROUPS; ++g) { Ma[g] *= f_a; Mb[g] *= f_b; }
+                    for (int g = 0; g < GROUPS; ++g) { Ma[g] = Ma[g] * f_a * f2_a; Mb[g] = Mb[g] * f_b * f2_b; }
 #pragma unroll
                     for (int c = 0; c < PIECES; ++c)
 #pragma unroll
                         for (int j = 0; j < 2; ++j) {
-                            O[c][j][0] *= f_a; O[c][j][2] *= f_a;
-                            O[c][j][1] *= f_b; O[c][j][3] *= f_b;
+                            O[c][j][0] *= fo_a; O[c][j][2] *= fo_a;
+                            O[c][j][1] *= fo_b; O[c][j][3] *= fo_b;
                         }
 #pragma unroll
                     for (int t = 0; t < SETS; ++t) {
