@@ -28,7 +28,14 @@
 //     four of the next: both pages' products go into one accumulator, each with zeros in the other's columns, and the
 //     softmax between the products costs two pages what it cost one. O has both pages' sums apart and adds them at the end
 //     (134 -> 130 us on 64 contexts of 2K-16K at 32/8 heads, 79 -> 73 us at head_dim 64; both under the power limit).
-// Sums, statistics, O and the rank-one terms are fp32.
+//   * the tensor core cuts what lies below fp32's last bit off its sums. Codes and weights are positive, so O fell behind with
+//     every product of a long segment, and the minima, summed exactly, did not: 65536 tokens in one segment were off by 6 to
+//     13 % of the output's rms (1024 pages: 1 to 3 %, 256: 0.3 to 0.6 %). So every 32 products of a lane's columns O is folded
+//     into shared memory, rounded to nearest: 0.18 %, of which bf16 is 0.17. It costs 0.7 to 1.2 % on the long
+//     batches; folds twice as far apart save nothing and leave 0.20 %.
+// Sums, statistics, O and the rank-one terms are fp32. Weights p_t sv_t are rounded to fp16, 2^-11 of each at most, which adds
+// 0.03 % of the output's rms to bf16's 0.17: adding 7.5 times the rounding to the minima's sum, which takes out the codes' mean,
+// halved that and made the long batches 1 to 2.5 % slower (2 to 4 % under the power limit).
 //
 // Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, 187 per page at head_dim 128 and four
 // heads, 205 at eight. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
@@ -90,12 +97,31 @@ __device__ __forceinline__ uint32_t transpose8x8(uint32_t a) {
     return d;
 }
 
+__device__ __forceinline__ float4 ld_shared_f4(uint32_t at) {
+    float4 f;
+    asm volatile("ld.shared.v4.f32 {%0,%1,%2,%3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(at) : "memory");
+    return f;
+}
+__device__ __forceinline__ float2 ld_shared_f2(uint32_t at) {
+    float2 f;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(f.x), "=f"(f.y) : "r"(at) : "memory");
+    return f;
+}
+__device__ __forceinline__ void st_shared_f4(uint32_t at, float x, float y, float z, float w) {
+    asm volatile("st.shared.v4.f32 [%0], {%1,%2,%3,%4};" ::"r"(at), "f"(x), "f"(y), "f"(z), "f"(w) : "memory");
+}
+__device__ __forceinline__ void st_shared_f2(uint32_t at, float x, float y) {
+    asm volatile("st.shared.v2.f32 [%0], {%1,%2};" ::"r"(at), "f"(x), "f"(y) : "memory");
+}
+
 // bulk_load with an L2 policy.
 __device__ __forceinline__ void bulk_load_hint(uint32_t dst, const void *src, uint32_t bytes, uint32_t bar, uint64_t pol) {
     asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;" ::"r"(dst),
                  "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar), "l"(pol)
                  : "memory");
 }
+constexpr int kQ4FoldProducts = 32;   // products (of 16 tokens) that an accumulator of O takes before it is folded
+constexpr int kQ4FoldRefBytes = 256;  // a float2 per lane
 constexpr uint32_t kNib0 = 0x000f000fu, kNib1 = 0x00f000f0u;
 
 // PACK = 2 (groups of at most four heads): the eight columns of the products are four heads of one page and the same four of the
@@ -117,7 +143,10 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t ring0 = (raw + 127u) & ~127u;
     uint8_t *aligned = smem_raw + (ring0 - raw);
-    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + WARPS * STAGES * STAGE);
+    // the folded part of a warp's O: a float4 per (piece, j) and lane, then per lane the reference it stands at
+    constexpr int FOLD = PIECES * 2 * 512, FOLD_BYTES = FOLD + kQ4FoldRefBytes, FOLD_PAGES = kQ4FoldProducts * PACK;
+    static_assert(FOLD_PAGES % TP == 0, "folds lie between tiles");
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + WARPS * (STAGES * STAGE + FOLD_BYTES));
     Plan *plan_s = reinterpret_cast<Plan *>(bars + WARPS * STAGES);
     int32_t *stage_range = reinterpret_cast<int32_t *>(plan_s + 1);
     int32_t *warp_sums = stage_range + WARPS * STAGES;
@@ -339,6 +368,20 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
 #pragma unroll
             for (int g = 0; g < GROUPS; ++g) { Ma[g] = 0.f; Mb[g] = 0.f; }
             float l_a = 0.f, l_b = 0.f, nr_a = 0.f, nr_b = 0.f;  // nr = -r
+            // O plus what earlier parts of the segment left in shared memory, brought to the present reference
+            auto fold_at = [&]() { return ring0 + WARPS * STAGES * STAGE + warp * FOLD_BYTES + lane * 16; };
+            auto join_folded = [&]() {
+                const float2 nr = ld_shared_f2(fold_at() + FOLD - lane * 8);
+                const float g_a = fast_exp2(nr_a - nr.x), g_b = fast_exp2(nr_b - nr.y);
+#pragma unroll
+                for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const float4 f = ld_shared_f4(fold_at() + (c * 2 + j) * 512);
+                        O[c][j][0] = fmaf(f.x, g_a, O[c][j][0]); O[c][j][1] = fmaf(f.y, g_b, O[c][j][1]);
+                        O[c][j][2] = fmaf(f.z, g_a, O[c][j][2]); O[c][j][3] = fmaf(f.w, g_b, O[c][j][3]);
+                    }
+            };
             float cap_x = -INFINITY, cap_v = -1.f;  // nothing passes before the first tile has set them
 
             for (int pg = 0; pg < pages; pg += TP, rem -= TP * kPageSize) {
@@ -506,6 +549,18 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                     cap_x = static_cast<float>(min(15 - (ev + 3), 100));
                 }
 
+                if (__builtin_expect(pg % FOLD_PAGES == 0 && pg > 0, 0)) {
+                    if (pg > FOLD_PAGES) join_folded();
+#pragma unroll
+                    for (int c = 0; c < PIECES; ++c)
+#pragma unroll
+                        for (int j = 0; j < 2; ++j) {
+                            st_shared_f4(fold_at() + (c * 2 + j) * 512, O[c][j][0], O[c][j][1], O[c][j][2], O[c][j][3]);
+                            O[c][j][0] = 0.f; O[c][j][1] = 0.f; O[c][j][2] = 0.f; O[c][j][3] = 0.f;
+                        }
+                    st_shared_f2(fold_at() + FOLD - lane * 8, nr_a, nr_b);
+                }
+
                 // weights, their sums, and the fp16 B operands: P^T transposed from (slot x head) to (head x slot)
                 uint32_t pb[SETS][GROUPS][2];
 #pragma unroll
@@ -556,6 +611,7 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
                 if (++stage == STAGES) { stage = 0; parity ^= 1u; }
             }
             if (!alive) break;
+            if (pages > FOLD_PAGES) join_folded();
 
             if (PACK > 1) {  // a pair's pages have summed the same heads in different lanes
 #pragma unroll
@@ -637,8 +693,8 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
 
 template <int D, int WARPS, int STAGES, int TP>
 constexpr size_t q4_smem_bytes() {
-    return static_cast<size_t>(WARPS) * STAGES * TP * q4_block_bytes<D>() + 128 + WARPS * STAGES * 8 + sizeof(Plan) +
-           WARPS * STAGES * 4 + 32 * 4 + (kMaxBatch + 1) * 4;
+    return static_cast<size_t>(WARPS) * (STAGES * TP * q4_block_bytes<D>() + D / 32 * 2 * 512 + kQ4FoldRefBytes) + 128 +
+           WARPS * STAGES * 8 + sizeof(Plan) + WARPS * STAGES * 4 + 32 * 4 + (kMaxBatch + 1) * 4;
 }
 
 // Worker warps x stages x pages per tile. A tile costs about 140 instructions beside its pages, so large tiles pay; the
