@@ -434,8 +434,9 @@ int pd_kv_scatter_fp8(pd_ctx *ctx, const void *packed, const int64_t *packed_pag
  *         the high one; the row's 16-byte piece c is stored at piece position c ^ ((slot >> 1) & 3) at head_dim 128,
  *         c ^ ((slot >> 2) & 1) at 64.
  * A value is scale * code + min, code in [0, 15]. Quantising a group: min = its smallest value (a bf16, stored exactly);
- * scale = (max - min) / 15 in fp32, rounded UP to bf16; code = (x - min) / scale to the nearest integer, ties to even,
- * with x - min rounded to fp32. So a value is off by at most scale / 2. Inputs below 2^-126 in magnitude count as 0, a
+ * scale = (max - min) / 15 in fp32, rounded UP to bf16, or down where 15 * scale + min would round past bf16's largest value;
+ * code = (x - min) / scale to the nearest integer, ties to even, with x - min rounded to fp32. So a finite value stays finite
+ * and is off by at most scale / 2. Inputs below 2^-126 in magnitude count as 0, a
  * scale below 2^-100 as 0 (every code 0). A group that holds a NaN or infinity, or whose max - min leaves fp32, gets the
  * scale NaN: all of it reads back as NaN. A token's row never touches another token's bytes, so slots can be written
  * in any order. head_dim 64 or 128. Calls of one context share its workspace: enqueue them on one stream or order

@@ -30,6 +30,9 @@ def quantize_group(bits):
     else:
         scale_bits = int((int(np.float32(s).view(np.uint32)) + 0xFFFF) >> 16)  # up to the next bf16
         scale = float(bf16_bits_to_f64(np.array([scale_bits], np.uint16))[0])
+        if 15 * scale + lo >= 511 * 2.0 ** 119:  # would round past bf16's largest value, 255 * 2^120: the bf16 below
+            scale_bits = int(np.float32(s).view(np.uint32)) >> 16
+            scale = float(bf16_bits_to_f64(np.array([scale_bits], np.uint16))[0])
     d = (x - lo).astype(np.float32).astype(np.float64)
     codes = np.rint(d / scale).astype(np.uint8) if scale > 0 else np.zeros(GROUP, np.uint8)
     assert codes.max() <= 15

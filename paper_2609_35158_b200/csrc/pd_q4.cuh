@@ -47,7 +47,8 @@ __device__ __forceinline__ uint32_t bf16x2_max_nan(uint32_t a, uint32_t b) {
 // differ in the low two bits). Returns the 16 codes, the first value in the lowest nibble; `rec` = {scale, min}.
 //
 //   min    the group's smallest value: a bf16 already, stored exactly
-//   scale  (max - min) / 15 rounded UP to bf16, so that no code passes 15; NaN where the group holds a non-finite value
+//   scale  (max - min) / 15 rounded UP to bf16, or down where 15 * scale + min would round past bf16's largest value (a code
+//          then stands for at most 15.12 steps, which is 15 after rounding); NaN where the group holds a non-finite value
 //          or its range leaves fp32 (min and codes are then 0 and the whole group reads back as NaN), 0 where it is below 2^-100 (all codes 0)
 //   code   (x - min) / scale to the nearest integer, ties to even; x - min is rounded to fp32 first
 //
@@ -108,6 +109,10 @@ __device__ __forceinline__ uint2 q4_quantize16(const uint4 &x0, const uint4 &x1,
             out[h] = sum - 0x4b400000u * 0x11111111u;  // 0x4b400000 is 1.5 * 2^23
         }
     } else {
+        if (__fmaf_rn(s, 15.f, lo) >= __uint_as_float(0x7f7f8000u)) {  // halfway between bf16's largest value and 2^128
+            s = __uint_as_float(__float_as_uint(s) - 0x10000u);       // (a range / 15 that is a bf16 does not get here)
+            rec -= 1u;
+        }
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             out[h] = 0u;

@@ -67,6 +67,26 @@ def test_quantiser_by_hand():
     assert q4.quantize_group(np.array([0x0001, 0x8001] + [0] * 62, np.uint16))[1:] == (0, 0, False)
 
 
+def test_groups_next_to_the_largest_value_stay_finite():
+    largest = 255 * 2.0 ** 120
+    rng = np.random.default_rng(7)
+    rows = [[0x7F7F, int(bits([-0.5 * 2.0 ** 120])[0])] + [0] * 62, [0x7F7F] + [0] * 63]
+    for _ in range(200):
+        low = int(bits([-2.0 ** rng.uniform(60, 119.9)])[0])
+        rows.append([0x7F7F, low] + rng.integers(0x7000, 0x7F80, 62).tolist())
+    down = 0
+    for row in rows:
+        b = np.array(row, np.uint16)
+        v = oracle.bf16_bits_to_f64(b)
+        codes, s, m, bad = q4.quantize_group(b)
+        scale, least = oracle.bf16_bits_to_f64(np.array([s, m], np.uint16))
+        got = codes * scale + least
+        assert not bad and least == v.min() and got.max() < largest + 2.0 ** 119     # rounds to a finite bf16
+        assert np.abs(got - v).max() <= scale / 2 * (1 + 2.0 ** -20)
+        down += scale < (v.max() - v.min()) / 15
+    assert down > 20
+
+
 def test_pack_and_unpack_agree():
     rng = np.random.default_rng(1)
     for d in (64, 128):
