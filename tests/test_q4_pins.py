@@ -186,3 +186,25 @@ def test_rope_config_checks_its_sequences():
     assert ctypes.sizeof(c) == 16 + 64 + 256
     with pytest.raises(ValueError):  # two axes, one row of positions
         pd.pd_rope_tokens(None, c, torch.zeros(4, dtype=torch.int32), *[torch.zeros(64)] * 4, total=4, stream=0)
+
+
+def test_empty_tensors_do_not_pass_for_arguments_left_out():
+    """The address of an empty tensor is null, which the library reads as an argument that was not given."""
+    import paper_2609_35158_b200 as pd
+
+    x, none = torch.zeros(64, dtype=torch.int32), torch.zeros(0, dtype=torch.int32)
+    rope = pd.rope_config(64, np.ones(32), num_axes=2)
+    rows = torch.zeros((2, 8), dtype=torch.int32)
+    for positions in (rows[:, :0], torch.empty((2, 0), dtype=torch.int32)):
+        with pytest.raises(ValueError):
+            pd.pd_rope_append_tokens(None, rope, positions, x, x, x, x, x, x, x, x, x, 1, batch=1, stream=0)
+        with pytest.raises(ValueError):
+            pd.pd_rope_append_tokens_q4(None, rope, positions, x, x, x, x, x, x, x, x, 1, batch=1, stream=0)
+    with pytest.raises(ValueError):
+        pd.pd_kv_dequantize_q4(None, x, x, none, x, x, x, x, batch=1, stream=0)
+    # a step without sequences or without tokens may come with empty tensors: the library answers
+    for call in (lambda: pd.pd_rope_append_tokens(None, rope, rows[:, :0], x, x, x, x, x, x, x, x, x, 1, batch=0, stream=0),
+                 lambda: pd.pd_rope_append_tokens_q4(None, rope, rows[:, :0], x, x, x, x, x, x, x, x, 0, batch=1, stream=0),
+                 lambda: pd.pd_kv_dequantize_q4(None, x, x, none, x, x, x, x, batch=0, stream=0)):
+        with pytest.raises(pd.PdError):
+            call()
