@@ -508,7 +508,8 @@ typedef struct pd_rope_config {
  * are to bf16 pools or, quantised, to 4-bit pages, in one pass: pools, lengths and q_out are bit for bit those of
  * pd_rope_tokens followed by pd_kv_append_tokens / pd_kv_append_tokens_q4 (rotated keys are rounded to bf16 before they are
  * quantised). positions NULL: every axis stands at the token's index in its sequence, ctx_lens[b] + i. A sequence whose append is
- * skipped for its length or a page still gets its q_out. One token per sequence is q_indptr = 0, 1, 2, ... with max_q_len 1.
+ * skipped for its length, for a page or (_q4) for more than one token under max_q_len 1 still gets its q_out. One token per
+ * sequence is q_indptr = 0, 1, 2, ... with max_q_len 1.
  * PD_ERR_UNSUPPORTED: rot_dim not a multiple of 16; for _q4 also num_kv_heads * head_dim above 14336.
  */
 int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,

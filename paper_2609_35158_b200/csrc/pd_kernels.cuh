@@ -187,7 +187,7 @@ struct RopeParams {
     const int32_t *page_table;
     int32_t *ctx_lens;
     int32_t *status;
-    int32_t B, Hq, Hkv, D, MP, num_pages, total, advance, tile, pdl;
+    int32_t B, Hq, Hkv, D, MP, num_pages, total, advance, tile, single, pdl;  // single: one token per sequence was announced
 };
 
 struct AttnVariant {

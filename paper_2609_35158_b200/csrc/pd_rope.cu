@@ -125,7 +125,8 @@ __global__ void __launch_bounds__(kThreads, 5) rope_kernel(const __grid_constant
             return;
         }
     }
-    const bool room = APPEND != kNoAppend && L >= 0 && L <= p.MP * kPageSize - n;
+    // the append to 4-bit pages takes no more tokens than announced where that is one, and this stands for it
+    const bool room = APPEND != kNoAppend && L >= 0 && L <= p.MP * kPageSize - n && !(APPEND == kAppendQ4 && p.single && n > 1);
     if (APPEND != kNoAppend && !room && tid == 0 && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);
     const int half = p.rot_dim / 2;
     // rows of a token: q, then k, then (bf16 pages) v, which is copied; without room for them k and v are left out
@@ -237,6 +238,7 @@ cudaError_t launch_rope(const RopeParams &base, int append, int max_q_len, int n
     p.tile = p.tile < 1 ? 1 : (p.tile > most_tokens ? most_tokens : p.tile);
     const int tiles = (max_q_len + p.tile - 1) / p.tile, want = (num_sms * 64 + seqs - 1) / seqs;
     const dim3 grid(tiles < want ? tiles : want, seqs);
+    p.single = max_q_len == 1;
     const size_t dyn = append == kAppendQ4 ? static_cast<size_t>(p.tile) * p.Hkv * p.D * 2 : 0;
     auto go = [&](auto *k) { return launch_pdl(k, grid, dim3(kThreads), dyn, stream, p.pdl != 0, p); };
     cudaError_t err;

@@ -331,3 +331,34 @@ def test_a_multi_turn_run_over_the_4bit_cache(Hq, Hkv, d):
                 ref = q4.decode_attn(oracle.bf16_bits(qo), kv4.cpu().numpy(), table, lens, scale)
                 check_attention(out, lse, ref)
         assert pd.pd_device_status(ctx.h)[0] == 0 and L.cpu().tolist() == lens.tolist()
+
+
+@pytest.mark.parametrize("four", [False, True])
+@pytest.mark.parametrize("d", [64, 128])
+def test_more_tokens_than_announced_are_treated_as_by_the_two_calls(four, d):
+    """max_q_len 1 and a sequence of two tokens: the append to 4-bit pages leaves it out, the bf16 one takes it; queries are
+    rotated in any case."""
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv = 8, 2
+    before, new = np.array([3, 15, 0], np.int32), np.array([1, 2, 1], np.int32)
+    indptr, pos, q, k, v = packed(before, new, 70, Hq, Hkv, d, 1)
+    rope, table = pd.rope_config(d, frequencies(d)), dev(np.arange(6, dtype=np.int32).reshape(3, 2))
+    ip, ps = dev(indptr), dev(pos)
+    with Ctx(Hq, Hkv, d, 3, 2, 6) as ctx:
+        def pools():
+            if four:
+                return [torch.full((6, Hkv, 18 * d), 7, dtype=torch.uint8, device=DEV)]
+            return [torch.full((6, Hkv, P, d), 3.0, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+
+        a, b, La, Lb = pools(), pools(), dev(before), dev(before)
+        qa, ka, qb = torch.empty_like(q), torch.empty_like(k), torch.full_like(q, float("nan"))
+        pd.pd_rope_tokens(ctx.h, rope, ps, q, k, qa, ka)
+        (pd.pd_kv_append_tokens_q4 if four else pd.pd_kv_append_tokens)(ctx.h, ka, v, ip, *a, table, La, 1)
+        one = pd.pd_device_status(ctx.h)
+        (pd.pd_rope_append_tokens_q4 if four else pd.pd_rope_append_tokens)(ctx.h, rope, ps, q, k, v, ip, qb, *b, table, Lb, 1)
+        two = pd.pd_device_status(ctx.h)
+    assert one == two == ((pd.PD_ERR_DEVICE_FAULT, 1, 15) if four else (0, one[1], one[2]))
+    assert La.cpu().tolist() == Lb.cpu().tolist() == ([4, 15, 1] if four else [4, 17, 1])
+    assert torch.equal(qa.view(torch.int16), qb.view(torch.int16))
+    assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
