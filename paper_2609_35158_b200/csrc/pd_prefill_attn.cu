@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(256) kv_append_tokens_kernel(const AppendToken
     const int r0 = p.q_indptr[b], n = p.q_indptr[b + 1] - r0;
     const int L = p.ctx_lens[b];
     if (n <= 0) return;
-    if (L < 0 || (L + n + kPageSize - 1) / kPageSize > p.MP) {
+    if (L < 0 || L > p.MP * kPageSize - n) {  // (L + n can pass 32 bits)
         if (threadIdx.x == 0 && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);
         return;
     }
@@ -487,7 +487,7 @@ __global__ void advance_lens_kernel(const AppendTokensParams p) {
     const int n = p.q_indptr[b + 1] - p.q_indptr[b];
     const int L = p.ctx_lens[b];
     if (p.row_limit > 0 && p.q_indptr[b + 1] > p.row_limit) return;
-    if (n > 0 && L >= 0 && (L + n + kPageSize - 1) / kPageSize <= p.MP) p.ctx_lens[b] = L + n;
+    if (n > 0 && L >= 0 && L <= p.MP * kPageSize - n) p.ctx_lens[b] = L + n;
 }
 
 }  // namespace

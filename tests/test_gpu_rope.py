@@ -362,3 +362,31 @@ def test_more_tokens_than_announced_are_treated_as_by_the_two_calls(four, d):
     assert La.cpu().tolist() == Lb.cpu().tolist() == ([4, 15, 1] if four else [4, 17, 1])
     assert torch.equal(qa.view(torch.int16), qb.view(torch.int16))
     assert all(torch.equal(x.view(torch.uint8), y.view(torch.uint8)) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("length", [2 ** 31 - 1, 2 ** 31 - 4, 2 ** 31 - 17, -2 ** 31, 65])
+def test_appends_of_several_tokens_refuse_lengths_whose_sum_passes_32_bits(length):
+    """Lengths past the table row, some so far that length plus tokens wraps: latched, length and pools as they were."""
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv, d = 4, 2, 64
+    before, new = np.array([5, length, 0], np.int64).astype(np.int32), np.array([3, 20, 4], np.int32)
+    indptr, pos, q, k, v = packed(before, new, 80, Hq, Hkv, d, 1)
+    rope, table = pd.rope_config(d, frequencies(d)), dev(np.arange(12, dtype=np.int32).reshape(3, 4))
+    ip, qo = dev(indptr), torch.empty_like(q)
+    with Ctx(Hq, Hkv, d, 3, 4, 12) as ctx:
+        for form in range(4):
+            L, kv = dev(before), torch.zeros((12, Hkv, 18 * d), dtype=torch.uint8, device=DEV)
+            kp, vp = (torch.zeros((12, Hkv, P, d), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+            if form == 0:
+                pd.pd_kv_append_tokens(ctx.h, k, v, ip, kp, vp, table, L, 20)
+            elif form == 1:
+                pd.pd_kv_append_tokens_q4(ctx.h, k, v, ip, kv, table, L, 20)
+            elif form == 2:
+                pd.pd_rope_append_tokens(ctx.h, rope, None, q, k, v, ip, qo, kp, vp, table, L, 20)
+            else:
+                pd.pd_rope_append_tokens_q4(ctx.h, rope, None, q, k, v, ip, qo, kv, table, L, 20)
+            assert pd.pd_device_status(ctx.h) == (pd.PD_ERR_DEVICE_FAULT, 1, int(before[1])), form
+            assert L.cpu().tolist() == [8, int(before[1]), 4], form
+            touched = (kp != 0).flatten(1).any(1) if form % 2 == 0 else kv.flatten(1).any(1)
+            assert torch.nonzero(touched).flatten().tolist() == [0, 8], form
