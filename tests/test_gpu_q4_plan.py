@@ -1,5 +1,5 @@
-"""Decode attention over long contexts of 4-bit pages, against a plain reference in 64 bits with bounds that shrink with the
-length."""
+"""Decode attention over 4-bit pages: plans with more ranges than workers, whose ranges are claimed while the kernel runs, the
+largest automatic plans, long contexts. Against a plain reference in 64 bits with bounds that shrink with the length."""
 import math
 
 import numpy as np
@@ -75,6 +75,109 @@ def check_tight(out, lse, ref, what=""):
     check_attention(out, lse, ref[:4], what)
     error = np.sqrt(((out.float().cpu().numpy() - ref[0]) ** 2).mean(-1))
     assert np.all(error <= 1.25 * ref[4]), f"{what}: {(error / np.maximum(ref[4], 1e-300)).max()}"  # 64 or 128 outputs: their mean square scatters
+
+
+def bits(x):
+    return x.view(torch.int16) if x.dtype == torch.bfloat16 else x
+
+
+@pytest.mark.parametrize("Hq,Hkv,d", [(8, 2, 128), (16, 2, 128), (8, 2, 64), (16, 2, 64)])
+def test_more_ranges_than_workers(Hq, Hkv, d):
+    """Ranges of one page: workers claim most of them. The counters are left as the next call needs them: three calls in a
+    row, one with a plan of few ranges between, one of the bf16 kernel that claims from the same counters."""
+    import paper_2609_35158_b200 as pd
+
+    lens = np.array([4000, 6001, 0, 3999, 1, 4016, 4200, 3500, 5000], np.int32)
+    kv4, table, NP = random_cache(lens, Hkv, d, 300 + Hq)
+    q = wl.random_bf16((len(lens), Hq, d), 301, DEV)
+    kv, t, L = dev(kv4), dev(table), dev(lens)
+    ref = reference(q, kv, table, lens, 0.1)
+    k16, v16 = (wl.random_bf16((NP, Hkv, P, d), 302 + i, DEV) for i in range(2))
+    outs = []
+    with Ctx(Hq, Hkv, d, len(lens), table.shape[1], NP) as ctx:
+        def call(split):
+            out = torch.full((len(lens), Hq, d), float("nan"), dtype=torch.bfloat16, device=DEV)
+            lse = torch.full((len(lens), Hq), float("nan"), device=DEV)
+            pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, out, lse, sm_scale=0.1, split_pages=split)
+            plan = pd.pd_last_plan(ctx.h)
+            check_tight(out, lse, ref, f"split {split}")
+            return plan, out, lse
+
+        for split in (1, 1, 0, 1):
+            plan, out, lse = call(split)
+            if split == 1:
+                assert plan["num_ranges"] == Hkv * int(((lens + P - 1) // P).sum()) > plan["num_workers"]
+                outs.append((out, lse))
+            else:
+                assert plan["num_ranges"] <= plan["num_workers"]
+        a, b = torch.empty_like(q), torch.empty_like(q)
+        pd.pd_decode_attn(ctx.h, q, k16, v16, t, L, a, sm_scale=0.1, split_pages=1)
+        _, out, lse = call(1)
+        pd.pd_decode_attn(ctx.h, q, k16, v16, t, L, b, sm_scale=0.1, split_pages=1)
+        outs.append((out, lse))
+        torch.cuda.synchronize()
+        assert pd.pd_device_status(ctx.h)[0] == 0
+    assert torch.equal(bits(a), bits(b))
+    for out, lse in outs[1:]:  # who claims a range changes nothing
+        assert torch.equal(bits(out), bits(outs[0][0])) and torch.equal(lse, outs[0][1])
+
+
+def test_more_ranges_than_workers_captured_and_replayed():
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv, d = 8, 2, 128
+    lens = np.array([7000, 9001, 40, 5000], np.int32)
+    kv4, table, NP = random_cache(lens, Hkv, d, 310)
+    q = wl.random_bf16((len(lens), Hq, d), 311, DEV)
+    kv, t, L = dev(kv4), dev(table), dev(lens)
+    out, again = (torch.empty_like(q) for _ in range(2))
+    with Ctx(Hq, Hkv, d, len(lens), table.shape[1], NP) as ctx:
+        pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, out, sm_scale=0.1, split_pages=1)
+        plan = pd.pd_last_plan(ctx.h)
+        assert plan["num_ranges"] > plan["num_workers"]
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=side):
+                for _ in range(3):
+                    pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, again, sm_scale=0.1, split_pages=1)
+            for _ in range(3):
+                again.fill_(float("nan"))
+                graph.replay()
+        torch.cuda.synchronize()
+        assert pd.pd_device_status(ctx.h)[0] == 0
+    assert torch.equal(bits(out), bits(again))
+    check_tight(out, None, reference(q, kv, table, lens, 0.1))
+
+
+@pytest.mark.parametrize("Hq,d,longest", [(32, 128, 17000), (8, 64, 22000)])
+def test_a_batch_of_256_long_contexts(Hq, d, longest):
+    """More than 1024 pages per worker under the automatic plan, over a pool whose pages the sequences share."""
+    import paper_2609_35158_b200 as pd
+
+    Hkv, B, NP = 8, 256, 1400
+    rng = np.random.default_rng(320)
+    lens = rng.integers(longest - 1500, longest, B).astype(np.int32)
+    lens[[3, 100, 255]] = [0, 1, 17]
+    kv4, _, _ = random_cache([NP * P], Hkv, d, 321, poison=False)
+    kv4 = kv4[:NP]
+    table = np.stack([rng.permutation(NP)[:(longest + P - 1) // P] for _ in range(B)]).astype(np.int32)
+    q = wl.random_bf16((B, Hq, d), 322, DEV)
+    kv, t, L = dev(kv4), dev(table), dev(lens)
+    out = torch.full((B, Hq, d), float("nan"), dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((B, Hq), float("nan"), device=DEV)
+    out2, lse2 = torch.empty_like(out), torch.empty_like(lse)
+    with Ctx(Hq, Hkv, d, B, table.shape[1], NP) as ctx:
+        pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, out, lse, sm_scale=0.1)
+        plan = pd.pd_last_plan(ctx.h)
+        pd.pd_decode_attn_q4(ctx.h, q, kv, t, L, out2, lse2, sm_scale=0.1)
+        torch.cuda.synchronize()
+        assert pd.pd_device_status(ctx.h)[0] == 0
+    units = Hkv * int(((lens + P - 1) // P).sum())
+    assert units > 1024 * plan["num_workers"]
+    check_tight(out, lse, reference(q, kv, table, lens, 0.1))
+    assert torch.equal(bits(out), bits(out2)) and torch.equal(lse, lse2)
 
 
 @pytest.mark.parametrize("Hq,Hkv,d", [(32, 8, 128), (16, 2, 64), (8, 1, 128)])
