@@ -5,6 +5,7 @@ import torch
 
 import oracle
 from oracle import q4
+import workloads as wl
 from pd_testlib import Ctx
 from test_gpu_q4 import P, attend, bf16_dev, check_attention, dev, random_cache, table_for
 
@@ -75,3 +76,52 @@ def test_groups_next_to_the_largest_value_read_back_finite(d):
                                for i in range(n)]), 64, -1)
     # half a step of the code, and the rounding of the value read back to bf16
     assert np.all(np.abs(back - given) <= step / 2 * (1 + 2.0 ** -20) + 2.0 ** -8 * np.abs(back))
+
+
+def test_a_key_group_with_a_nan_reaches_every_row_of_its_kv_head_only():
+    """A NaN in K makes the logit NaN, and with it the softmax of every query head that reads that KV head."""
+    import paper_2609_35158_b200 as pd
+
+    for Hq, d in ((8, 128), (16, 64)):
+        Hkv, G = 2, Hq // 2
+        lens = np.array([40, 700], np.int32)
+        kv4, table, NP = random_cache(lens, Hkv, d, 220)
+        q = wl.random_bf16((2, Hq, d), 221, "cpu")
+        ref = q4.decode_attn(oracle.bf16_bits(q), kv4, table, lens, 0.1)
+        bad = kv4.copy()
+        bad[table[1, 1], 1, 16 * d:].view(np.uint16).reshape(P, d // 64, 4)[3, 0, :2] = [0x7FC0, 0]
+        for split in (0, 1, 100000):
+            out, lse = attend(pd, Hq, Hkv, d, q.to(DEV), bad, table, lens, NP, 0.1, split)
+            assert torch.isnan(out[1, G:].float()).all() and torch.isnan(lse[1, G:]).all()
+            for sel in ((0, slice(None)), (1, slice(0, G))):
+                check_attention(out[sel], lse[sel], [x[sel] for x in ref], f"{Hq} {d} split {split}")
+
+
+def ragged_case(seed):
+    """(Hq, Hkv, d, lengths, split_pages): every sequence draws its own length, empty ones and thousands of tokens among them."""
+    rng = np.random.default_rng(2000 + seed)
+    d, Hkv = [64, 128][seed % 2], int(rng.choice([1, 2, 3]))
+    n = int(rng.integers(3, 9))
+    lens = np.where(rng.random(n) < 0.2, 0, np.exp(rng.uniform(0, 8.6, n)) + rng.integers(0, 17, n)).astype(np.int32)
+    lens[rng.integers(0, n)] = int(rng.integers(2500, 6000))
+    return Hkv * [1, 2, 4, 8][(seed // 2) % 4], Hkv, d, lens, int(rng.choice([0, 0, 2, 7]))
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_ragged_random_batches(seed):
+    import paper_2609_35158_b200 as pd
+
+    Hq, Hkv, d, lens, split = ragged_case(seed)
+    assert len(set(lens.tolist())) > 1 and lens.max() >= 2500
+    rng = np.random.default_rng(2100 + seed)
+    kv4, table, NP = random_cache(lens, Hkv, d, 2200 + seed, scale_k=float(10 ** rng.uniform(-3, 0.5)), scale_v=float(10 ** rng.uniform(-3, 3)))
+    q = wl.random_bf16((len(lens), Hq, d), 2300 + seed, "cpu")
+    scale = float(rng.uniform(0.02, 0.3))
+    ref = q4.decode_attn(oracle.bf16_bits(q), kv4, table, lens, scale)
+    out, lse = attend(pd, Hq, Hkv, d, q.to(DEV), kv4, table, lens, NP, scale, split)
+    check_attention(out, lse, ref, f"seed {seed}: {Hq}/{Hkv} d={d} {lens.tolist()}")
+
+
+def test_ragged_cases_are_ragged():
+    cases = [ragged_case(s) for s in range(12)]
+    assert sum((c[3] == 0).any() for c in cases) >= 3 and {(c[0] // c[1], c[2]) for c in cases} >= {(g, d) for g in (1, 2, 4, 8) for d in (64, 128)}
