@@ -755,9 +755,11 @@ int decode_attn_q4(pd_ctx *ctx, const void *q, const void *kv4, const int32_t *p
     p.min_pages_auto = ctx->min_pages_auto;
     p.halving_levels = ctx->halving_levels;
     p.tail_pages = ctx->tail_pages;
-    // One equal range per worker as long as the FP8 kernel takes it: claiming short ranges late measured 168 against 145 us on
-    // 64 contexts of 2K-16K (32/8 heads) and 128 against 88 us on 64 lognormal ones (32/4 heads).
-    p.static_fair_max = kFp8StaticFairMax;
+    // One equal range per worker at every size; only split_pages makes ranges that are claimed. Claiming short ranges late, as
+    // the bf16 kernel does, against one range each: 168 against 145 us on 64 contexts of 2K-16K (32/8 heads), 128 against 88 on
+    // 64 lognormal ones (32/4 heads) in an early form; now, on 256 contexts, 790 against 780 us at 15K-16K tokens, 1325 against
+    // 1309 at 12K-40K (both 32/8), 1132 against 1110 at 12K-30K (64/8), 880 against 858 at 24K-40K (head_dim 64).
+    p.static_fair_max = INT32_MAX;
     const bool hooked = ctx->ev_before != nullptr;
     p.pdl = hooked ? 0 : ctx->pdl;
     p.merge_rows = ctx->merge_rows;
