@@ -58,6 +58,13 @@ int pd_host_step_counts(const pd_ctx *ctx, int64_t *direct, int64_t *staged);
  */
 int pd_read_probe(const void *src, size_t bytes, int32_t blocks, int32_t threads, void *sink16, void *stream);
 
+/*
+ * The conversion that the rotary entry points make of a frequency, on the host, without a context: *turns receives inv_freq
+ * (radians per position) as a 64-bit fixed-point fraction of a turn per position, whole turns dropped, off by less than
+ * 2^-63 turns. PD_ERR_INVALID_ARG for a null pointer and for a frequency that they refuse (NaN, 64 turns or more).
+ */
+int pd_rope_turns(float inv_freq, uint64_t *turns);
+
 #ifdef __cplusplus
 }
 #endif

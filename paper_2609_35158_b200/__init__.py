@@ -35,7 +35,7 @@ EXPORTS = (
     "pd_rope_tokens", "pd_rope_append_tokens", "pd_rope_append_tokens_q4",
     "pd_pool_create", "pd_pool_resize", "pd_pool_base", "pd_pool_capacity", "pd_pool_chunk_bytes", "pd_pool_resident_bytes",
     "pd_pool_last_error", "pd_pool_destroy",
-    "pd_set_profile_events", "pd_read_probe", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
+    "pd_set_profile_events", "pd_read_probe", "pd_rope_turns", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
 )
 
 
@@ -132,6 +132,7 @@ def _load() -> ctypes.CDLL:
     lib.pd_rope_append_tokens.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
     lib.pd_rope_append_tokens_q4.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
     u64 = ctypes.c_uint64
+    lib.pd_rope_turns.argtypes = [f32, ctypes.POINTER(u64)]
     lib.pd_pool_create.argtypes = [i32, u64, u64, ctypes.POINTER(vp)]
     lib.pd_pool_resize.argtypes = [vp, u64, vp]
     lib.pd_pool_destroy.argtypes = [vp]
@@ -366,6 +367,13 @@ def rope_config(rot_dim: int, inv_freq, axis_of_pair=None, num_axes: int = 1, ad
     c.axis_of_pair[:half] = axis
     c.inv_freq[:half] = inv_freq
     return c
+
+
+def pd_rope_turns(inv_freq: float) -> int:
+    """``inv_freq`` as the kernels take it: turns per position, times 2^64, modulo 2^64."""
+    turns = ctypes.c_uint64()
+    _check(_lib.pd_rope_turns(inv_freq, ctypes.byref(turns)), "pd_rope_turns")
+    return turns.value
 
 
 def _position_stride(positions, rope) -> int:

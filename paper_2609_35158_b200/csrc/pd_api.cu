@@ -792,6 +792,11 @@ uint64_t turns_fixed(float f) {
     return f < 0.f ? 0ull - fixed : fixed;
 }
 
+bool frequency_in_range(float f) {
+    const double turns = static_cast<double>(f) * 0.15915494309189533577;  // 1 / (2 pi)
+    return turns > -64.0 && turns < 64.0;  // NaN compares false
+}
+
 // Checks a rotation and lays it out for the kernels.
 int rope_params(pd_ctx *ctx, const pd_rope_config *rope, pd::RopeParams *p) {
     if (rope == nullptr) return fail(ctx, PD_ERR_INVALID_ARG, "rope: null configuration");
@@ -800,8 +805,7 @@ int rope_params(pd_ctx *ctx, const pd_rope_config *rope, pd::RopeParams *p) {
         return fail(ctx, PD_ERR_INVALID_ARG, "rope: rot_dim, num_axes, adjacent or magnitude out of range");
     if (rope->rot_dim % 16 != 0) return fail(ctx, PD_ERR_UNSUPPORTED, "rope: rot_dim must be a multiple of 16");
     for (int i = 0; i < rope->rot_dim / 2; ++i) {
-        const double turns = static_cast<double>(rope->inv_freq[i]) * 0.15915494309189533577;  // 1 / (2 pi)
-        if (rope->axis_of_pair[i] >= rope->num_axes || !(turns > -64.0 && turns < 64.0))
+        if (rope->axis_of_pair[i] >= rope->num_axes || !frequency_in_range(rope->inv_freq[i]))
             return fail(ctx, PD_ERR_INVALID_ARG, "rope: axis or frequency of a pair out of range");
         p->freq[i] = turns_fixed(rope->inv_freq[i]);
         p->axis_of_pair[i] = rope->axis_of_pair[i];
@@ -925,6 +929,12 @@ int pd_decode_step_q4(pd_ctx *ctx, const void *q, const void *k_new, const void 
     if (int rc = q4_attn_check_args(ctx, "pd_decode_step_q4", q, kv4, page_table, ctx_lens, out, batch, sm_scale, split_pages)) return rc;
     if (int rc = append_q4(ctx, "pd_decode_step_q4", k_new, v_new, nullptr, kv4, page_table, ctx_lens, batch, 1, 0u, stream)) return rc;
     return decode_attn_q4(ctx, q, kv4, page_table, ctx_lens, out, lse, batch, sm_scale, split_pages, stream);
+}
+
+int pd_rope_turns(float inv_freq, uint64_t *turns) {
+    if (turns == nullptr || !frequency_in_range(inv_freq)) return PD_ERR_INVALID_ARG;
+    *turns = turns_fixed(inv_freq);
+    return PD_OK;
 }
 
 int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,

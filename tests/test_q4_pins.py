@@ -208,3 +208,27 @@ def test_empty_tensors_do_not_pass_for_arguments_left_out():
                  lambda: pd.pd_kv_dequantize_q4(None, x, x, none, x, x, x, x, batch=0, stream=0)):
         with pytest.raises(pd.PdError):
             call()
+
+
+def test_frequencies_are_converted_to_turns_exactly():
+    """The library's own conversion against integers: any sign and size, and the angle at any int32 position."""
+    from test_gpu_rope import inv_two_pi
+    import paper_2609_35158_b200 as pd
+
+    bits_ = 400
+    unit, rng = inv_two_pi(bits_), np.random.default_rng(8)
+    freqs = [0.0, -0.0, 1.0, -1.0, 2.0 ** -126, 2.0 ** -149, -2.0 ** -140, 2.0 ** -40, 402.0, -402.0, np.pi, 2 * np.pi, 6.2831855, 1e-38]
+    freqs += (2.0 ** rng.uniform(-130, 8.6, 300) * rng.choice([-1, 1], 300)).tolist()
+    freqs += (10000.0 ** (-np.arange(64) / 64)).tolist()
+    for f in np.array(freqs, np.float32):
+        num, den = float(f).as_integer_ratio()
+        got = pd.pd_rope_turns(float(f))
+        assert 0 <= got < 2 ** 64
+        for pos in [1, -1, 2 ** 31 - 1, -2 ** 31, *rng.integers(-2 ** 31, 2 ** 31, 5).tolist()]:
+            whole = den << bits_                                              # one turn, in units of 2^-bits / den
+            off = ((got * pos << bits_) * den - (num * unit * pos << 64)) % (whole << 64)
+            off = min(off, (whole << 64) - off)                               # the shorter way round
+            assert off <= abs(pos) * whole * 2, (f, pos)                      # 2^-63 turns for each position
+    for bad in (float("nan"), float("inf"), 403.0, -403.0):
+        with pytest.raises(pd.PdError):
+            pd.pd_rope_turns(bad)
