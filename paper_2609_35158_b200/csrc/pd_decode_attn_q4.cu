@@ -682,6 +682,12 @@ __global__ void __launch_bounds__(WARPS * 32, 1) decode_attn_split_q4_kernel(con
             advance(cur, cum, p.B, p.Hkv);
         }
     }
+    if (!alive) {  // copies may still be on their way: shared memory is not given back without another bounded wait for them
+        for (; inflight > 0; --inflight) {
+            mbar_wait(full + stage * 8, parity);
+            if (++stage == STAGES) { stage = 0; parity ^= 1u; }
+        }
+    }
     if (lane == 0) {
         if (!alive) latch_status(p.status, kDevTimeout, -1, worker);
         if (claims && atomicAdd(p.status + kSchedDone, 1) == n_workers - 1) {  // the last worker re-arms the claim counter
