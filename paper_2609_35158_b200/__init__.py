@@ -158,10 +158,14 @@ def _ptr(t) -> int:
     return 0 if t is None else t.data_ptr()
 
 
-def _refuse_empty(t, name: str):
-    """An argument that may be None: an empty tensor's address is null too, and must not pass for None."""
-    if t is not None and t.numel() == 0:
+def _optional_ptr(t, needed: bool, name: str) -> int:
+    """An argument that may be None. The address of an empty tensor is null too, and must not pass for None where it counts."""
+    if t is None:
+        return 0
+    p = t.data_ptr()
+    if p == 0 and needed:
         raise ValueError(f"{name}: an empty tensor; pass None to leave it out")
+    return p
 
 
 def _stream(stream) -> int:
@@ -335,23 +339,22 @@ def pd_kv_append_tokens_q4(ctx, k_new, v_new, q_indptr, kv4, page_table, ctx_len
 def pd_kv_dequantize_q4(ctx, kv4, page_table, first_token, ctx_lens, k_pages, v_pages, dst_page_table, batch=None, stream=None):
     """``first_token`` may be None (every sequence from its first token)."""
     batch = ctx_lens.shape[0] if batch is None else batch
-    if batch > 0:
-        _refuse_empty(first_token, "first_token")
-    _check(_lib.pd_kv_dequantize_q4(ctx, _ptr(kv4), _ptr(page_table), _ptr(first_token), _ptr(ctx_lens), _ptr(k_pages),
-                                    _ptr(v_pages), _ptr(dst_page_table), batch, _stream(stream)), "pd_kv_dequantize_q4", ctx)
+    first = _optional_ptr(first_token, batch > 0, "first_token")
+    _check(_lib.pd_kv_dequantize_q4(ctx, _ptr(kv4), _ptr(page_table), first, _ptr(ctx_lens), _ptr(k_pages), _ptr(v_pages),
+                                    _ptr(dst_page_table), batch, _stream(stream)), "pd_kv_dequantize_q4", ctx)
 
 
 def pd_decode_attn_q4(ctx, q, kv4, page_table, ctx_lens, out, lse=None, batch=None, sm_scale=1.0, split_pages=0, stream=None):
     batch = q.shape[0] if batch is None else batch
-    _check(_lib.pd_decode_attn_q4(ctx, _ptr(q), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens), _ptr(out), _ptr(lse), batch,
-                                  sm_scale, split_pages, _stream(stream)), "pd_decode_attn_q4", ctx)
+    _check(_lib.pd_decode_attn_q4(ctx, _ptr(q), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens), _ptr(out),
+                                  _optional_ptr(lse, batch > 0, "lse"), batch, sm_scale, split_pages, _stream(stream)), "pd_decode_attn_q4", ctx)
 
 
 def pd_decode_step_q4(ctx, q, k_new, v_new, kv4, page_table, ctx_lens, out, lse=None, batch=None, sm_scale=1.0, split_pages=0,
                       stream=None):
     batch = q.shape[0] if batch is None else batch
     _check(_lib.pd_decode_step_q4(ctx, _ptr(q), _ptr(k_new), _ptr(v_new), _ptr(kv4), _ptr(page_table), _ptr(ctx_lens),
-                                  _ptr(out), _ptr(lse), batch, sm_scale, split_pages, _stream(stream)),
+                                  _ptr(out), _optional_ptr(lse, batch > 0, "lse"), batch, sm_scale, split_pages, _stream(stream)),
            "pd_decode_step_q4", ctx)
 
 
@@ -395,9 +398,8 @@ def pd_rope_append_tokens(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out
                           max_q_len, batch=None, call_flags=0, stream=None):
     """``positions`` may be None: every axis stands at the token's index in its sequence."""
     batch = q_indptr.shape[0] - 1 if batch is None else batch
-    if batch > 0 and max_q_len > 0:
-        _refuse_empty(positions, "positions")
-    _check(_lib.pd_rope_append_tokens(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
+    at = _optional_ptr(positions, batch > 0 and max_q_len > 0, "positions")
+    _check(_lib.pd_rope_append_tokens(ctx, ctypes.byref(rope), at, _position_stride(positions, rope), _ptr(q),
                                       _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
                                       _ptr(page_table), _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
            "pd_rope_append_tokens", ctx)
@@ -406,9 +408,8 @@ def pd_rope_append_tokens(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out
 def pd_rope_append_tokens_q4(ctx, rope, positions, q, k_new, v_new, q_indptr, q_out, kv4, page_table, ctx_lens, max_q_len,
                              batch=None, call_flags=0, stream=None):
     batch = q_indptr.shape[0] - 1 if batch is None else batch
-    if batch > 0 and max_q_len > 0:
-        _refuse_empty(positions, "positions")
-    _check(_lib.pd_rope_append_tokens_q4(ctx, ctypes.byref(rope), _ptr(positions), _position_stride(positions, rope), _ptr(q),
+    at = _optional_ptr(positions, batch > 0 and max_q_len > 0, "positions")
+    _check(_lib.pd_rope_append_tokens_q4(ctx, ctypes.byref(rope), at, _position_stride(positions, rope), _ptr(q),
                                          _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(kv4), _ptr(page_table),
                                          _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
            "pd_rope_append_tokens_q4", ctx)

@@ -202,6 +202,10 @@ def test_empty_tensors_do_not_pass_for_arguments_left_out():
             pd.pd_rope_append_tokens_q4(None, rope, positions, x, x, x, x, x, x, x, x, 1, batch=1, stream=0)
     with pytest.raises(ValueError):
         pd.pd_kv_dequantize_q4(None, x, x, none, x, x, x, x, batch=1, stream=0)
+    for call in (lambda: pd.pd_decode_attn_q4(None, x, x, x, x, x, none, batch=1, stream=0),
+                 lambda: pd.pd_decode_step_q4(None, x, x, x, x, x, x, x, none, batch=1, stream=0)):
+        with pytest.raises(ValueError):
+            call()
     # a step without sequences or without tokens may come with empty tensors: the library answers
     for call in (lambda: pd.pd_rope_append_tokens(None, rope, rows[:, :0], x, x, x, x, x, x, x, x, x, 1, batch=0, stream=0),
                  lambda: pd.pd_rope_append_tokens_q4(None, rope, rows[:, :0], x, x, x, x, x, x, x, x, 0, batch=1, stream=0),
