@@ -97,6 +97,21 @@ def test_a_key_group_with_a_nan_reaches_every_row_of_its_kv_head_only():
                 check_attention(out[sel], lse[sel], [x[sel] for x in ref], f"{Hq} {d} split {split}")
 
 
+@pytest.mark.parametrize("gain", [2.0 ** 95, 2.0 ** -90])
+@pytest.mark.parametrize("Hq,d", [(8, 128), (16, 64)])
+def test_attention_at_the_documented_ends_of_q_and_v(gain, Hq, d):
+    """q and V some binades below 2^100 and as far down, over a K that leaves the logits as they are."""
+    import paper_2609_35158_b200 as pd
+
+    lens = np.array([40, 900, 1], np.int32)
+    kv4, table, NP = random_cache(lens, 2, d, 230, scale_k=0.3 / gain, scale_v=0.3 * gain)
+    q = (wl.random_bf16((3, Hq, d), 231, "cpu").float() * gain).to(torch.bfloat16)
+    ref = q4.decode_attn(oracle.bf16_bits(q), kv4, table, lens, 0.1)
+    for split in (0, 1, 100000):
+        out, lse = attend(pd, Hq, 2, d, q.to(DEV), kv4, table, lens, NP, 0.1, split)
+        check_attention(out, lse, ref, f"gain {gain} split {split}")
+
+
 def ragged_case(seed):
     """(Hq, Hkv, d, lengths, split_pages): every sequence draws its own length, empty ones and thousands of tokens among them."""
     rng = np.random.default_rng(2000 + seed)
