@@ -436,11 +436,13 @@ int pd_kv_scatter_fp8(pd_ctx *ctx, const void *packed, const int64_t *packed_pag
  * A value is scale * code + min, code in [0, 15]. Quantising a group: min = its smallest value (a bf16, stored exactly);
  * scale = (max - min) / 15 in fp32, rounded UP to bf16, or down where 15 * scale + min would round past bf16's largest value;
  * code = (x - min) / scale to the nearest integer, ties to even, with x - min rounded to fp32. So a finite value stays finite
- * and is off by at most scale / 2. Inputs below 2^-126 in magnitude count as 0, a
- * scale below 2^-100 as 0 (every code 0). A group that holds a NaN or infinity, or whose max - min leaves fp32, gets the
- * scale NaN: all of it reads back as NaN. A token's row never touches another token's bytes, so slots can be written
- * in any order. head_dim 64 or 128. Calls of one context share its workspace: enqueue them on one stream or order
- * them with events. None of them allocates or synchronises, so all can be captured in CUDA graphs after one eager call.
+ * and is off by at most scale / 2. Inputs below 2^-126 in magnitude count as 0, a scale below 2^-100 as 0 (every code 0). A
+ * group that holds a NaN or infinity, or whose max - min leaves fp32, gets the scale NaN: all of it reads back as NaN. A
+ * token's row never touches another token's bytes, so slots can be written in any order. There is no gather or scatter of
+ * 4-bit pages: a cache that moves between GPUs does so in bf16 or FP8 pages (pd_kv_gather and the like, after
+ * pd_kv_dequantize_q4 where it is held in 4 bits), or is written where it is read. head_dim 64 or 128. Calls of one context
+ * share its workspace: enqueue them on one stream or order them with events. None of them allocates or synchronises, so all
+ * can be captured in CUDA graphs after one eager call.
  */
 
 /*
@@ -470,8 +472,11 @@ int pd_kv_dequantize_q4(pd_ctx *ctx, const void *kv4, const int32_t *page_table,
 
 /*
  * pd_decode_attn over 4-bit pages: same outputs, plan, split_pages meaning, error behaviour and bit-reproducibility.
- * K and V are scale * code + min unrounded. q must be finite and below 2^100; the products run in fp16 with fp32
- * accumulation, q scaled per head to fp16's range.
+ * K and V are scale * code + min unrounded. q must be finite, q and the cached values below 2^100 in magnitude; the products
+ * run in fp16 with fp32 accumulation, q scaled per head to fp16's range. Probability times V scale is rounded to fp16 (2^-11 of
+ * itself) relative to the largest such weight of the head in a worker's range: below 2^-16 of that it loses bits, below 2^-27
+ * it counts as 0 (so the V groups of one token may differ by some 2^16 in size before the smaller ones lose accuracy).
+ * A NaN group of K makes out and lse of every query head of its KV head NaN, one of V the 64 output columns of that group.
  * pd_decode_step_q4: pd_kv_append_q4 (advancing) followed by pd_decode_attn_q4, enqueued by one call after every
  * argument is validated; ctx_lens holds the lengths BEFORE the append on entry.
  */
@@ -485,8 +490,8 @@ int pd_decode_step_q4(pd_ctx *ctx, const void *q, const void *k_new, const void 
  *
  * The first rot_dim values of a head form rot_dim / 2 pairs: (i, i + rot_dim / 2), or (2i, 2i + 1) with `adjacent`.
  * Pair i turns by position[axis_of_pair[i]] * inv_freq[i] radians: (a, b) -> magnitude * (a cos - b sin, a sin + b cos).
- * Values past rot_dim are copied. The angle is off by less than 2^-31 turns at every int32 position, then rounded to fp32; sums are fp32, results are
- * rounded once to bf16. The structure lies in HOST memory and is read during the call. */
+ * Values past rot_dim are copied. The angle is off by less than 2^-31 turns at every int32 position, then rounded to fp32;
+ * sums are fp32, results are rounded once to bf16. The structure lies in HOST memory and is read during the call. */
 typedef struct pd_rope_config {
     int32_t rot_dim;          /* multiple of 16, 16 .. head_dim                                          */
     int32_t num_axes;         /* 1 .. 4                                                                   */

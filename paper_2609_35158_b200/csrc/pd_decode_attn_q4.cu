@@ -37,12 +37,12 @@
 // 0.03 % of the output's rms to bf16's 0.17: adding 7.5 times the rounding to the minima's sum, which takes out the codes' mean,
 // halved that and made the long batches 1 to 2.5 % slower (2 to 4 % under the power limit).
 //
-// Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, 187 per page at head_dim 128 and four
-// heads, 205 at eight. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
+// Bound by its bytes (18 D per page and KV head) and nearly as much by its instructions, 193 per page at head_dim 128 and four
+// heads, 227 at eight. Steps and what they gave on 64 contexts of 2K-16K at 32/8 heads, 713 MB (us): a page at a time with a scale
 // reference for V beside the softmax maximum 193; two pages, one reference, minima by mma, bytes as V operands 147;
-// independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119,
-// which is 0.93 of the copy bandwidth (126, 0.88, when it runs for long and the power limit takes the SM clock to about
-// 1.8 GHz). The skeleton without arithmetic takes 117. Pages fetched four at a time by a TMA gather instead of four bulk
+// independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119;
+// folds and the check of the minima 120, which is 0.92 of the copy bandwidth (132 to 135, 0.82 to 0.84, when it runs for long
+// and the power limit takes the SM clock to about 1.8 GHz). The skeleton without arithmetic takes 117. Pages fetched four at a time by a TMA gather instead of four bulk
 // copies: 1 % slower at head_dim 128. Partial results merged inside this kernel instead of by the next one: 2 us slower.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
@@ -706,8 +706,8 @@ constexpr size_t q4_smem_bytes() {
 // Worker warps x stages x pages per tile. A tile costs about 140 instructions beside its pages, so large tiles pay; the
 // warps have to be the same number on each of the four schedulers, because they get equal ranges (14 and 15 lose to 12).
 // One stage is enough: with its V codes in registers a worker hands the stage back before its last products, and the
-// other workers' copies keep the memory busy. Measured, 64 contexts of 2K-16K at 32/8 heads, head_dim 128 (us):
-// 12 x 1 x 4 119.0, 12 x 1 x 5 119.0 (but 13 % slower on 3K tokens per sequence), 16 x 1 x 3 120.3, 12 x 2 x 3 121.9,
+// other workers' copies keep the memory busy. Measured before O was folded, 64 contexts of 2K-16K at 32/8 heads, head_dim 128 (us):
+// 12 x 1 x 4 119.0, 12 x 1 x 5 119.0 (but 13 % slower on short contexts), 16 x 1 x 3 120.3, 12 x 2 x 3 121.9,
 // 12 x 1 x 3 124.0, 8 x 2 x 4 126.2. head_dim 64, same lengths / 37 sequences of 0-5000 tokens at 16/2 heads:
 // 16 x 1 x 4 73.2 / 19.2, 16 x 1 x 6 69.3 / 20.1, 16 x 2 x 4 73.2 / 19.7, 12 x 2 x 4 74.6 / 19.3.
 constexpr int kQ4Warps = 12, kQ4Warps64 = 16, kQ4Stages = 1, kQ4TilePages = 4;

@@ -4,7 +4,8 @@
 // position[axis(i)] * inv_freq[i]. Far positions: an fp32 product of position and frequency loses the angle's
 // fraction of a turn (at position 10^6 a float angle steps by 1/16 rad). Here a frequency is a 64-bit fixed-point
 // fraction of a turn and the product with the position wraps modulo 2^64, i.e. modulo whole turns, exactly; its top
-// 32 bits are the angle to 2^-32 turns. The frequency itself is rounded once, to 2^-53 of its value.
+// 32 bits are the angle to 2^-32 turns. The frequency itself is off by less than 2^-63 turns (the host converts it in integers),
+// so the angle by less than 2^-31 at every int32 position.
 //
 // Bound by its bytes: every row is read and written once. The sines of a token serve all its heads, so a CTA computes
 // them once per token into shared memory, laid out so that the lanes of a row read neighbouring 16 bytes. A lane holds two
@@ -31,7 +32,8 @@ __device__ __forceinline__ void latch(int32_t *status, int code, int seq, int de
 constexpr int kThreads = 256;
 template <int D>
 constexpr int kRopeTokens = D == 128 ? 4 : 16;  // most tokens a CTA takes at a time
-constexpr int kRopeRowBytes = 28672;  // rotated K rows a CTA may hold in shared memory, beside 17 KB of sines
+// rotated K rows a CTA may hold in shared memory: beside at most 8.3 KB of sines and page ids, five CTAs still fit an SM
+constexpr int kRopeRowBytes = 28672;
 
 // pairs of the half-split form: x holds the first elements, y the second
 __device__ __forceinline__ void rotate2(uint32_t &x, uint32_t &y, const float4 &cs) {
