@@ -475,7 +475,7 @@ int pd_kv_dequantize_q4(pd_ctx *ctx, const void *kv4, const int32_t *page_table,
  * K and V are scale * code + min unrounded. q must be finite, q and the cached values below 2^100 in magnitude; the products
  * run in fp16 with fp32 accumulation, q scaled per head to fp16's range. Probability times V scale is rounded to fp16 (2^-11 of
  * itself) relative to the largest such weight of the head in a worker's range: below 2^-16 of that it loses bits, below 2^-27
- * it counts as 0 (so the V groups of one token may differ by some 2^16 in size before the smaller ones lose accuracy).
+ * it counts as 0. (The two V groups of a head share that scale; one may be some 2^8 smaller than the other and keep its accuracy.)
  * A NaN group of K makes out and lse of every query head of its KV head NaN, one of V the 64 output columns of that group.
  * pd_decode_step_q4: pd_kv_append_q4 (advancing) followed by pd_decode_attn_q4, enqueued by one call after every
  * argument is validated; ctx_lens holds the lengths BEFORE the append on entry.

@@ -112,6 +112,30 @@ def test_attention_at_the_documented_ends_of_q_and_v(gain, Hq, d):
         check_attention(out, lse, ref, f"gain {gain} split {split}")
 
 
+@pytest.mark.parametrize("small", [0, 1])
+@pytest.mark.parametrize("Hq", [4, 8])
+def test_the_smaller_of_two_v_groups_keeps_its_accuracy(Hq, small):
+    """V groups of one head that differ by 2^8. Beside the usual bound, a weight may be off by half of fp16's smallest step,
+    2^-25, where the head's largest is at least 2^2, times a code of up to 15."""
+    import paper_2609_35158_b200 as pd
+
+    d, lens = 128, np.array([1500, 33], np.int32)
+    kv4, table, NP = random_cache(lens, 1, d, 240, poison=False)
+    rec = kv4[..., 16 * d:].view(np.uint16).reshape(NP, 1, P, 2, 4)
+    rec[..., small, 2:] = oracle.f32_to_bf16_bits((oracle.bf16_bits_to_f64(rec[..., small, 2:]) / 256).astype(np.float32))
+    q = wl.random_bf16((2, Hq, d), 241, "cpu")
+    out_, lse_, tol, tol_lse = q4.decode_attn(oracle.bf16_bits(q), kv4, table, lens, 0.1)
+    for b in range(2):
+        k, _, steps = q4.sequence_values(kv4, table, b, int(lens[b]), 0, d)
+        z = np.float64(np.float32(0.1)) * (k @ oracle.bf16_bits_to_f64(oracle.bf16_bits(q[b])).T)     # [n, Hq]
+        largest = (np.exp(z - z.max(0)) / np.exp(z - z.max(0)).sum(0) * (steps[0].max(1) / 15)[:, None]).max(0)
+        tol[b] += (lens[b] * 15 * 2.0 ** -27 * largest)[:, None]
+    assert np.abs(out_[0][:, 64 * small:64 * small + 64]).max() < 0.1 * np.abs(out_[0]).max()
+    for split in (0, 7, 100000):
+        out, lse = attend(pd, Hq, 1, d, q.to(DEV), kv4, table, lens, NP, 0.1, split)
+        check_attention(out, lse, (out_, lse_, tol, tol_lse), f"split {split}")
+
+
 def ragged_case(seed):
     """(Hq, Hkv, d, lengths, split_pages): every sequence draws its own length, empty ones and thousands of tokens among them."""
     rng = np.random.default_rng(2000 + seed)
