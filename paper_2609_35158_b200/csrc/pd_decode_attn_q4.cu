@@ -29,10 +29,10 @@
 //     softmax between the products costs two pages what it cost one. O has both pages' sums apart and adds them at the end
 //     (134 -> 130 us on 64 contexts of 2K-16K at 32/8 heads, 79 -> 73 us at head_dim 64; both under the power limit).
 //   * the tensor core cuts what lies below fp32's last bit off its sums. Codes and weights are positive, so O fell behind with
-//     every product of a long segment, and the minima, summed exactly, did not: 65536 tokens in one segment were off by 6 to
-//     13 % of the output's rms (1024 pages: 1 to 3 %, 256: 0.3 to 0.6 %). So every 32 products of a lane's columns O is folded
-//     into shared memory, rounded to nearest: 0.18 %, of which bf16 is 0.17. It costs 0.7 to 1.2 % on the long
-//     batches; folds twice as far apart save nothing and leave 0.20 %.
+//     every product of a long segment, and the minima, whose sums are rounded, did not: 65536 tokens in one segment were off
+//     by 6 to 13 % of the output's rms (1024 pages: 1 to 3 %, 256: 0.3 to 0.6 %). So every 32 products of a lane's columns O is
+//     folded into shared memory, rounded to nearest: 0.18 %, of which bf16 is 0.17. It costs 0.7 to 1.2 % on the long batches;
+//     folds twice as far apart save nothing and leave 0.20 %.
 // Sums, statistics, O and the rank-one terms are fp32. Weights p_t sv_t are rounded to fp16, 2^-11 of each at most, which adds
 // 0.03 % of the output's rms to bf16's 0.17: adding 7.5 times the rounding to the minima's sum, which takes out the codes' mean,
 // halved that and made the long batches 1 to 2.5 % slower (2 to 4 % under the power limit).
@@ -42,8 +42,9 @@
 // reference for V beside the softmax maximum 193; two pages, one reference, minima by mma, bytes as V operands 147;
 // independent chains of products, nothing cleared beforehand 129; four pages per tile 124; pages marked evict-first 119;
 // folds and the check of the minima 120, which is 0.92 of the copy bandwidth (132 to 135, 0.82 to 0.84, when it runs for long
-// and the power limit takes the SM clock to about 1.8 GHz). The skeleton without arithmetic takes 117. Pages fetched four at a time by a TMA gather instead of four bulk
-// copies: 1 % slower at head_dim 128. Partial results merged inside this kernel instead of by the next one: 2 us slower.
+// and the power limit takes the SM clock to about 1.8 GHz). The skeleton without arithmetic takes 117. Pages fetched four at
+// a time by a TMA gather instead of four bulk copies: 1 % slower at head_dim 128. Partial results merged inside this kernel
+// instead of by the next one: 2 us slower.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
