@@ -49,6 +49,7 @@ extern "C" {
 
 /* pd_config.flags */
 #define PD_FLAG_NONE 0u
+#define PD_FLAG_LATENT 1u /* a context for the *_latent calls: one shared latent vector per cached token */
 /* pd_kv_append call_flags */
 #define PD_APPEND_NO_ADVANCE 1u /* leave ctx_lens unchanged */
 
@@ -527,6 +528,44 @@ int pd_rope_append_tokens_q4(pd_ctx *ctx, const pd_rope_config *rope, const int3
                              const void *q, const void *k_new, const void *v_new, const int32_t *q_indptr, void *q_out,
                              void *kv4, const int32_t *page_table, int32_t *ctx_lens, int32_t batch, int32_t max_q_len,
                              uint32_t call_flags, void *stream);
+
+/* ---- A cache of one shared latent vector per token. The paper has no counterpart; the reason is that of the FP8 and 4-bit
+ * pages (fewer bytes read per concurrent sequence, Eq. 1): a token is one row for all heads.
+ *   kv_pages  [num_pages][16][576] bf16, device, 16-byte aligned. A row is a latent c of 512 values and a rotated
+ *             key part r of 64.
+ * Head h has K_h = (W_h[0:128] c, r) and V_h = W_h[128:256] c with the model's W [num_q_heads][256][512]. Attention in the absorbed
+ * form multiplies W into the queries and outputs instead: logits q . (c, r) with q = (W_h[0:128]^T q_nope, q_rope), output
+ * sum p c, to be multiplied by W_h[128:256] by the caller.
+ * These calls need a context of their own: pd_create with PD_FLAG_LATENT, num_q_heads in [1, 128], num_kv_heads 1,
+ * head_dim 512, page_size 16; the other calls on caches and rotations refuse such a context, and these any other, with
+ * PD_ERR_UNSUPPORTED. Calls of one context share its workspace: enqueue them on one stream or order them with events. None of
+ * them allocates or synchronises, so all can be captured in CUDA graphs after one eager call with the same pointers.
+ */
+
+/*
+ * Append of packed new tokens (rows as in pd_kv_append_tokens; one token per sequence is q_indptr = 0, 1, 2, ... with max_q_len
+ * 1). Row t of kv_new (kv_stride values apart, at least 576, a multiple of 8) is (c, r) as it leaves its projection:
+ * the cache gets c / sqrt(mean(c^2) + norm_eps) * norm_weight ([512] bf16; NULL: c as it is) and r rotated, each
+ * computed in fp32 and rounded once to bf16. q_rope, the 64 values per query head that are rotated with the same position, goes to
+ * q_out; both NULL: no queries. Their rows are addressed by strides in values (multiples of 8) over tokens and heads, so that they
+ * may lie inside wider rows; q_out may be q_rope with the same strides, and its rows must not overlap. Rotation, positions (NULL: the
+ * token's index in its sequence), skipping and error reporting as in pd_rope_append_tokens, with rot_dim at most 64.
+ */
+int pd_rope_append_tokens_latent(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                                 const void *q_rope, int64_t q_token_stride, int64_t q_head_stride, const void *kv_new,
+                                 int64_t kv_stride, const void *norm_weight, float norm_eps, const int32_t *q_indptr, void *q_out,
+                                 int64_t q_out_token_stride, int64_t q_out_head_stride, void *kv_pages, const int32_t *page_table,
+                                 int32_t *ctx_lens, int32_t batch, int32_t max_q_len, uint32_t call_flags, void *stream);
+
+/*
+ * Decode attention in the absorbed form: q [batch][num_q_heads][576], out [batch][num_q_heads][512] bf16,
+ * lse [batch][num_q_heads] fp32 or NULL. out[b][h] = softmax(sm_scale * q[b][h] . (c, r)) c over the ctx_lens[b] cached tokens;
+ * empty contexts, unread slots, sm_scale, split_pages (pages per range of the flattened (sequence, page) list) and error behaviour
+ * as in pd_decode_attn. Results are bit-reproducible. Probabilities are rounded to bf16 before the second product; the
+ * sum that normalises the output adds the rounded ones, lse the unrounded.
+ */
+int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_table, const int32_t *ctx_lens,
+                          void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream);
 
 /* ---- Elastic KV pool on CUDA virtual memory management (Sec. 4.6: the intra-scale toggle keeps the
  * rollout process and swaps device state; Sec. 5: the KV cache is released when training begins and

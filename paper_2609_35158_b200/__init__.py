@@ -23,6 +23,7 @@ PD_ERR_WORKSPACE = -4
 PD_ERR_DEVICE_FAULT = -5
 PD_ERR_TIMEOUT = -6
 PD_APPEND_NO_ADVANCE = 1
+PD_FLAG_LATENT = 1
 
 # every symbol include/pd.h declares
 EXPORTS = (
@@ -33,6 +34,7 @@ EXPORTS = (
     "pd_kv_quantize_pages", "pd_kv_append_fp8", "pd_decode_attn_fp8", "pd_decode_step_fp8", "pd_kv_gather_fp8", "pd_kv_scatter_fp8",
     "pd_kv_append_q4", "pd_kv_append_tokens_q4", "pd_kv_dequantize_q4", "pd_decode_attn_q4", "pd_decode_step_q4",
     "pd_rope_tokens", "pd_rope_append_tokens", "pd_rope_append_tokens_q4",
+    "pd_rope_append_tokens_latent", "pd_decode_attn_latent",
     "pd_pool_create", "pd_pool_resize", "pd_pool_base", "pd_pool_capacity", "pd_pool_chunk_bytes", "pd_pool_resident_bytes",
     "pd_pool_last_error", "pd_pool_destroy",
     "pd_set_profile_events", "pd_read_probe", "pd_rope_turns", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
@@ -131,6 +133,9 @@ def _load() -> ctypes.CDLL:
     lib.pd_rope_tokens.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, i32, vp]
     lib.pd_rope_append_tokens.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
     lib.pd_rope_append_tokens_q4.argtypes = [vp, pr, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, i32, i32, u32, vp]
+    lib.pd_rope_append_tokens_latent.argtypes = [vp, pr, vp, i64, vp, i64, i64, vp, i64, vp, f32, vp, vp, i64, i64, vp, vp, vp, i32,
+                                                 i32, u32, vp]
+    lib.pd_decode_attn_latent.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp]
     u64 = ctypes.c_uint64
     lib.pd_rope_turns.argtypes = [f32, ctypes.POINTER(u64)]
     lib.pd_pool_create.argtypes = [i32, u64, u64, ctypes.POINTER(vp)]
@@ -413,6 +418,40 @@ def pd_rope_append_tokens_q4(ctx, rope, positions, q, k_new, v_new, q_indptr, q_
                                          _ptr(k_new), _ptr(v_new), _ptr(q_indptr), _ptr(q_out), _ptr(kv4), _ptr(page_table),
                                          _ptr(ctx_lens), batch, max_q_len, call_flags, _stream(stream)),
            "pd_rope_append_tokens_q4", ctx)
+
+
+def _row_strides(t, name: str):
+    """(token stride, head stride) of rows [tokens, heads, 64] that may lie inside wider ones."""
+    if t is None:
+        return 0, 0
+    if t.dim() != 3 or t.shape[-1] != 64 or t.stride(-1) != 1:
+        raise ValueError(f"{name}: [tokens, heads, 64] with neighbouring values is needed")
+    head = t.stride(1) if t.shape[1] > 1 else 64                      # the stride of an axis of one means nothing
+    return (t.stride(0) if t.shape[0] > 1 else t.shape[1] * head), head
+
+
+def pd_rope_append_tokens_latent(ctx, rope, positions, q_rope, kv_new, norm_weight, norm_eps, q_indptr, q_out, kv_pages, page_table,
+                                 ctx_lens, max_q_len, batch=None, call_flags=0, stream=None):
+    """``q_rope`` and ``q_out``: [tokens, heads, 64], possibly inside wider rows (``q[..., -64:]``), or None; ``kv_new``:
+    [tokens, 576], possibly inside wider rows; ``norm_weight`` [512] and ``positions`` may be None."""
+    batch = q_indptr.shape[0] - 1 if batch is None else batch
+    needed = batch > 0 and max_q_len > 0
+    if kv_new.dim() != 2 or kv_new.shape[-1] != 576 or kv_new.stride(-1) != 1:
+        raise ValueError("kv_new: [tokens, 576] with neighbouring values is needed")
+    kv_stride = kv_new.stride(0) if kv_new.shape[0] > 1 else 576
+    _check(_lib.pd_rope_append_tokens_latent(
+        ctx, ctypes.byref(rope), _optional_ptr(positions, needed, "positions"), _position_stride(positions, rope),
+        _optional_ptr(q_rope, needed, "q_rope"), *_row_strides(q_rope, "q_rope"), _ptr(kv_new), kv_stride,
+        _optional_ptr(norm_weight, needed, "norm_weight"), norm_eps, _ptr(q_indptr), _optional_ptr(q_out, needed, "q_out"),
+        *_row_strides(q_out, "q_out"), _ptr(kv_pages), _ptr(page_table), _ptr(ctx_lens), batch, max_q_len, call_flags,
+        _stream(stream)), "pd_rope_append_tokens_latent", ctx)
+
+
+def pd_decode_attn_latent(ctx, q, kv_pages, page_table, ctx_lens, out, lse=None, batch=None, sm_scale=1.0, split_pages=0, stream=None):
+    batch = q.shape[0] if batch is None else batch
+    _check(_lib.pd_decode_attn_latent(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(out),
+                                      _optional_ptr(lse, batch > 0, "lse"), batch, sm_scale, split_pages, _stream(stream)),
+           "pd_decode_attn_latent", ctx)
 
 
 def pd_pool_create(device: int, capacity_bytes: int, chunk_bytes: int = 0):

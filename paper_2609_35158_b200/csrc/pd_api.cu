@@ -77,6 +77,13 @@ struct pd_ctx {
     int64_t host_steps_direct = 0, host_steps_staged = 0;
     __nv_bfloat16 *host_out_alias = nullptr;  // set for the duration of one pd_decode_step_host call
     cudaEvent_t ev_before = nullptr, ev_after = nullptr;  // optional timing hook around the split kernel
+    // a context for shared latent vectors (PD_FLAG_LATENT): its pool's and its queries' tensor maps
+    bool latent = false;
+    bool latent_decode_ready = false;
+    const void *map_latent_ptr = nullptr, *map_latent_q_ptr = nullptr;
+    alignas(64) CUtensorMap tm_latent{};
+    alignas(64) CUtensorMap tm_latent_q{};
+    float4 *part_ml4 = nullptr;
     bool prefill_ready = false;
     bool fp8_ready = false;
     bool q4_ready = false;
@@ -145,8 +152,44 @@ int encode_pool_map_fp8(pd_ctx *ctx, const void *pool, CUtensorMap *out) {
     return PD_OK;
 }
 
-int check_batch(pd_ctx *ctx, int32_t batch) {
+// Heads of one group of the latent decode kernel: as even as they come, at most 64.
+int latent_groups(int heads) { return (heads + 63) / 64; }
+int latent_group_heads(int heads) { return (heads + latent_groups(heads) - 1) / latent_groups(heads); }
+
+// A pool of shared latent vectors: rows = (page, slot), 576 columns; box = 16 rows x 64 columns with the 128-byte swizzle.
+int encode_latent_map(pd_ctx *ctx, const void *pool, CUtensorMap *out) {
+    const cuuint64_t dims[2] = {pd::kLatentRow, static_cast<cuuint64_t>(ctx->cfg.num_pages) * pd::kPageSize};
+    const cuuint64_t strides[1] = {pd::kLatentRow * 2};
+    const cuuint32_t box[2] = {64, pd::kPageSize}, elem_strides[2] = {1, 1};
+    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pool), dims, strides, box,
+                                   elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return PD_OK;
+    std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+    return PD_ERR_CUDA;
+}
+
+// Absorbed queries [batch][heads][576]: box = 64 columns of the heads one block takes; heads past the last are zero fill.
+int encode_latent_q_map(pd_ctx *ctx, const void *q, CUtensorMap *out) {
+    const cuuint64_t heads = static_cast<cuuint64_t>(ctx->cfg.num_q_heads);
+    const cuuint64_t dims[3] = {pd::kLatentRow, heads, static_cast<cuuint64_t>(ctx->cfg.max_batch)};
+    const cuuint64_t strides[2] = {pd::kLatentRow * 2, heads * pd::kLatentRow * 2};
+    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(pd::latent_heads_per_cta(latent_group_heads(ctx->cfg.num_q_heads))), 1};
+    const cuuint32_t elem_strides[3] = {1, 1, 1};
+    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box,
+                                   elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return PD_OK;
+    std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+    return PD_ERR_CUDA;
+}
+
+// `latent`: the kind of context the call is for.
+int check_batch(pd_ctx *ctx, int32_t batch, bool latent = false) {
     if (ctx == nullptr) return PD_ERR_INVALID_ARG;
+    if (ctx->latent != latent)
+        return fail(ctx, PD_ERR_UNSUPPORTED, latent ? "the call needs a context created with PD_FLAG_LATENT"
+                                                    : "the call does not take a context created with PD_FLAG_LATENT");
     if (batch < 0 || batch > ctx->cfg.max_batch) return fail(ctx, PD_ERR_INVALID_ARG, "batch outside [0, max_batch]");
     return PD_OK;
 }
@@ -181,8 +224,12 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
         cfg->device < 0)
         return PD_ERR_INVALID_ARG;
     const int group = cfg->num_q_heads / cfg->num_kv_heads;
-    if (cfg->page_size != pd::kPageSize || (cfg->head_dim != 64 && cfg->head_dim != 128) ||
-        (group != 1 && group != 2 && group != 4 && group != 8))
+    const bool latent = (cfg->flags & PD_FLAG_LATENT) != 0;
+    if (latent && (cfg->page_size != pd::kPageSize || cfg->head_dim != pd::kLatentDim || cfg->num_kv_heads != 1 ||
+                   cfg->num_q_heads > pd::kLatentMaxHeads))
+        return PD_ERR_UNSUPPORTED;
+    if (!latent && (cfg->page_size != pd::kPageSize || (cfg->head_dim != 64 && cfg->head_dim != 128) ||
+                    (group != 1 && group != 2 && group != 4 && group != 8)))
         return PD_ERR_UNSUPPORTED;
     // TMA row coordinates and page ids are 32-bit
     if (cfg->num_pages * cfg->num_kv_heads * cfg->page_size >= (int64_t(1) << 31)) return PD_ERR_UNSUPPORTED;
@@ -219,7 +266,8 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
         delete ctx;
         return PD_ERR_INVALID_ARG;
     }
-    cudaError_t err = pd::prepare_decode_attn(v, &ctx->smem_bytes);
+    ctx->latent = latent;
+    cudaError_t err = latent ? cudaSuccess : pd::prepare_decode_attn(v, &ctx->smem_bytes);
     if (err != cudaSuccess) {
         delete ctx;
         return err == cudaErrorInvalidValue ? PD_ERR_UNSUPPORTED : PD_ERR_CUDA;
@@ -238,14 +286,19 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
     const int n_workers = ctx->num_ctas * v.warps;
     ctx->max_ranges = 16 * n_workers;
     ctx->slots = static_cast<size_t>(ctx->max_ranges) + static_cast<size_t>(cfg->max_batch) * cfg->num_kv_heads;
+    if (latent) {  // a worker is a whole CTA; a range leaves at most two cut segments, of all heads
+        ctx->max_ranges = 2 * ctx->num_sms;
+        ctx->slots = 2 * static_cast<size_t>(ctx->max_ranges);
+    }
     auto round256 = [](size_t n) { return (n + 255) & ~size_t(255); };
     const size_t b_part_o = round256(ctx->slots * group * cfg->head_dim * sizeof(float));
-    const size_t b_part_ml = round256(ctx->slots * group * sizeof(float2));
+    const size_t b_part_ml = round256(ctx->slots * group * (latent ? sizeof(float4) : sizeof(float2)));
     const size_t b_cum = round256((static_cast<size_t>(cfg->max_batch) + 1) * sizeof(int32_t));
     const size_t b_plan = round256(pd::kPlanWords * sizeof(int32_t));
     const size_t b_status = round256(pd::kStatusWords * sizeof(int32_t));
-    const size_t b_q = round256(static_cast<size_t>(cfg->max_batch) * cfg->num_q_heads * cfg->head_dim * 2);
-    const size_t b_kv = round256(static_cast<size_t>(cfg->max_batch) * cfg->num_kv_heads * cfg->head_dim * 2);
+    // staging of pd_decode_step_host, which a latent context does not have
+    const size_t b_q = latent ? 0 : round256(static_cast<size_t>(cfg->max_batch) * cfg->num_q_heads * cfg->head_dim * 2);
+    const size_t b_kv = latent ? 0 : round256(static_cast<size_t>(cfg->max_batch) * cfg->num_kv_heads * cfg->head_dim * 2);
     const size_t b_trace = tune_int("PD_TRACE_WORKERS", 0) ? round256(static_cast<size_t>(n_workers) * 4 * 8) : 0;
     ctx->workspace_bytes = b_part_o + b_part_ml + b_cum + b_plan + b_status + 2 * b_q + 2 * b_kv + b_trace;
     err = cudaMalloc(&ctx->workspace, ctx->workspace_bytes);
@@ -255,7 +308,8 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
     }
     char *w = static_cast<char *>(ctx->workspace);
     ctx->part_o = reinterpret_cast<float *>(w); w += b_part_o;
-    ctx->part_ml = reinterpret_cast<float2 *>(w); w += b_part_ml;
+    ctx->part_ml = reinterpret_cast<float2 *>(w);
+    ctx->part_ml4 = reinterpret_cast<float4 *>(w); w += b_part_ml;
     ctx->cum_pages = reinterpret_cast<int32_t *>(w); w += b_cum;
     ctx->plan = reinterpret_cast<int32_t *>(w); w += b_plan;
     ctx->status = reinterpret_cast<int32_t *>(w); w += b_status;
@@ -505,7 +559,7 @@ int pd_decode_step(pd_ctx *ctx, const void *q, const void *k_new, const void *v_
 
 int pd_kv_quantize_pages(pd_ctx *ctx, const void *k_pages, const void *v_pages, const int32_t *tokens_in_page, void *k8,
                          void *v8, float *kv_scales, void *stream) {
-    if (ctx == nullptr) return PD_ERR_INVALID_ARG;
+    if (int rc = check_batch(ctx, 0)) return rc;
     if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(k8) || !aligned16(v8) || !aligned16(kv_scales) ||
         tokens_in_page == nullptr)
         return fail(ctx, PD_ERR_INVALID_ARG, "pd_kv_quantize_pages: null or misaligned pointer");
@@ -939,7 +993,7 @@ int pd_rope_turns(float inv_freq, uint64_t *turns) {
 
 int pd_rope_tokens(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride, const void *q,
                    const void *k, void *q_out, void *k_out, int32_t total, void *stream) {
-    if (ctx == nullptr) return PD_ERR_INVALID_ARG;
+    if (int rc = check_batch(ctx, 0)) return rc;
     if (!aligned16(q) || !aligned16(k) || !aligned16(q_out) || !aligned16(k_out) || positions == nullptr)
         return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_tokens: null or misaligned pointer");
     if (total < 0 || position_stride < total) return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_tokens: negative total, or position_stride below it");
@@ -1263,6 +1317,133 @@ int pd_last_plan(pd_ctx *ctx, void *stream, int64_t *total_units, int32_t *pages
     if (pages_per_range != nullptr) *pages_per_range = host[pd::kPlanHeaderWords + 2];  // first (largest) level
     if (num_ranges != nullptr) *num_ranges = host[3];
     if (num_workers != nullptr) *num_workers = host[4];
+    return PD_OK;
+}
+
+}  // extern "C"
+
+namespace {
+
+bool stride8(int64_t n, int64_t least) { return n >= least && n % 8 == 0; }
+
+}  // namespace
+
+extern "C" {
+
+int pd_rope_append_tokens_latent(pd_ctx *ctx, const pd_rope_config *rope, const int32_t *positions, int64_t position_stride,
+                                 const void *q_rope, int64_t q_token_stride, int64_t q_head_stride, const void *kv_new,
+                                 int64_t kv_stride, const void *norm_weight, float norm_eps, const int32_t *q_indptr, void *q_out,
+                                 int64_t q_out_token_stride, int64_t q_out_head_stride, void *kv_pages, const int32_t *page_table,
+                                 int32_t *ctx_lens, int32_t batch, int32_t max_q_len, uint32_t call_flags, void *stream) {
+    if (int rc = check_batch(ctx, batch, true)) return rc;
+    if (!aligned16(kv_new) || !aligned16(kv_pages) || q_indptr == nullptr || page_table == nullptr || ctx_lens == nullptr ||
+        (q_rope != nullptr) != (q_out != nullptr) || (q_rope != nullptr && (!aligned16(q_rope) || !aligned16(q_out))) ||
+        (norm_weight != nullptr && !aligned16(norm_weight)))
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_append_tokens_latent: null or misaligned pointer");
+    if (!stride8(kv_stride, pd::kLatentRow) ||
+        (q_rope != nullptr && (!stride8(q_token_stride, 0) || !stride8(q_head_stride, 0) ||
+                               !stride8(q_out_token_stride, pd::kLatentRope) || !stride8(q_out_head_stride, pd::kLatentRope))))
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_append_tokens_latent: strides must be multiples of 8 values and rows must not overlap");
+    if (!(norm_eps >= 0.f) || !(norm_eps < 3.0e38f)) return fail(ctx, PD_ERR_INVALID_ARG, "norm_eps must be finite and >= 0");
+    if (call_flags & ~PD_APPEND_NO_ADVANCE) return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_append_tokens_latent: unknown call flag");
+    if (max_q_len < 0 || position_stride < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len and position_stride must be >= 0");
+    if (positions != nullptr && position_stride == 0 && batch > 0 && max_q_len > 0)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_rope_append_tokens_latent: no positions (position_stride 0)");
+    if (rope != nullptr && rope->rot_dim > pd::kLatentRope)
+        return fail(ctx, PD_ERR_INVALID_ARG, "rope: rot_dim, num_axes, adjacent or magnitude out of range");
+    pd::RopeParams r{};
+    if (int rc = rope_params(ctx, rope, &r)) return rc;
+    if (batch == 0 || max_q_len == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    pd::LatentAppendParams p{};
+    for (int i = 0; i < pd::kLatentRope / 2; ++i) {
+        p.freq[i] = r.freq[i];
+        p.axis_of_pair[i] = r.axis_of_pair[i];
+    }
+    p.magnitude = r.magnitude;
+    p.rot_dim = r.rot_dim;
+    p.adjacent = r.adjacent;
+    p.positions = positions;
+    p.position_stride = position_stride;
+    p.q = static_cast<const __nv_bfloat16 *>(q_rope);
+    p.kv_new = static_cast<const __nv_bfloat16 *>(kv_new);
+    p.norm_weight = static_cast<const __nv_bfloat16 *>(norm_weight);
+    p.q_out = static_cast<__nv_bfloat16 *>(q_out);
+    p.q_token_stride = q_token_stride;
+    p.q_head_stride = q_head_stride;
+    p.q_out_token_stride = q_out_token_stride;
+    p.q_out_head_stride = q_out_head_stride;
+    p.kv_stride = kv_stride;
+    p.norm_eps = norm_eps;
+    p.q_indptr = q_indptr;
+    p.kv_pages = static_cast<__nv_bfloat16 *>(kv_pages);
+    p.page_table = page_table;
+    p.ctx_lens = ctx_lens;
+    p.status = ctx->status;
+    p.B = batch;
+    p.Hq = ctx->cfg.num_q_heads;
+    p.MP = ctx->cfg.max_pages_per_seq;
+    p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.advance = (call_flags & PD_APPEND_NO_ADVANCE) ? 0 : 1;
+    p.pdl = ctx->pdl;
+    int launched = 0;
+    const cudaError_t err = pd::launch_rope_append_latent(p, max_q_len, ctx->num_sms, &launched, static_cast<cudaStream_t>(stream));
+    ctx->launches += launched;
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent append launch", err);
+    return PD_OK;
+}
+
+int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_table, const int32_t *ctx_lens,
+                          void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream) {
+    if (int rc = check_batch(ctx, batch, true)) return rc;
+    if (!aligned16(q) || !aligned16(kv_pages) || !aligned16(out) || page_table == nullptr || ctx_lens == nullptr)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_decode_attn_latent: null or misaligned pointer");
+    if (!(sm_scale > 0.f) || !(sm_scale < 3.0e38f)) return fail(ctx, PD_ERR_INVALID_ARG, "sm_scale must be finite and positive");
+    if (split_pages < 0) return fail(ctx, PD_ERR_INVALID_ARG, "split_pages must be >= 0");
+    if (batch == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    if (!ctx->latent_decode_ready) {
+        const cudaError_t e = pd::prepare_decode_attn_latent();
+        if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent decode kernel attribute", e);
+        ctx->latent_decode_ready = true;
+    }
+    if (ctx->map_latent_ptr != kv_pages) {
+        if (int rc = encode_latent_map(ctx, kv_pages, &ctx->tm_latent)) return rc;
+        ctx->map_latent_ptr = kv_pages;
+    }
+    if (ctx->map_latent_q_ptr != q) {
+        if (int rc = encode_latent_q_map(ctx, q, &ctx->tm_latent_q)) return rc;
+        ctx->map_latent_q_ptr = q;
+    }
+    pd::LatentAttnParams p{};
+    p.a.q = static_cast<const __nv_bfloat16 *>(q);
+    p.a.page_table = page_table;
+    p.a.ctx_lens = ctx_lens;
+    p.a.out = static_cast<__nv_bfloat16 *>(out);
+    p.a.lse = lse;
+    p.a.part_o = ctx->part_o;
+    p.part_ml = ctx->part_ml4;
+    p.a.cum_pages = ctx->cum_pages;
+    p.a.plan = ctx->plan;
+    p.a.status = ctx->status;
+    p.a.B = batch;
+    p.a.Hq = ctx->cfg.num_q_heads;
+    p.a.Hkv = 1;
+    p.a.MP = ctx->cfg.max_pages_per_seq;
+    p.a.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.a.scale_log2 = sm_scale * 1.4426950408889634f;
+    p.a.split_pages = split_pages;
+    p.a.max_ranges = ctx->max_ranges;
+    p.a.min_pages_auto = ctx->min_pages_auto;
+    p.groups = latent_groups(ctx->cfg.num_q_heads);
+    p.heads = latent_group_heads(ctx->cfg.num_q_heads);
+    p.a.pdl = ctx->pdl;
+    const cudaError_t err = pd::launch_decode_attn_latent(ctx->tm_latent, ctx->tm_latent_q, p, ctx->num_sms / p.groups * p.groups,
+                                                          static_cast<cudaStream_t>(stream));
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent decode launch", err);
+    ctx->launches += 2;
     return PD_OK;
 }
 

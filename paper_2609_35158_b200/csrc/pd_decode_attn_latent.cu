@@ -1,0 +1,728 @@
+// Decode attention over a cache of shared latent vectors (the absorbed form), on the fifth-generation tensor cores.
+//
+// A token's cached row is 576 values, a latent c (512) and a rotated key part r (64), and every head reads the same row:
+// s_t = scale q . (c_t, r_t), out = sum_t softmax(s)_t c_t. A token costs 1152 bytes and 2 * 1088 operations per head, so
+// up to about 100 heads the bound is memory. The form of decode_attn_split_kernel (warp MMAs, one ring per warp) would have to
+// read every row once per 8 heads; here a CTA takes up to 64 heads over one row in shared memory.
+//
+// One CTA per SM walks its range of pages in tiles of 64 tokens (4 pages). TOKENS are the M dimension of the logits
+// and LATENTS that of the output, so the heads (N) need no padding to 128 and the row, as TMA stores it, is both operands:
+//   S^T [64 tokens][N heads]   = rows (K-major) x Q^T             36 MMAs 64 x N x 16
+//   O^T [4][128 latents][N]   += latents^T (M-major) x P^T        16 MMAs 128 x N x 16
+// The operands' bytes bound the tensor pipe, (A + B) / 128 per clock: measured 32 cycles for a 64 x 64 x 16 product, 48 for
+// 128 x 64 x 16 (23 and 39 at N = 16); 1936 cycles a tile at N = 64, beside 3200 for its 73,728 bytes at the measured copy
+// bandwidth. These rates need the issuing thread to be chosen by elect.sync: under `lane == 0` one MMA takes 46 cycles to issue.
+// The ring holds pairs of 64-column blocks (128 latents of a tile, 16 KB) and, apart, the rotated parts (8 KB): a tile's
+// pairs are handed back one by one as the output products pass over them, so nearly two tiles are in flight beside 72 KB of Q.
+//
+// Softmax: one thread holds half the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
+// tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
+// than 8 log2 units, so a tile needs one vote and no reduction over tokens. P is rounded to bf16 (2^-9 of itself: a second
+// product for its remainder would make 128 heads a third slower); the sum that normalises the output adds the rounded
+// values, lse takes the unrounded sum.
+//
+// More than 64 heads go in groups: neighbouring CTAs read the same pages for different heads, the second one from L2.
+// A segment (the part of a range inside one sequence) that covers its sequence writes the result, any other an fp32 partial;
+// latent_merge_kernel joins them. Every wait is bounded.
+#include "pd_decode_plan.cuh"
+#include "pd_kernels.cuh"
+#include "pd_ptx.cuh"
+#include "pd_tcgen05.cuh"
+
+namespace pd {
+
+namespace {
+
+constexpr int kTile = 64;                        // tokens per step
+constexpr int kTilePages = kTile / kPageSize;
+constexpr int kChunkBytes = kTile * 128;         // 64 columns of a tile's rows
+constexpr int kPairBytes = 2 * kChunkBytes;
+constexpr int kPairs = 4;                        // pairs of a tile: 512 latents
+constexpr int kRopeSlots = 2;
+constexpr int kRowChunks = kLatentRow / 64;      // 9
+constexpr int kSoftmaxThreads = 128;
+constexpr int kThreads = kSoftmaxThreads + 64;   // + TMA warp + MMA warp
+constexpr int kPBytes = kTile * 128;
+constexpr int kSmemLimit = 232448;
+constexpr int kControlBytes = 512;
+constexpr int kTmemCols = 512;
+
+// Pairs the ring holds beside Q, P and the rotated parts: 8 (two tiles) with 64 heads, more with fewer.
+template <int N>
+__host__ __device__ constexpr int pair_slots() {
+    return (kSmemLimit - 1024 - kControlBytes - kRowChunks * N * 128 - kPBytes - kRopeSlots * kChunkBytes) / kPairBytes;
+}
+template <int N>
+__host__ __device__ constexpr size_t smem_bytes() {
+    return 1024 + kRowChunks * N * 128 + kPBytes + kRopeSlots * kChunkBytes + pair_slots<N>() * kPairBytes + kControlBytes;
+}
+
+__device__ __forceinline__ bool elect_one() {
+    uint32_t e;
+    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(e));
+    return e != 0;
+}
+
+__device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory"); }
+__device__ __forceinline__ bool softmax_any(bool v) {
+    uint32_t r;
+    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %1, 0;\nbarrier.cta.red.or.pred q, 1, %2, p;\nselp.u32 %0, 1, 0, q;\n}"
+                 : "=r"(r) : "r"(static_cast<uint32_t>(v)), "n"(kSoftmaxThreads) : "memory");
+    return r != 0;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int32_t x, int32_t y, int32_t z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+}
+
+// Half a row's columns per thread: threads 0..15 of the warp get lanes 0..15 from column 0 on, threads 16..31 the same
+// lanes from column K on.
+template <int K>
+__device__ __forceinline__ void tmem_ld_halves(uint32_t taddr, uint32_t (&r)[K]);
+template <>
+__device__ __forceinline__ void tmem_ld_halves<8>(uint32_t taddr, uint32_t (&r)[8]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], 8;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void tmem_ld_halves<16>(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16], 16;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+                   "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+template <>
+__device__ __forceinline__ void tmem_ld_halves<32>(uint32_t taddr, uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x32bx2.x32.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
+        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32], 32;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+        "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
+          "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+// How the flattened list of (sequence, page) units is cut: ranges of `size` pages, `per_worker` consecutive ranges per worker.
+struct LatentPlan {
+    int total, size, ranges, per_worker;
+};
+__device__ __forceinline__ LatentPlan latent_plan(int total, int workers, const LatentAttnParams &p) {
+    LatentPlan pl;
+    pl.total = total;
+    int size = p.a.split_pages > 0 ? p.a.split_pages : max((total + workers - 1) / workers, p.a.min_pages_auto);
+    size = max(size, (total + p.a.max_ranges - 1) / p.a.max_ranges);
+    pl.size = max(size, 1);
+    pl.ranges = (total + pl.size - 1) / pl.size;
+    pl.per_worker = (pl.ranges + workers - 1) / workers;
+    return pl;
+}
+
+// The segments of one worker, in order; every role of the CTA walks them by itself.
+struct Segment {
+    int b, page0, pages, tokens, slot;
+    bool whole;
+};
+struct Walk {
+    int b, page, np, len, r, r_end, left;
+    bool at_start;
+};
+__device__ __forceinline__ bool next_segment(Walk &w, Segment &s, const LatentPlan &pl, const LatentAttnParams &p) {
+    if (w.left == 0) {
+        if (++w.r >= w.r_end) return false;
+        w.left = min(pl.size, pl.total - w.r * pl.size);
+        w.at_start = true;
+    }
+    while (w.page >= w.np) {  // units are left, so a sequence with pages follows
+        ++w.b;
+        w.page = 0;
+        w.len = clamp_len(__ldg(p.a.ctx_lens + w.b), p.a.MP);
+        w.np = (w.len + kPageSize - 1) / kPageSize;
+    }
+    s.b = w.b;
+    s.page0 = w.page;
+    s.pages = min(w.np - w.page, w.left);
+    s.tokens = min(w.len - w.page * kPageSize, s.pages * kPageSize);
+    s.whole = s.pages == w.np;
+    s.slot = 2 * w.r + (w.at_start ? 0 : 1);  // a cut segment begins its range or ends it
+    w.page += s.pages;
+    w.left -= s.pages;
+    w.at_start = false;
+    return true;
+}
+
+// Reduces K values per thread over the 16 lanes of a half warp: afterwards lane l (of 16) holds, in v[0..K/16), those of
+// index (l & 15) * (K / 16) + i for K >= 16; for K = 8 lanes l and l ^ 8 both hold index l & 7.
+template <int K, bool MAX>
+__device__ __forceinline__ void reduce_half_warp(float (&v)[K], int lane) {
+    int n = K;
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) {
+        if (n > 1 && !(K == 8 && o == 8)) {
+            const int half = n / 2;
+            const bool upper = (lane & o) != 0;
+#pragma unroll
+            for (int i = 0; i < K / 2; ++i)
+                if (i < half) {
+                    const float send = upper ? v[i] : v[i + half], keep = upper ? v[i + half] : v[i];
+                    const float got = __shfl_xor_sync(0xffffffffu, send, o);
+                    v[i] = MAX ? fmaxf(keep, got) : keep + got;
+                }
+            n = half;
+        } else {
+#pragma unroll
+            for (int i = 0; i < K; ++i) {
+                const float got = __shfl_xor_sync(0xffffffffu, v[i], o);
+                v[i] = MAX ? fmaxf(v[i], got) : v[i] + got;
+            }
+        }
+    }
+}
+// Index of v[0] after reduce_half_warp (lanes with a duplicate excluded by `owner`).
+template <int K>
+__device__ __forceinline__ int reduced_index(int lane) { return K >= 16 ? (lane & 15) * (K / 16) : (lane & 7); }
+
+template <int N>
+__global__ void __launch_bounds__(kThreads, 1)
+decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_q, const LatentAttnParams p) {
+    constexpr int kSlots = pair_slots<N>();
+    constexpr int K = N / 2;                           // heads per softmax thread
+    constexpr int kColS = 4 * N;                       // O^T in columns [0, 4 N), then two buffers of S^T
+    constexpr int kQBytes = kRowChunks * N * 128;
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int32_t warp_sums[kThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int group = blockIdx.x % p.groups, worker = blockIdx.x / p.groups, workers = gridDim.x / p.groups;
+    const int h0 = group * p.heads, nh = min(p.heads, p.a.Hq - h0);
+
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *aligned = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t ring = base, rope_ring = ring + kSlots * kPairBytes, q_s = rope_ring + kRopeSlots * kChunkBytes, p_s = q_s + kQBytes;
+    float *scratch = reinterpret_cast<float *>(aligned + (p_s - base));  // P's buffer, free whenever it is used
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + (p_s - base) + kPBytes);
+    const uint32_t bar_full = smem_u32(bars), bar_empty = bar_full + kSlots * 8;               // pairs
+    const uint32_t bar_rfull = bar_empty + kSlots * 8, bar_rempty = bar_rfull + kRopeSlots * 8;  // rotated parts
+    const uint32_t bar_qfull = bar_rempty + kRopeSlots * 8, bar_qempty = bar_qfull + 8;        // Q of a segment's sequence
+    const uint32_t bar_s = bar_qempty + 8, bar_sempty = bar_s + 16;                            // [2] S^T buffers
+    const uint32_t bar_p = bar_sempty + 16;                                                    // P written
+    const uint32_t bar_pv = bar_p + 8;                                                         // output products of a tile done
+    const uint32_t bar_o = bar_pv + 8;                                                         // O^T of a segment read out
+    const uint32_t bar_drain = bar_o + 8;
+    static_assert((2 * kSlots + 2 * kRopeSlots + 2 + 4 + 4) * 8 <= kControlBytes, "barriers");
+
+    if (tid == 0) {
+        for (int i = 0; i < 2 * kSlots + 2 * kRopeSlots + 4; ++i) mbar_init(bar_full + i * 8, 1);  // .. bar_s[2]
+        mbar_init(bar_sempty, 4);
+        mbar_init(bar_sempty + 8, 4);
+        mbar_init(bar_p, 4);
+        mbar_init(bar_pv, 1);
+        mbar_init(bar_o, 4);
+        mbar_init(bar_drain, 1);
+        mbar_init_fence();
+        prefetch_tensormap(&tm_kv);
+        prefetch_tensormap(&tm_q);
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
+        tmem_relinquish_alloc_permit();
+    }
+    grid_dependency_wait();
+    launch_dependents();
+
+    // ---- the plan: page sums in the ring's memory, which no copy uses yet
+    int32_t *cum = reinterpret_cast<int32_t *>(aligned);
+    scan_pages<kThreads>(p.a, cum, warp_sums);
+    const LatentPlan pl = latent_plan(cum[p.a.B], workers, p);
+    Walk w0{};
+    w0.r = worker * pl.per_worker;
+    w0.r_end = min(w0.r + pl.per_worker, pl.ranges);
+    const bool busy = w0.r < w0.r_end;
+    if (busy) {
+        const Cursor c = locate(cum, p.a.B, 1, static_cast<long long>(w0.r) * pl.size);
+        w0.b = c.b;
+        w0.page = c.page;
+        w0.np = c.np;
+        w0.len = clamp_len(__ldg(p.a.ctx_lens + c.b), p.a.MP);
+        w0.left = min(pl.size, pl.total - w0.r * pl.size);
+        w0.at_start = true;
+    }
+    if (blockIdx.x == 0) {
+        for (int i = tid; i <= p.a.B; i += kThreads) p.a.cum_pages[i] = cum[i];
+        if (tid == 0) {
+            p.a.plan[0] = pl.total;
+            p.a.plan[1] = 0;
+            p.a.plan[2] = 1;
+            p.a.plan[3] = pl.ranges;
+            p.a.plan[4] = workers;
+            p.a.plan[kPlanHeaderWords + 2] = pl.size;
+        }
+    }
+    fence_proxy_async();  // the copies that follow overwrite what was read here
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tm = tmem_slot;
+    bool ok = true;
+
+    if (busy && warp == 4) {
+        // ================= TMA warp: one box of 64 columns x 16 rows per lane =================
+        const uint64_t policy = l2_policy_evict_first();
+        const int32_t oob_row = p.a.num_pages * kPageSize;  // a box that starts here is all zero fill
+        Walk w = w0;
+        Segment s;
+        int pc = 0, rc = 0, seg = 0;
+        while (ok && next_segment(w, s, pl, p)) {
+            const int32_t *row = p.a.page_table + static_cast<size_t>(s.b) * p.a.MP + s.page0;
+            auto ids = [&](int g) { return g * 32 + lane < s.pages ? __ldg(row + g * 32 + lane) : -1; };
+            int val = ids(0), nval = ids(1);
+            for (int i = 0; i * kTilePages < s.pages && ok; ++i) {
+                const int pg0 = i * kTilePages;
+                if (i > 0 && (pg0 & 31) == 0) {
+                    val = nval;
+                    nval = ids((pg0 >> 5) + 1);
+                }
+                const int pg = (lane >> 1) & (kTilePages - 1);
+                int pid = __shfl_sync(0xffffffffu, val, (pg0 + pg) & 31);
+                int32_t y = oob_row;
+                if (pg0 + pg < s.pages) {
+                    if (pid < 0 || pid >= p.a.num_pages) {
+                        if (lane < 2 * kTilePages && (lane & 1) == 0) latch_status(p.a.status, kDevBadPage, s.b, pid);
+                        pid = 0;
+                    }
+                    y = pid * kPageSize;
+                }
+                {
+                    const int slot = rc % kRopeSlots, fill = rc / kRopeSlots;
+                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_rempty + slot * 8, (fill - 1) & 1));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(bar_rfull + slot * 8, kChunkBytes);
+                    __syncwarp();
+                    if (lane < 2 * kTilePages && (lane & 1) == 0)
+                        tma_load_2d(rope_ring + slot * kChunkBytes + pg * (kPageSize * 128), &tm_kv, kLatentDim, y, bar_rfull + slot * 8, policy);
+                    ++rc;
+                }
+                for (int j = 0; j < kPairs; ++j) {
+                    const int slot = pc % kSlots, fill = pc / kSlots;
+                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + slot * 8, (fill - 1) & 1));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(bar_full + slot * 8, kPairBytes);
+                    __syncwarp();
+                    if (lane < 2 * kTilePages)
+                        tma_load_2d(ring + slot * kPairBytes + (lane & 1) * kChunkBytes + pg * (kPageSize * 128), &tm_kv,
+                                    (2 * j + (lane & 1)) * 64, y, bar_full + slot * 8, policy);
+                    ++pc;
+                }
+                if (i == 0 && ok) {  // Q behind the first tile: it has to wait for the last segment's logits
+                    if (seg > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_qempty, (seg - 1) & 1));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(bar_qfull, kQBytes);
+                    __syncwarp();
+                    if (lane < kRowChunks) tma_load_3d(q_s + lane * (N * 128), &tm_q, lane * 64, h0, s.b, bar_qfull);
+                    ++seg;
+                }
+            }
+        }
+        if (!ok) {  // copies in flight have to land before the block's memory goes
+            if (lane == 0) latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
+            for (int i = max(0, pc - kSlots); i < pc; ++i) mbar_wait(bar_full + (i % kSlots) * 8, (i / kSlots) & 1);
+            for (int i = max(0, rc - kRopeSlots); i < rc; ++i) mbar_wait(bar_rfull + (i % kRopeSlots) * 8, (i / kRopeSlots) & 1);
+            if (seg > 0) mbar_wait(bar_qfull, (seg - 1) & 1);
+        }
+    } else if (busy && warp == 5) {
+        // ================= MMA warp: one elected thread issues every product =================
+        if (elect_one()) {
+            constexpr uint32_t idesc_s = umma_idesc_bf16(64, N, false);
+            constexpr uint32_t idesc_o = umma_idesc_bf16(128, N, true) | (1u << 15);  // A M-major
+            const uint64_t q_desc = umma_smem_desc(q_s, 16, 1024), p_desc = umma_smem_desc(p_s, 16, 1024);
+            const uint64_t ring_k = umma_smem_desc(ring, 16, 1024), ring_m = umma_smem_desc(ring, kChunkBytes, 1024);
+            const uint64_t rope_k = umma_smem_desc(rope_ring, 16, 1024);
+            int pv_tile = 0, pv_seg_first = 0;   // next tile whose output product is due; segments begun by them
+            // one tile's output products
+            auto issue_pv = [&](bool first) {
+                tc_fence_after_sync();
+#pragma unroll
+                for (int j = 0; j < kPairs; ++j) {
+                    const int slot = (pv_tile * kPairs + j) % kSlots;
+                    const uint64_t a = ring_m + slot * (kPairBytes >> 4);
+#pragma unroll
+                    for (int ks = 0; ks < kTile / 16; ++ks)
+                        umma_ss(tm + j * N, a + ks * (2048 >> 4), p_desc + ks * (2048 >> 4), idesc_o, !first || ks != 0);
+                    umma_commit(bar_empty + slot * 8);
+                }
+                umma_commit(bar_pv);
+                ++pv_tile;
+            };
+            Walk w = w0;
+            Segment s;
+            int t = 0, seg = 0;
+            bool due = false, due_first = false;  // the previous tile's output products, and whether it opened its segment
+            auto pv_ready = [&]() { return mbar_try_wait(bar_p, pv_tile & 1); };
+            auto do_pv = [&]() {
+                if (due_first) {
+                    if (pv_seg_first > 0) ok = mbar_wait(bar_o, (pv_seg_first - 1) & 1);  // the last segment's O^T has been read
+                    ++pv_seg_first;
+                }
+                if (ok) issue_pv(due_first);
+                due = false;
+            };
+            // waits for `bar`; the previous tile's output products go in between as soon as its P is there
+            auto wait_for = [&](uint32_t bar, uint32_t parity) {
+                if (mbar_try_wait(bar, parity)) return;
+                const uint64_t t0 = global_timer_ns();
+                for (uint32_t poll = 1; ok; ++poll) {
+                    if (due && pv_ready()) do_pv();
+                    if (mbar_try_wait(bar, parity)) return;
+                    if ((poll & 255u) == 0 && (poll >= (1u << 24) || global_timer_ns() - t0 > 2000000000ull)) ok = false;
+                }
+            };
+            while (ok && next_segment(w, s, pl, p)) {
+                const int tiles = (s.pages + kTilePages - 1) / kTilePages;
+                for (int i = 0; i < tiles && ok; ++i, ++t) {
+                    if (i == 0) wait_for(bar_qfull, seg & 1);
+                    if (t >= 2) wait_for(bar_sempty + (t & 1) * 8, ((t >> 1) - 1) & 1);
+                    wait_for(bar_rfull + (t % kRopeSlots) * 8, (t / kRopeSlots) & 1);
+                    if (!ok) break;
+                    const uint32_t d = tm + kColS + (t & 1) * N;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        umma_ss(d, rope_k + (t % kRopeSlots) * (kChunkBytes >> 4) + ks * 2, q_desc + (8 * N * 128 >> 4) + ks * 2, idesc_s, ks != 0);
+                    umma_commit(bar_rempty + (t % kRopeSlots) * 8);
+#pragma unroll
+                    for (int j = 0; j < kPairs; ++j) {
+                        const int pc = t * kPairs + j, slot = pc % kSlots;
+                        wait_for(bar_full + slot * 8, (pc / kSlots) & 1);
+                        if (!ok) break;
+                        tc_fence_after_sync();
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int ks = 0; ks < 4; ++ks)
+                                umma_ss(d, ring_k + slot * (kPairBytes >> 4) + c * (kChunkBytes >> 4) + ks * 2,
+                                        q_desc + ((2 * j + c) * N * 128 >> 4) + ks * 2, idesc_s, true);
+                    }
+                    if (!ok) break;
+                    umma_commit(bar_s + (t & 1) * 8);
+                    if (i == tiles - 1) umma_commit(bar_qempty);
+                    if (due) {
+                        ok = mbar_wait(bar_p, pv_tile & 1);
+                        if (ok) do_pv();
+                    }
+                    due = true;
+                    due_first = i == 0;
+                }
+                ++seg;
+            }
+            if (ok && due) {
+                ok = mbar_wait(bar_p, pv_tile & 1);
+                if (ok) do_pv();
+            }
+            if (!ok) latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
+            umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
+            mbar_wait(bar_drain, 0);
+        }
+    } else if (busy && warp < 4) {
+        // ================= softmax: thread = (token of the tile, half of the heads) =================
+        const int tok = warp * 16 + (lane & 15), hb = lane >> 4;
+        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+        Walk w = w0;
+        Segment s;
+        int t = 0;
+        while (ok && next_segment(w, s, pl, p)) {
+            float m[K], l[K], lr[K];
+#pragma unroll
+            for (int i = 0; i < K; ++i) m[i] = l[i] = lr[i] = 0.f;
+            const int tiles = (s.pages + kTilePages - 1) / kTilePages;
+            for (int i = 0; i < tiles && ok; ++i, ++t) {
+                ok = mbar_wait(bar_s + (t & 1) * 8, (t >> 1) & 1);
+                if (!ok) break;
+                tc_fence_after_sync();
+                uint32_t sreg[K];
+                tmem_ld_halves<K>(tm + lane_base + kColS + (t & 1) * N, sreg);
+                tmem_wait_ld();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_sempty + (t & 1) * 8);
+                const int valid = s.tokens - i * kTile;
+                if (valid < kTile) {
+                    // slots past the context may hold NaN, and 0 * NaN is NaN: their latents are cleared before the output
+                    // product (pages past the segment came as zero fill); S^T of the tile is complete, so all has landed
+                    const int last = min(kTile, (valid + kPageSize - 1) / kPageSize * kPageSize);
+                    for (int x = tid; x < (last - valid) * (kLatentDim / 8); x += kSoftmaxThreads) {
+                        const int r = valid + x / (kLatentDim / 8), c = x % (kLatentDim / 8);
+                        const int slot = (t * kPairs + (c >> 4)) % kSlots;
+                        st_shared_zero16(ring + slot * kPairBytes + ((c >> 3) & 1) * kChunkBytes + r * 128 + (c & 7) * 16);
+                    }
+                }
+                const bool dead = tok >= valid;
+                float x[K];
+                // the reference of every head of this thread: the largest logit over all tokens of the tile
+                auto tile_max = [&](float (&top)[K]) {
+                    float v[K];
+#pragma unroll
+                    for (int k = 0; k < K; ++k) v[k] = dead ? -INFINITY : __uint_as_float(sreg[k]) * p.a.scale_log2;
+                    reduce_half_warp<K, true>(v, lane);
+                    const int at = reduced_index<K>(lane);
+#pragma unroll
+                    for (int k = 0; k < (K >= 16 ? K / 16 : 1); ++k) scratch[warp * 64 + hb * K + at + k] = v[k];
+                    softmax_sync();
+#pragma unroll
+                    for (int k = 0; k < K; ++k)
+                        top[k] = fmaxf(fmaxf(scratch[hb * K + k], scratch[64 + hb * K + k]), fmaxf(scratch[128 + hb * K + k], scratch[192 + hb * K + k]));
+                    softmax_sync();
+                };
+                if (i == 0) {
+                    tile_max(m);  // (the last segment's products are over, P's buffer is free)
+#pragma unroll
+                    for (int k = 0; k < K; ++k) m[k] = fmaxf(m[k], -1e30f);
+                }
+                float over = -INFINITY;
+#pragma unroll
+                for (int k = 0; k < K; ++k) {
+                    x[k] = dead ? -INFINITY : fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]);
+                    over = fmaxf(over, x[k]);
+                }
+                if (i > 0) {
+                    const bool raise = softmax_any(over > kRescaleSlack);
+                    ok = mbar_wait(bar_pv, (t - 1) & 1);  // P's buffer is free and O^T holds every tile before this one
+                    if (!ok) break;
+                    if (raise) {
+                        tc_fence_after_sync();
+                        float top[K];
+                        tile_max(top);
+#pragma unroll
+                        for (int k = 0; k < K; ++k) {
+                            float alpha = 1.f;
+                            if (top[k] - m[k] > kRescaleSlack) {
+                                alpha = fast_exp2(m[k] - top[k]);
+                                x[k] += m[k] - top[k];
+                                m[k] = top[k];
+                            }
+                            l[k] *= alpha;
+                            lr[k] *= alpha;
+                            if ((lane & 15) == 0 && warp == 0) scratch[hb * K + k] = alpha;
+                        }
+                        softmax_sync();
+#pragma unroll 1
+                        for (int c = 0; c < 4 * N; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(tm + lane_base + c, o);
+                            tmem_wait_ld();
+#pragma unroll
+                            for (int k = 0; k < 16; ++k) o[k] = __float_as_uint(__uint_as_float(o[k]) * scratch[(c + k) % N]);
+                            tmem_st16(tm + lane_base + c, o);
+                        }
+                        tmem_wait_st();
+                        softmax_sync();
+                    }
+                }
+                uint32_t pk[K / 2];
+#pragma unroll
+                for (int k = 0; k < K; k += 2) {
+                    const float e0 = fast_exp2(x[k]), e1 = fast_exp2(x[k + 1]);
+                    pk[k / 2] = pack_bf16x2(e0, e1);
+                    l[k] += e0;
+                    l[k + 1] += e1;
+                    lr[k] += __uint_as_float(pk[k / 2] << 16);
+                    lr[k + 1] += __uint_as_float(pk[k / 2] & 0xffff0000u);
+                }
+#pragma unroll
+                for (int c = 0; c < K / 8; ++c) {
+                    const uint32_t a = p_s + sw128_offset(tok, hb * (K / 8) + c);
+                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(pk[4 * c]), "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]),
+                                 "r"(pk[4 * c + 3]) : "memory");
+                }
+                fence_proxy_async();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_p);
+            }
+            if (!ok) break;
+            // ---- the segment's end
+            ok = mbar_wait(bar_pv, (t - 1) & 1);
+            if (!ok) break;
+            tc_fence_after_sync();
+            float *sum_l = scratch, *sum_lr = scratch + 256, *ref = scratch + 512, *inv = scratch + 576;
+            if (warp == 0 && (lane & 15) == 0) {
+#pragma unroll
+                for (int k = 0; k < K; ++k) ref[hb * K + k] = m[k];
+            }
+            reduce_half_warp<K, false>(l, lane);
+            reduce_half_warp<K, false>(lr, lane);
+            const int at = reduced_index<K>(lane);
+#pragma unroll
+            for (int k = 0; k < (K >= 16 ? K / 16 : 1); ++k) {
+                sum_l[warp * 64 + hb * K + at + k] = l[k];
+                sum_lr[warp * 64 + hb * K + at + k] = lr[k];
+            }
+            softmax_sync();
+            if (tid < nh) {
+                const float sl = (sum_l[tid] + sum_l[64 + tid]) + (sum_l[128 + tid] + sum_l[192 + tid]);
+                const float slr = (sum_lr[tid] + sum_lr[64 + tid]) + (sum_lr[128 + tid] + sum_lr[192 + tid]);
+                if (s.whole) {
+                    inv[tid] = 1.f / slr;
+                    if (p.a.lse != nullptr) p.a.lse[static_cast<size_t>(s.b) * p.a.Hq + h0 + tid] = (ref[tid] + log2f(sl)) * kLn2;
+                } else {
+                    p.part_ml[static_cast<size_t>(s.slot) * p.a.Hq + h0 + tid] = make_float4(ref[tid], sl, slr, 0.f);
+                }
+            }
+            softmax_sync();
+#pragma unroll 1
+            for (int j = 0; j < 4; ++j) {
+                const int latent = j * 128 + tid;
+#pragma unroll 1
+                for (int c = 0; c < N; c += 16) {
+                    uint32_t o[16];
+                    tmem_ld16(tm + lane_base + j * N + c, o);
+                    tmem_wait_ld();
+                    if (s.whole) {
+                        __nv_bfloat16 *dst = p.a.out + (static_cast<size_t>(s.b) * p.a.Hq + h0 + c) * kLatentDim + latent;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (c + k < nh) dst[static_cast<size_t>(k) * kLatentDim] = __float2bfloat16_rn(__uint_as_float(o[k]) * inv[c + k]);
+                    } else {
+                        float *dst = p.a.part_o + (static_cast<size_t>(s.slot) * p.a.Hq + h0 + c) * kLatentDim + latent;
+#pragma unroll
+                        for (int k = 0; k < 16; ++k)
+                            if (c + k < nh) dst[static_cast<size_t>(k) * kLatentDim] = __uint_as_float(o[k]);
+                    }
+                }
+            }
+            tc_fence_before_sync();
+            softmax_sync();
+            if (lane == 0) mbar_arrive(bar_o);
+        }
+        if (!ok && lane == 0) latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
+    }
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tm, kTmemCols);
+}
+
+// Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A group of
+// 128 threads holds 4 values each of a row; PARTS groups share a row's partials (few rows, many partials), or
+// each takes rows of its own.
+constexpr int kMergeGroups = 4;
+template <int PARTS>
+__global__ void __launch_bounds__(128 * kMergeGroups) latent_merge_kernel(const LatentAttnParams p) {
+    __shared__ float4 part_o[kMergeGroups][128];
+    __shared__ float part_m[kMergeGroups], part_l[kMergeGroups], part_lr[kMergeGroups];
+    grid_dependency_wait();
+    launch_dependents();
+    const int b = blockIdx.y, g = threadIdx.x >> 7, col = threadIdx.x & 127;
+    const int c0 = p.a.cum_pages[b], c1 = p.a.cum_pages[b + 1], size = p.a.plan[kPlanHeaderWords + 2];
+    const int r0 = c0 / size, r1 = (c1 - 1) / size;
+    if (c0 != c1 && r0 == r1) return;  // written by the split kernel
+    const int first = 2 * r0 + (c0 > r0 * size ? 1 : 0);
+    auto slot = [&](int r) { return static_cast<size_t>(r == r0 ? first : 2 * r); };
+    const int h_end = min(static_cast<int>(blockIdx.x + 1) * p.merge_heads, p.a.Hq);
+    for (int h = blockIdx.x * p.merge_heads + g / PARTS; h < h_end; h += kMergeGroups / PARTS) {
+        const size_t row_out = static_cast<size_t>(b) * p.a.Hq + h;
+        __nv_bfloat16 *out = p.a.out + row_out * kLatentDim + col * 4;
+        if (c0 == c1) {
+            if (g % PARTS == 0) *reinterpret_cast<uint2 *>(out) = make_uint2(0u, 0u);
+            if (g % PARTS == 0 && col == 0 && p.a.lse != nullptr) p.a.lse[row_out] = -INFINITY;
+            continue;
+        }
+        float m = -INFINITY, l = 0.f, lr = 0.f;
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto join = [&](float pm, float pl, float plr, const float4 &v) {
+            const float a = fast_exp2(pm - m);
+            o.x = fmaf(a, v.x, o.x), o.y = fmaf(a, v.y, o.y), o.z = fmaf(a, v.z, o.z), o.w = fmaf(a, v.w, o.w);
+            l = fmaf(a, pl, l);
+            lr = fmaf(a, plr, lr);
+        };
+        auto raise = [&](float top) {
+            const float keep = m == top ? 1.f : fast_exp2(m - top);
+            o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep, l *= keep, lr *= keep;
+            m = top;
+        };
+        constexpr int U = 4;  // partials in flight
+        for (int r = r0 + g % PARTS; r <= r1; r += PARTS * U) {
+            float4 v[U], ml[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int x = r + u * PARTS;
+                if (x <= r1) {
+                    const size_t row = slot(x) * p.a.Hq + h;
+                    ml[u] = p.part_ml[row];
+                    v[u] = reinterpret_cast<const float4 *>(p.a.part_o + row * kLatentDim)[col];
+                } else {
+                    ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+                    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+                }
+            }
+            raise(fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)));  // finite: ml[0] is a partial's reference
+#pragma unroll
+            for (int u = 0; u < U; ++u) join(ml[u].x, ml[u].y, ml[u].z, v[u]);
+        }
+        if (PARTS > 1) {
+            part_o[g][col] = o;
+            if (col == 0) part_m[g] = m, part_l[g] = l, part_lr[g] = lr;
+            __syncthreads();
+            if (g != 0) return;  // (one row per block)
+#pragma unroll
+            for (int i = 1; i < PARTS; ++i) {
+                raise(fmaxf(m, part_m[i]));  // the first group has a partial
+                join(part_m[i], part_l[i], part_lr[i], part_o[i][col]);
+            }
+        }
+        const float inv = 1.f / lr;
+        *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+        if (col == 0 && p.a.lse != nullptr) p.a.lse[row_out] = (m + log2f(l)) * kLn2;
+    }
+}
+
+template <int N>
+cudaError_t prepare() {
+    return cudaFuncSetAttribute(decode_attn_latent_kernel<N>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem_bytes<N>()));
+}
+
+}  // namespace
+
+int latent_heads_per_cta(int heads) { return heads <= 16 ? 16 : heads <= 32 ? 32 : 64; }
+
+cudaError_t prepare_decode_attn_latent() {
+    cudaError_t e = prepare<16>();
+    if (e == cudaSuccess) e = prepare<32>();
+    if (e == cudaSuccess) e = prepare<64>();
+    return e;
+}
+
+cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_q, const LatentAttnParams &p, int num_ctas,
+                                      cudaStream_t stream) {
+    auto go = [&](auto *k, size_t smem) { return launch_pdl(k, dim3(num_ctas), dim3(kThreads), smem, stream, p.a.pdl != 0, tm_kv, tm_q, p); };
+    const int n = latent_heads_per_cta(p.heads);
+    const cudaError_t err = n == 16   ? go(decode_attn_latent_kernel<16>, smem_bytes<16>())
+                            : n == 32 ? go(decode_attn_latent_kernel<32>, smem_bytes<32>())
+                                      : go(decode_attn_latent_kernel<64>, smem_bytes<64>());
+    if (err != cudaSuccess) return err;
+    // Few rows are cut into many partials each: a block per row, its groups side by side. Otherwise a group per row, and as
+    // many rows per block as leave a few thousand blocks (most of which find nothing to do on large batches).
+    LatentAttnParams q = p;
+    const long long rows = static_cast<long long>(p.a.B) * p.a.Hq;
+    const bool few = rows <= 2048;
+    q.merge_heads = few ? 1 : kMergeGroups * static_cast<int>((rows + 16383) / 16384);
+    const dim3 grid((p.a.Hq + q.merge_heads - 1) / q.merge_heads, p.a.B);
+    return few ? launch_pdl(latent_merge_kernel<kMergeGroups>, grid, dim3(128 * kMergeGroups), 0, stream, p.a.pdl != 0, q)
+               : launch_pdl(latent_merge_kernel<1>, grid, dim3(128 * kMergeGroups), 0, stream, p.a.pdl != 0, q);
+}
+
+}  // namespace pd

@@ -190,6 +190,38 @@ struct RopeParams {
     int32_t B, Hq, Hkv, D, MP, num_pages, total, advance, tile, single, pdl;  // single: one token per sequence was announced
 };
 
+// ---- a cache of shared latent vectors: one row of kLatentRow values per token, pages [num_pages][16][kLatentRow]
+constexpr int kLatentDim = 512, kLatentRope = 64, kLatentRow = kLatentDim + kLatentRope;
+constexpr int kLatentHead = 128;             // width of a head's expanded K (beside the rotated part) and V
+constexpr int kLatentMaxHeads = 128;
+
+struct LatentAttnParams {
+    AttnParams a;                // q [B][Hq][576], out [B][Hq][512], part_o [slots][Hq][512]
+    float4 *part_ml;             // [slots][Hq] reference (log2 units), sum, sum of the rounded weights
+    int32_t groups, heads;       // groups of at most 64 heads, heads per group
+    int32_t merge_heads;         // heads per block of the merge kernel (set at its launch)
+};
+
+// New tokens' rows into the pages: latent normalised, key part and queries rotated.
+struct LatentAppendParams {
+    unsigned long long freq[kLatentRope / 2];  // turns per position, 64-bit fixed point
+    uint8_t axis_of_pair[kLatentRope / 2];
+    float magnitude;
+    int32_t rot_dim, adjacent;
+    const int32_t *positions;    // [axes][position_stride] or null: the token's index in its sequence
+    long long position_stride;
+    const __nv_bfloat16 *q, *kv_new, *norm_weight;  // q, norm_weight: or null
+    __nv_bfloat16 *q_out;
+    long long q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, kv_stride;  // in values
+    float norm_eps;
+    const int32_t *q_indptr;
+    __nv_bfloat16 *kv_pages;
+    const int32_t *page_table;
+    int32_t *ctx_lens;
+    int32_t *status;
+    int32_t B, Hq, MP, num_pages, advance, tile, pdl;
+};
+
 struct AttnVariant {
     int head_dim, warps, stages, hilo;
 };
@@ -238,6 +270,12 @@ cudaError_t launch_kv_append_q4(const AppendQ4Params &p, int max_q_len, int num_
 cudaError_t launch_kv_dequantize_q4(const DequantizeQ4Params &p, int num_sms, cudaStream_t stream);
 // *launched: kernels enqueued. append: 0 = rotate only, 1 = into bf16 pages, 2 = into 4-bit pages
 cudaError_t launch_rope(const RopeParams &p, int append, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
+// shared latent vectors
+int latent_heads_per_cta(int heads);         // heads the kernel is built for that takes `heads` (box height of the Q tensor map)
+cudaError_t prepare_decode_attn_latent();
+cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_q, const LatentAttnParams &p, int num_ctas,
+                                      cudaStream_t stream);
+cudaError_t launch_rope_append_latent(const LatentAppendParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_transfer(const TransferParams &p, bool scatter, int num_sms, cudaStream_t stream);
 
 }  // namespace pd
