@@ -567,6 +567,28 @@ int pd_rope_append_tokens_latent(pd_ctx *ctx, const pd_rope_config *rope, const 
 int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_table, const int32_t *ctx_lens,
                           void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream);
 
+/*
+ * Expanded K and V: for tokens [first_token[b], ctx_lens[b]) of every sequence (first_token NULL = from 0) and every head,
+ * W_h[0:128] c goes to k_pages and W_h[128:256] c to v_pages, both [expanded_num_pages][num_q_heads][16][128] bf16 and 32-byte
+ * aligned, at the same slots of the pages of expanded_table ([batch][max_pages_per_seq], of its own ids in
+ * [0, expanded_num_pages)). w_kv is W, [num_q_heads][256][512] bf16. Sums are fp32, rounded once to bf16. Other slots of the
+ * destination keep what they hold. A page id out of range in either table skips that page, a negative first_token or length or a
+ * length past the table skips the sequence; both are latched for pd_device_status. Two sequences may share latent
+ * pages; pages they share in expanded_table get the same values twice.
+ */
+int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, const int32_t *page_table, const int32_t *first_token,
+                        const int32_t *ctx_lens, void *k_pages, void *v_pages, const int32_t *expanded_table,
+                        int64_t expanded_num_pages, int32_t batch, void *stream);
+
+/*
+ * Append-prefill attention in the expanded form: as pd_prefill_attn with q [total][num_q_heads][192], out
+ * [total][num_q_heads][128] bf16, logits sm_scale * (q[0:128] . K_h + q[128:192] . r) with K_h and V_h from the expanded
+ * pages and r from the latent pages, all of which hold the new tokens already (ctx_lens counts them).
+ */
+int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, const void *k_pages, const void *v_pages,
+                           const int32_t *expanded_table, int64_t expanded_num_pages, const void *kv_pages, const int32_t *page_table,
+                           const int32_t *ctx_lens, void *out, float *lse, int32_t batch, int32_t max_q_len, float sm_scale, void *stream);
+
 /* ---- Elastic KV pool on CUDA virtual memory management (Sec. 4.6: the intra-scale toggle keeps the
  * rollout process and swaps device state; Sec. 5: the KV cache is released when training begins and
  * restored when the GPU is available again). A pool is a device address range of `capacity` bytes whose

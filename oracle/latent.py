@@ -41,16 +41,17 @@ def _weights(logits, size):
     return e / total, (top + np.log(total))[..., 0], 36 * 2.0 ** -20 * size.max(-1)
 
 
-def _attend(p, v, shift, extra):
-    """sum p v and its bound. Rounded weights p (1 + d), normalised by their own sum, move the result by at most the largest d times
-    sum p |v - out|; a change of the logits by `shift` by twice that; fp32 sums by 2^-20 per 16 tokens of sum p |v|; then one
-    rounding to bf16."""
+def _attend(p, v, shift, own_sum):
+    """sum p v and its bound. Rounded weights p (1 + d), |d| <= 2^-8, move the result by sum p d v: at most 2^-8 of sum p |v|
+    where the unrounded weights' sum normalises it; where the rounded ones' does (`own_sum`), sum p d (v - out) / sum p (1 + d): at most
+    1.01 * 2^-8 of sum p |v - out|. A change of every logit by at most `shift` moves it by 2 shift (1 + shift) sum p |v - out|; fp32 sums
+    by 2^-22 per 16 tokens of sum p |v|; then one rounding to bf16."""
     out = p @ v
     spread = np.empty_like(out)
     for i in range(out.shape[0]):
         spread[i] = p[i] @ np.abs(v - out[i])
     size = p @ np.abs(v)
-    err = (1.02 * BF16 + 2.1 * shift[:, None]) * spread + (v.shape[0] / 16 + 32) * 2.0 ** -22 * size + extra
+    err = 1.02 * BF16 * (spread if own_sum else size) + 2.1 * shift[:, None] * spread + (v.shape[0] / 16 + 32) * 2.0 ** -22 * size
     return out, err + BF16 * (np.abs(out) + err)
 
 
@@ -64,7 +65,7 @@ def decode(q, pages, table, lens, scale):
             continue
         x = rows_of(pages, table[i], int(n))
         p, lse[i], shift = _weights(scale * (q[i] @ x.T), scale * (np.abs(q[i]) @ np.abs(x).T))
-        out[i], bound[i] = _attend(p, x[:, :LATENT], shift, 0.0)
+        out[i], bound[i] = _attend(p, x[:, :LATENT], shift, True)
         lbound[i] = shift + 2.0 ** -18 + 2.0 ** -21 * np.abs(lse[i])
     return out, lse, bound, lbound
 
@@ -75,8 +76,9 @@ def expand(w, pages, table, lens, first=None):
     for i, n in enumerate(lens):
         lo = 0 if first is None else int(first[i])
         c = rows_of(pages, table[i], int(n))[lo:, :LATENT]
-        kv = np.einsum("hdl,tl->thd", w, c)
-        tol = 32 * 2.0 ** -20 * np.einsum("hdl,tl->thd", np.abs(w), np.abs(c))
+        flat, shape = w.reshape(-1, LATENT), (len(c), w.shape[0], 2 * HEAD)
+        kv = (c @ flat.T).reshape(shape)
+        tol = 32 * 2.0 ** -20 * (np.abs(c) @ np.abs(flat).T).reshape(shape)
         tol = tol + BF16 * (np.abs(kv) + tol)
         done.append((lo, kv[..., :HEAD], kv[..., HEAD:], tol[..., :HEAD], tol[..., HEAD:]))
     return done
@@ -100,6 +102,6 @@ def prefill(q, indptr, k_pages, v_pages, kv_table, pages, table, lens, scale):
             v = v_pages[ids, j].reshape(-1, HEAD)[:n]
             z = np.where(seen, scale * (q[lo:hi, j] @ k.T), -np.inf)
             p, lse[lo:hi, j], shift = _weights(z, np.where(seen, scale * (np.abs(q[lo:hi, j]) @ np.abs(k).T), 0.0))
-            out[lo:hi, j], bound[lo:hi, j] = _attend(p, v, shift, 0.0)
+            out[lo:hi, j], bound[lo:hi, j] = _attend(p, v, shift, False)
             lbound[lo:hi, j] = shift + 2.0 ** -18 + 2.0 ** -21 * np.abs(lse[lo:hi, j])
     return out, lse, bound, lbound

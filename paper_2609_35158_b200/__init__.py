@@ -34,7 +34,7 @@ EXPORTS = (
     "pd_kv_quantize_pages", "pd_kv_append_fp8", "pd_decode_attn_fp8", "pd_decode_step_fp8", "pd_kv_gather_fp8", "pd_kv_scatter_fp8",
     "pd_kv_append_q4", "pd_kv_append_tokens_q4", "pd_kv_dequantize_q4", "pd_decode_attn_q4", "pd_decode_step_q4",
     "pd_rope_tokens", "pd_rope_append_tokens", "pd_rope_append_tokens_q4",
-    "pd_rope_append_tokens_latent", "pd_decode_attn_latent",
+    "pd_rope_append_tokens_latent", "pd_decode_attn_latent", "pd_kv_expand_latent", "pd_prefill_attn_latent",
     "pd_pool_create", "pd_pool_resize", "pd_pool_base", "pd_pool_capacity", "pd_pool_chunk_bytes", "pd_pool_resident_bytes",
     "pd_pool_last_error", "pd_pool_destroy",
     "pd_set_profile_events", "pd_read_probe", "pd_rope_turns", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
@@ -136,6 +136,8 @@ def _load() -> ctypes.CDLL:
     lib.pd_rope_append_tokens_latent.argtypes = [vp, pr, vp, i64, vp, i64, i64, vp, i64, vp, f32, vp, vp, i64, i64, vp, vp, vp, i32,
                                                  i32, u32, vp]
     lib.pd_decode_attn_latent.argtypes = [vp, vp, vp, vp, vp, vp, vp, i32, f32, i32, vp]
+    lib.pd_kv_expand_latent.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, i64, i32, vp]
+    lib.pd_prefill_attn_latent.argtypes = [vp, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp, vp, i32, i32, f32, vp]
     u64 = ctypes.c_uint64
     lib.pd_rope_turns.argtypes = [f32, ctypes.POINTER(u64)]
     lib.pd_pool_create.argtypes = [i32, u64, u64, ctypes.POINTER(vp)]
@@ -452,6 +454,23 @@ def pd_decode_attn_latent(ctx, q, kv_pages, page_table, ctx_lens, out, lse=None,
     _check(_lib.pd_decode_attn_latent(ctx, _ptr(q), _ptr(kv_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(out),
                                       _optional_ptr(lse, batch > 0, "lse"), batch, sm_scale, split_pages, _stream(stream)),
            "pd_decode_attn_latent", ctx)
+
+
+def pd_kv_expand_latent(ctx, w_kv, kv_pages, page_table, first_token, ctx_lens, k_pages, v_pages, expanded_table, batch=None, stream=None):
+    """``first_token`` may be None (every sequence from its first token). The expanded pools' page count is ``k_pages.shape[0]``."""
+    batch = ctx_lens.shape[0] if batch is None else batch
+    _check(_lib.pd_kv_expand_latent(ctx, _ptr(w_kv), _ptr(kv_pages), _ptr(page_table), _optional_ptr(first_token, batch > 0, "first_token"),
+                                    _ptr(ctx_lens), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), k_pages.shape[0], batch,
+                                    _stream(stream)), "pd_kv_expand_latent", ctx)
+
+
+def pd_prefill_attn_latent(ctx, q, q_indptr, k_pages, v_pages, expanded_table, kv_pages, page_table, ctx_lens, out, lse=None, max_q_len=0,
+                           batch=None, sm_scale=1.0, stream=None):
+    batch = q_indptr.shape[0] - 1 if batch is None else batch
+    _check(_lib.pd_prefill_attn_latent(ctx, _ptr(q), _ptr(q_indptr), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), k_pages.shape[0],
+                                       _ptr(kv_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(out),
+                                       _optional_ptr(lse, batch > 0 and max_q_len > 0, "lse"), batch, max_q_len, sm_scale, _stream(stream)),
+           "pd_prefill_attn_latent", ctx)
 
 
 def pd_pool_create(device: int, capacity_bytes: int, chunk_bytes: int = 0):

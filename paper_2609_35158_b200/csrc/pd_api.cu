@@ -79,8 +79,13 @@ struct pd_ctx {
     cudaEvent_t ev_before = nullptr, ev_after = nullptr;  // optional timing hook around the split kernel
     // a context for shared latent vectors (PD_FLAG_LATENT): its pool's and its queries' tensor maps
     bool latent = false;
-    bool latent_decode_ready = false;
-    const void *map_latent_ptr = nullptr, *map_latent_q_ptr = nullptr;
+    bool latent_decode_ready = false, latent_expand_ready = false, latent_prefill_ready = false;
+    const void *map_latent_ptr = nullptr, *map_latent_q_ptr = nullptr, *map_latent_w_ptr = nullptr;
+    const void *map_expanded_k_ptr = nullptr, *map_expanded_v_ptr = nullptr;
+    int64_t map_expanded_pages = 0;  // of both expanded pools' maps
+    alignas(64) CUtensorMap tm_latent_w{};
+    alignas(64) CUtensorMap tm_expanded_k{};
+    alignas(64) CUtensorMap tm_expanded_v{};
     alignas(64) CUtensorMap tm_latent{};
     alignas(64) CUtensorMap tm_latent_q{};
     float4 *part_ml4 = nullptr;
@@ -156,19 +161,6 @@ int encode_pool_map_fp8(pd_ctx *ctx, const void *pool, CUtensorMap *out) {
 int latent_groups(int heads) { return (heads + 63) / 64; }
 int latent_group_heads(int heads) { return (heads + latent_groups(heads) - 1) / latent_groups(heads); }
 
-// A pool of shared latent vectors: rows = (page, slot), 576 columns; box = 16 rows x 64 columns with the 128-byte swizzle.
-int encode_latent_map(pd_ctx *ctx, const void *pool, CUtensorMap *out) {
-    const cuuint64_t dims[2] = {pd::kLatentRow, static_cast<cuuint64_t>(ctx->cfg.num_pages) * pd::kPageSize};
-    const cuuint64_t strides[1] = {pd::kLatentRow * 2};
-    const cuuint32_t box[2] = {64, pd::kPageSize}, elem_strides[2] = {1, 1};
-    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(pool), dims, strides, box,
-                                   elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r == CUDA_SUCCESS) return PD_OK;
-    std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
-    return PD_ERR_CUDA;
-}
-
 // Absorbed queries [batch][heads][576]: box = 64 columns of the heads one block takes; heads past the last are zero fill.
 int encode_latent_q_map(pd_ctx *ctx, const void *q, CUtensorMap *out) {
     const cuuint64_t heads = static_cast<cuuint64_t>(ctx->cfg.num_q_heads);
@@ -182,6 +174,27 @@ int encode_latent_q_map(pd_ctx *ctx, const void *q, CUtensorMap *out) {
     if (r == CUDA_SUCCESS) return PD_OK;
     std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
     return PD_ERR_CUDA;
+}
+
+// A matrix of bf16 rows, `width` columns; box = 64 columns x `box_rows`, 128-byte swizzle.
+int encode_rows_map(pd_ctx *ctx, const void *ptr, int width, int64_t rows, int box_rows, CUtensorMap *out) {
+    const cuuint64_t dims[2] = {static_cast<cuuint64_t>(width), static_cast<cuuint64_t>(rows)};
+    const cuuint64_t strides[1] = {static_cast<cuuint64_t>(width) * 2};
+    const cuuint32_t box[2] = {64, static_cast<cuuint32_t>(box_rows)}, elem_strides[2] = {1, 1};
+    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void *>(ptr), dims, strides, box,
+                                   elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return PD_OK;
+    std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+    return PD_ERR_CUDA;
+}
+
+// A pool of shared latent vectors: rows = (page, slot).
+int latent_map(pd_ctx *ctx, const void *kv_pages) {
+    if (ctx->map_latent_ptr == kv_pages) return PD_OK;
+    if (int rc = encode_rows_map(ctx, kv_pages, pd::kLatentRow, ctx->cfg.num_pages * pd::kPageSize, pd::kPageSize, &ctx->tm_latent)) return rc;
+    ctx->map_latent_ptr = kv_pages;
+    return PD_OK;
 }
 
 // `latent`: the kind of context the call is for.
@@ -1409,10 +1422,7 @@ int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, cons
         if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent decode kernel attribute", e);
         ctx->latent_decode_ready = true;
     }
-    if (ctx->map_latent_ptr != kv_pages) {
-        if (int rc = encode_latent_map(ctx, kv_pages, &ctx->tm_latent)) return rc;
-        ctx->map_latent_ptr = kv_pages;
-    }
+    if (int rc = latent_map(ctx, kv_pages)) return rc;
     if (ctx->map_latent_q_ptr != q) {
         if (int rc = encode_latent_q_map(ctx, q, &ctx->tm_latent_q)) return rc;
         ctx->map_latent_q_ptr = q;
@@ -1443,6 +1453,110 @@ int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, cons
     const cudaError_t err = pd::launch_decode_attn_latent(ctx->tm_latent, ctx->tm_latent_q, p, ctx->num_sms / p.groups * p.groups,
                                                           static_cast<cudaStream_t>(stream));
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent decode launch", err);
+    ctx->launches += 2;
+    return PD_OK;
+}
+
+// Pages of the expanded pools: ids and tensor-map rows are 32-bit.
+static int check_expanded_pages(pd_ctx *ctx, int64_t n) {
+    if (n < 1) return fail(ctx, PD_ERR_INVALID_ARG, "expanded_num_pages must be positive");
+    if (n >= (int64_t(1) << 31) / (static_cast<int64_t>(ctx->cfg.num_q_heads) * pd::kPageSize))
+        return fail(ctx, PD_ERR_UNSUPPORTED, "expanded_num_pages * num_q_heads * page_size must stay below 2^31");
+    return PD_OK;
+}
+
+int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, const int32_t *page_table, const int32_t *first_token,
+                        const int32_t *ctx_lens, void *k_pages, void *v_pages, const int32_t *expanded_table,
+                        int64_t expanded_num_pages, int32_t batch, void *stream) {
+    if (int rc = check_batch(ctx, batch, true)) return rc;
+    if (!aligned16(w_kv) || !aligned16(kv_pages) || page_table == nullptr || ctx_lens == nullptr || expanded_table == nullptr ||
+        k_pages == nullptr || v_pages == nullptr || ((reinterpret_cast<uintptr_t>(k_pages) | reinterpret_cast<uintptr_t>(v_pages)) & 31u) != 0)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_kv_expand_latent: null or misaligned pointer");
+    if (int rc = check_expanded_pages(ctx, expanded_num_pages)) return rc;
+    if (batch == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    if (!ctx->latent_expand_ready) {
+        const cudaError_t e = pd::prepare_kv_expand_latent();
+        if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent expansion kernel attribute", e);
+        ctx->latent_expand_ready = true;
+    }
+    if (int rc = latent_map(ctx, kv_pages)) return rc;
+    if (ctx->map_latent_w_ptr != w_kv) {
+        const int rows = 2 * pd::kLatentHead;
+        if (int rc = encode_rows_map(ctx, w_kv, pd::kLatentDim, static_cast<int64_t>(ctx->cfg.num_q_heads) * rows, rows, &ctx->tm_latent_w)) return rc;
+        ctx->map_latent_w_ptr = w_kv;
+    }
+    pd::LatentExpandParams p{};
+    p.page_table = page_table;
+    p.dst_table = expanded_table;
+    p.first_token = first_token;
+    p.ctx_lens = ctx_lens;
+    p.k_pages = static_cast<__nv_bfloat16 *>(k_pages);
+    p.v_pages = static_cast<__nv_bfloat16 *>(v_pages);
+    p.status = ctx->status;
+    p.B = batch;
+    p.Hq = ctx->cfg.num_q_heads;
+    p.MP = ctx->cfg.max_pages_per_seq;
+    p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.dst_num_pages = static_cast<int32_t>(expanded_num_pages);
+    p.pdl = ctx->pdl;
+    const cudaError_t err = pd::launch_kv_expand_latent(ctx->tm_latent, ctx->tm_latent_w, p, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent expansion launch", err);
+    ctx->launches += 1;
+    return PD_OK;
+}
+
+int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, const void *k_pages, const void *v_pages,
+                           const int32_t *expanded_table, int64_t expanded_num_pages, const void *kv_pages, const int32_t *page_table,
+                           const int32_t *ctx_lens, void *out, float *lse, int32_t batch, int32_t max_q_len, float sm_scale, void *stream) {
+    if (int rc = check_batch(ctx, batch, true)) return rc;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(kv_pages) || !aligned16(out) || q_indptr == nullptr ||
+        page_table == nullptr || expanded_table == nullptr || ctx_lens == nullptr)
+        return fail(ctx, PD_ERR_INVALID_ARG, "pd_prefill_attn_latent: null or misaligned pointer");
+    if (!(sm_scale > 0.f) || !(sm_scale < 3.0e38f)) return fail(ctx, PD_ERR_INVALID_ARG, "sm_scale must be finite and positive");
+    if (max_q_len < 0) return fail(ctx, PD_ERR_INVALID_ARG, "max_q_len must be >= 0");
+    if (int rc = check_expanded_pages(ctx, expanded_num_pages)) return rc;
+    if (batch == 0 || max_q_len == 0) return PD_OK;
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    if (!ctx->latent_prefill_ready) {
+        const cudaError_t e = pd::prepare_prefill_attn_latent();
+        if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent prefill kernel attribute", e);
+        ctx->latent_prefill_ready = true;
+    }
+    if (int rc = latent_map(ctx, kv_pages)) return rc;
+    const int64_t rows = expanded_num_pages * ctx->cfg.num_q_heads * pd::kPageSize;
+    if (ctx->map_expanded_k_ptr != k_pages || ctx->map_expanded_v_ptr != v_pages || ctx->map_expanded_pages != expanded_num_pages) {
+        ctx->map_expanded_k_ptr = nullptr;
+        if (int rc = encode_rows_map(ctx, k_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_k)) return rc;
+        if (int rc = encode_rows_map(ctx, v_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_v)) return rc;
+        ctx->map_expanded_k_ptr = k_pages;
+        ctx->map_expanded_v_ptr = v_pages;
+        ctx->map_expanded_pages = expanded_num_pages;
+    }
+    pd::LatentPrefillParams p{};
+    p.a.q = static_cast<const __nv_bfloat16 *>(q);
+    p.a.q_indptr = q_indptr;
+    p.a.page_table = page_table;
+    p.a.ctx_lens = ctx_lens;
+    p.a.out = static_cast<__nv_bfloat16 *>(out);
+    p.a.lse = lse;
+    p.a.status = ctx->status;
+    p.a.B = batch;
+    p.a.Hq = ctx->cfg.num_q_heads;
+    p.a.Hkv = p.a.Hq;
+    p.a.G = 1;
+    p.a.MP = ctx->cfg.max_pages_per_seq;
+    p.a.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
+    p.a.scale_log2 = sm_scale * 1.4426950408889634f;
+    p.a.pdl = ctx->pdl;
+    p.a.order = ctx->cum_pages;  // the decode kernel's prefix-sum buffer is free here
+    p.kv_table = expanded_table;
+    p.kv_num_pages = static_cast<int32_t>(expanded_num_pages);
+    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len,
+                                                           static_cast<cudaStream_t>(stream));
+    if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent prefill launch", err);
     ctx->launches += 2;
     return PD_OK;
 }

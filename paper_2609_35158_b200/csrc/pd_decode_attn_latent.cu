@@ -57,12 +57,6 @@ __host__ __device__ constexpr size_t smem_bytes() {
     return 1024 + kRowChunks * N * 128 + kPBytes + kRopeSlots * kChunkBytes + pair_slots<N>() * kPairBytes + kControlBytes;
 }
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t e;
-    asm volatile("{\n.reg .pred p;\nelect.sync _|p, 0xffffffff;\nselp.u32 %0, 1, 0, p;\n}" : "=r"(e));
-    return e != 0;
-}
-
 __device__ __forceinline__ void softmax_sync() { asm volatile("barrier.cta.sync 1, %0;" ::"n"(kSoftmaxThreads) : "memory"); }
 __device__ __forceinline__ bool softmax_any(bool v) {
     uint32_t r;

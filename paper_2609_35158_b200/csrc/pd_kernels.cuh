@@ -222,6 +222,22 @@ struct LatentAppendParams {
     int32_t B, Hq, MP, num_pages, advance, tile, pdl;
 };
 
+// Expanded K and V of cached tokens [first_token[b], ctx_lens[b]).
+struct LatentExpandParams {
+    const int32_t *page_table, *dst_table;       // [B][MP] each
+    const int32_t *first_token;                  // [B] or null (0)
+    const int32_t *ctx_lens;
+    __nv_bfloat16 *k_pages, *v_pages;            // [dst_num_pages][Hq][16][128]
+    int32_t *status;
+    int32_t B, Hq, MP, num_pages, dst_num_pages, pdl;
+};
+
+struct LatentPrefillParams {
+    PrefillParams a;             // q [total][Hq][192], out [total][Hq][128]; page_table, num_pages: the latent pages
+    const int32_t *kv_table;     // [B][MP] pages of the expanded K and V
+    int32_t kv_num_pages;
+};
+
 struct AttnVariant {
     int head_dim, warps, stages, hilo;
 };
@@ -260,6 +276,8 @@ cudaError_t launch_kv_append_fp8(const AppendFp8Params &p, cudaStream_t stream);
 cudaError_t prepare_prefill_attn(int head_dim);  // opt-in shared memory, once
 cudaError_t launch_prefill_attn(int head_dim, const CUtensorMap &tm_k, const CUtensorMap &tm_v, const PrefillParams &p,
                                 int max_q_len, cudaStream_t stream);
+// p.order[i] = the sequence with the i-th most attention work
+cudaError_t launch_prefill_order(const PrefillParams &p, cudaStream_t stream);
 cudaError_t launch_kv_append_tokens(const AppendTokensParams &p, int max_q_len, cudaStream_t stream);
 // ctx_lens[b] += q_indptr[b + 1] - q_indptr[b] where the table row has room (the second half of a multi-token append)
 cudaError_t launch_advance_lens(const AppendTokensParams &p, cudaStream_t stream);
@@ -275,6 +293,12 @@ int latent_heads_per_cta(int heads);         // heads the kernel is built for th
 cudaError_t prepare_decode_attn_latent();
 cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_q, const LatentAttnParams &p, int num_ctas,
                                       cudaStream_t stream);
+cudaError_t prepare_kv_expand_latent();
+cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_sms,
+                                    cudaStream_t stream);
+cudaError_t prepare_prefill_attn_latent();
+cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
+                                       const LatentPrefillParams &p, int max_q_len, cudaStream_t stream);
 cudaError_t launch_rope_append_latent(const LatentAppendParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_transfer(const TransferParams &p, bool scatter, int num_sms, cudaStream_t stream);
 

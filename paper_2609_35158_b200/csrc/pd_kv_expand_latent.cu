@@ -1,0 +1,276 @@
+// K and V of every head from cached latents: K_h = W_h[0:128] c, V_h = W_h[128:256] c, for the tokens of a batch of contexts,
+// from latent pages into pages of bf16 K and V. A matrix product [tokens x 512] x [512 x 256 per head] whose rows are gathered
+// by page and whose results are scattered by page.
+//
+// A unit is (tile of 128 tokens, head): 32 MMAs of 128 x 256 x 16, 4096 cycles, for 128 KB of latents, 256 KB of W (from L2)
+// and 64 KB of results. A CTA per SM walks a run of units, heads innermost: the tile's latents (8 blocks of 64 columns) stay in
+// shared memory over its heads, W streams through a ring of three 32 KB blocks, and each block of the next tile is
+// fetched as soon as the last head's product has passed it. Two accumulators of 256 columns fill tensor memory, so the products
+// of one unit run while the results of the last are stored: a thread holds a token's row and stores 32 bytes at a time.
+#include "pd_decode_plan.cuh"
+#include "pd_kernels.cuh"
+#include "pd_ptx.cuh"
+#include "pd_tcgen05.cuh"
+
+namespace pd {
+
+namespace {
+
+constexpr int kTile = 128, kTilePages = kTile / kPageSize;
+constexpr int kCols = 2 * kLatentHead;           // K and V of a head
+constexpr int kChunks = kLatentDim / 64;
+constexpr int kABytes = kTile * 128;             // 64 columns of the tile
+constexpr int kBBytes = kCols * 128;
+constexpr int kStages = 3;
+constexpr int kThreads = 128 + 64;               // store warps + TMA warp + MMA warp
+constexpr int kTmemCols = 512;
+constexpr int kNumBars = 2 * kChunks + 2 * kStages + 4 + 1;
+constexpr size_t kSmemBytes = 1024 + kChunks * kABytes + kStages * kBBytes + kNumBars * 8;
+
+// The tokens of a sequence that are wanted, and the tiles they take: from the page of the first one on.
+struct Span {
+    int first, len, page0, tiles;
+};
+__device__ __forceinline__ Span span_of(const LatentExpandParams &p, int b) {
+    Span s;
+    s.first = p.first_token != nullptr ? __ldg(p.first_token + b) : 0;
+    s.len = __ldg(p.ctx_lens + b);
+    if (s.first < 0 || s.len < 0 || s.len > p.MP * kPageSize || s.first >= s.len) s.first = s.len = 0;
+    s.page0 = s.first / kPageSize;
+    s.tiles = (s.len - s.page0 * kPageSize + kTile - 1) / kTile;
+    return s;
+}
+
+struct Walk {
+    int b, tile, head;
+    Span s;
+};
+__device__ __forceinline__ void step(Walk &w, const LatentExpandParams &p) {
+    if (++w.head < p.Hq) return;
+    w.head = 0;
+    if (++w.tile < w.s.tiles) return;
+    w.tile = 0;
+    do {
+        if (++w.b >= p.B) return;  // behind the last unit
+        w.s = span_of(p, w.b);
+    } while (w.s.tiles == 0);
+}
+
+__device__ __forceinline__ void store32(void *dst, const uint32_t (&v)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+kv_expand_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_w, const LatentExpandParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int32_t warp_sums[kThreads / 32];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t *aligned = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t a_s = base, b_ring = base + kChunks * kABytes;
+    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + kChunks * kABytes + kStages * kBBytes);
+    const uint32_t bar_a = smem_u32(bars), bar_afree = bar_a + kChunks * 8;
+    const uint32_t bar_b = bar_afree + kChunks * 8, bar_bfree = bar_b + kStages * 8;
+    const uint32_t bar_d = bar_bfree + kStages * 8, bar_dfree = bar_d + 16, bar_drain = bar_dfree + 16;
+    if (tid == 0) {
+        for (int i = 0; i < kNumBars; ++i) mbar_init(bar_a + i * 8, bar_a + i * 8 == bar_dfree || bar_a + i * 8 == bar_dfree + 8 ? 4 : 1);
+        mbar_init_fence();
+        prefetch_tensormap(&tm_kv);
+        prefetch_tensormap(&tm_w);
+    }
+    if (warp == 0) {
+        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
+        tmem_relinquish_alloc_permit();
+    }
+    grid_dependency_wait();
+    launch_dependents();
+
+    // ---- prefix sums of the tiles, in memory that no copy uses yet
+    int32_t *cum = reinterpret_cast<int32_t *>(aligned);
+    {
+        const int items = (p.B + kThreads - 1) / kThreads, begin = min(p.B, tid * items), end = min(p.B, begin + items);
+        int sum = 0;
+        for (int i = begin; i < end; ++i) {
+            const int len = __ldg(p.ctx_lens + i), first = p.first_token != nullptr ? __ldg(p.first_token + i) : 0;
+            if (blockIdx.x == 0 && (len < 0 || len > p.MP * kPageSize || first < 0)) latch_status(p.status, kDevBadLength, i, first < 0 ? first : len);
+            const int tiles = span_of(p, i).tiles;
+            cum[i] = tiles;
+            sum += tiles;
+        }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (lane == 31) warp_sums[warp] = incl;
+        __syncthreads();
+        int run = incl - sum;
+        for (int w = 0; w < warp; ++w) run += warp_sums[w];
+        for (int i = begin; i < end; ++i) {
+            const int tiles = cum[i];
+            cum[i] = run;
+            run += tiles;
+        }
+        if (tid == kThreads - 1) cum[p.B] = run;
+        __syncthreads();
+    }
+    const long long total = static_cast<long long>(cum[p.B]) * p.Hq;
+    const long long u0 = total * blockIdx.x / gridDim.x;
+    const int units = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x - u0);
+    Walk w{};
+    if (units > 0) {
+        const Cursor c = locate(cum, p.B, 1, div_positive(u0, p.Hq));
+        w.b = c.b;
+        w.tile = c.page;
+        w.head = static_cast<int>(u0 - div_positive(u0, p.Hq) * p.Hq);
+        w.s = span_of(p, c.b);
+    }
+    fence_proxy_async();  // the copies that follow overwrite what was read here
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tm = tmem_slot;
+    bool ok = true;
+
+    if (units > 0 && warp == 4) {
+        // ================= TMA warp =================
+        const uint64_t policy = l2_policy_evict_first();
+        const int32_t oob_row = p.num_pages * kPageSize;
+        int ac = 0, bc = 0;  // blocks of latents and of W issued
+        for (int u = 0; u < units && ok; ++u) {
+            const bool new_tile = u == 0 || w.head == 0;
+            int32_t y = oob_row;
+            if (new_tile && lane < kTilePages) {
+                const int page = w.s.page0 + w.tile * kTilePages + lane;
+                if (page * kPageSize < w.s.len) {
+                    const int pid = __ldg(p.page_table + static_cast<size_t>(w.b) * p.MP + page);
+                    if (pid >= 0 && pid < p.num_pages) y = pid * kPageSize;  // (the store warps latch the others)
+                }
+            }
+            for (int c = 0; c < kChunks && ok; ++c) {
+                if (new_tile) {
+                    if (ac >= kChunks) ok = __all_sync(0xffffffffu, mbar_wait(bar_afree + c * 8, (ac / kChunks - 1) & 1));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(bar_a + c * 8, kABytes);
+                    __syncwarp();
+                    if (lane < kTilePages) tma_load_2d(a_s + c * kABytes + lane * (kPageSize * 128), &tm_kv, c * 64, y, bar_a + c * 8, policy);
+                    ++ac;
+                }
+                const int slot = bc % kStages, fill = bc / kStages;
+                if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_bfree + slot * 8, (fill - 1) & 1));
+                if (!ok) break;
+                if (lane == 0) {
+                    mbar_arrive_expect_tx(bar_b + slot * 8, kBBytes);
+                    tma_load_2d(b_ring + slot * kBBytes, &tm_w, c * 64, w.head * kCols, bar_b + slot * 8, l2_policy_evict_last());
+                }
+                __syncwarp();
+                ++bc;
+            }
+            step(w, p);
+        }
+        if (!ok) {  // copies in flight have to land before the block's memory goes
+            if (lane == 0) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
+            for (int i = max(0, bc - kStages); i < bc; ++i) mbar_wait(bar_b + (i % kStages) * 8, (i / kStages) & 1);
+            for (int i = max(0, ac - kChunks); i < ac; ++i) mbar_wait(bar_a + (i % kChunks) * 8, (i / kChunks) & 1);
+        }
+    } else if (units > 0 && warp == 5) {
+        // ================= MMA warp: one elected thread =================
+        if (elect_one()) {
+            constexpr uint32_t idesc = umma_idesc_bf16(kTile, kCols, false);
+            const uint64_t a_desc = umma_smem_desc(a_s, 16, 1024), b_desc = umma_smem_desc(b_ring, 16, 1024);
+            int tiles = 0, bc = 0;
+            for (int u = 0; u < units && ok; ++u) {
+                const bool new_tile = u == 0 || w.head == 0, last_head = u == units - 1 || w.head == p.Hq - 1;
+                if (new_tile) ++tiles;
+                if (u >= 2) ok = mbar_wait(bar_dfree + (u & 1) * 8, ((u >> 1) - 1) & 1);
+                const uint32_t d = tm + (u & 1) * kCols;
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) {
+                    const int slot = bc % kStages;
+                    if (new_tile) ok = ok && mbar_wait(bar_a + c * 8, (tiles - 1) & 1);
+                    ok = ok && mbar_wait(bar_b + slot * 8, (bc / kStages) & 1);
+                    if (!ok) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        umma_ss(d, a_desc + (c * kABytes >> 4) + ks * 2, b_desc + slot * (kBBytes >> 4) + ks * 2, idesc, (c | ks) != 0);
+                    umma_commit(bar_bfree + slot * 8);
+                    if (last_head) umma_commit(bar_afree + c * 8);
+                    ++bc;
+                }
+                if (!ok) break;
+                umma_commit(bar_d + (u & 1) * 8);
+                step(w, p);
+            }
+            if (!ok) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
+            umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
+            mbar_wait(bar_drain, 0);
+        }
+    } else if (units > 0 && warp < 4) {
+        // ================= store warps: thread = token of the tile =================
+        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+        __nv_bfloat16 *k_dst = nullptr, *v_dst = nullptr;
+        for (int u = 0; u < units && ok; ++u) {
+            if (u == 0 || w.head == 0) {  // where this token's rows of head 0 go, if anywhere
+                const int tok = (w.s.page0 + w.tile * kTilePages) * kPageSize + tid, page = tok / kPageSize;
+                k_dst = v_dst = nullptr;
+                if (tok >= w.s.first && tok < w.s.len) {
+                    const int from = __ldg(p.page_table + static_cast<size_t>(w.b) * p.MP + page);
+                    const int to = __ldg(p.dst_table + static_cast<size_t>(w.b) * p.MP + page);
+                    if (from < 0 || from >= p.num_pages) latch_status(p.status, kDevBadPage, w.b, from);
+                    else if (to < 0 || to >= p.dst_num_pages) latch_status(p.status, kDevBadPage, w.b, to);
+                    else {
+                        const size_t at = (static_cast<size_t>(to) * p.Hq * kPageSize + tok % kPageSize) * kLatentHead;
+                        k_dst = p.k_pages + at;
+                        v_dst = p.v_pages + at;
+                    }
+                }
+            }
+            ok = mbar_wait(bar_d + (u & 1) * 8, (u >> 1) & 1);
+            if (!ok) break;
+            tc_fence_after_sync();
+#pragma unroll
+            for (int c = 0; c < kCols / 32; ++c) {
+                uint32_t o[32];
+                tmem_ld32(tm + lane_base + (u & 1) * kCols + c * 32, o);
+                tmem_wait_ld();
+                if (k_dst != nullptr) {
+                    __nv_bfloat16 *dst = (c < kLatentHead / 32 ? k_dst : v_dst) + static_cast<size_t>(w.head) * kPageSize * kLatentHead + (c % (kLatentHead / 32)) * 32;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        uint32_t v[8];
+#pragma unroll
+                        for (int i = 0; i < 8; ++i)
+                            v[i] = pack_bf16x2(__uint_as_float(o[h * 16 + 2 * i]), __uint_as_float(o[h * 16 + 2 * i + 1]));
+                        store32(dst + h * 16, v);
+                    }
+                }
+            }
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_dfree + (u & 1) * 8);
+            step(w, p);
+        }
+        if (!ok && lane == 0) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
+    }
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 0) tmem_dealloc(tm, kTmemCols);
+}
+
+}  // namespace
+
+cudaError_t prepare_kv_expand_latent() {
+    return cudaFuncSetAttribute(kv_expand_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+}
+
+cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_sms,
+                                    cudaStream_t stream) {
+    return launch_pdl(kv_expand_latent_kernel, dim3(num_sms), dim3(kThreads), kSmemBytes, stream, p.pdl != 0, tm_kv, tm_w, p);
+}
+
+}  // namespace pd

@@ -512,13 +512,17 @@ cudaError_t launch_prefill_attn(int head_dim, const CUtensorMap &tm_k, const CUt
                                 int max_q_len, cudaStream_t stream) {
     if (p.B == 0 || max_q_len <= 0) return cudaSuccess;
     if (p.order != nullptr) {
-        const cudaError_t e = launch_pdl(prefill_order_kernel, dim3((p.B + 255) / 256), dim3(256), 0, stream, p.pdl != 0, p);
+        const cudaError_t e = launch_prefill_order(p, stream);
         if (e != cudaSuccess) return e;
     }
     if (head_dim == 128) return launch_prefill_attn_d128(tm_k, tm_v, p, max_q_len, stream);
     const int tok = kRows / p.G;
     const dim3 grid((max_q_len + tok - 1) / tok, p.Hkv, p.B);
     return launch_pdl(prefill_attn_kernel<64>, grid, dim3(kThreads), prefill_smem_bytes(head_dim), stream, p.pdl != 0, tm_k, tm_v, p);
+}
+
+cudaError_t launch_prefill_order(const PrefillParams &p, cudaStream_t stream) {
+    return launch_pdl(prefill_order_kernel, dim3((p.B + 255) / 256), dim3(256), 0, stream, p.pdl != 0, p);
 }
 
 cudaError_t launch_kv_append_tokens(const AppendTokensParams &p, int max_q_len, cudaStream_t stream) {
