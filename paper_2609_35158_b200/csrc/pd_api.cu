@@ -86,7 +86,7 @@ struct pd_ctx {
     alignas(64) CUtensorMap tm_latent_w{};
     alignas(64) CUtensorMap tm_expanded_k{};
     alignas(64) CUtensorMap tm_expanded_v{};
-    alignas(64) CUtensorMap tm_latent{};
+    alignas(64) CUtensorMap tm_latent{}, tm_latent_pairs{};
     alignas(64) CUtensorMap tm_latent_q{};
     float4 *part_ml4 = nullptr;
     bool prefill_ready = false;
@@ -189,10 +189,22 @@ int encode_rows_map(pd_ctx *ctx, const void *ptr, int width, int64_t rows, int b
     return PD_ERR_CUDA;
 }
 
-// A pool of shared latent vectors: rows = (page, slot).
+// A pool of shared latent vectors, twice: rows = (page, slot) with a box of 16 rows x 64 columns; and as [row group][block of 64
+// columns][8 rows][64], box = both row groups of a page x 2 blocks.
 int latent_map(pd_ctx *ctx, const void *kv_pages) {
     if (ctx->map_latent_ptr == kv_pages) return PD_OK;
+    ctx->map_latent_ptr = nullptr;
     if (int rc = encode_rows_map(ctx, kv_pages, pd::kLatentRow, ctx->cfg.num_pages * pd::kPageSize, pd::kPageSize, &ctx->tm_latent)) return rc;
+    const cuuint64_t dims[4] = {64, 8, pd::kLatentRow / 64, static_cast<cuuint64_t>(ctx->cfg.num_pages) * 2};
+    const cuuint64_t strides[3] = {pd::kLatentRow * 2, 128, 8 * pd::kLatentRow * 2};
+    const cuuint32_t box[4] = {64, 8, 2, 2}, elem_strides[4] = {1, 1, 1, 1};
+    const CUresult r = ctx->encode(&ctx->tm_latent_pairs, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(kv_pages), dims, strides,
+                                   box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r != CUDA_SUCCESS) {
+        std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+        return PD_ERR_CUDA;
+    }
     ctx->map_latent_ptr = kv_pages;
     return PD_OK;
 }
@@ -1450,8 +1462,8 @@ int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, cons
     p.groups = latent_groups(ctx->cfg.num_q_heads);
     p.heads = latent_group_heads(ctx->cfg.num_q_heads);
     p.a.pdl = ctx->pdl;
-    const cudaError_t err = pd::launch_decode_attn_latent(ctx->tm_latent, ctx->tm_latent_q, p, ctx->num_sms / p.groups * p.groups,
-                                                          static_cast<cudaStream_t>(stream));
+    const cudaError_t err = pd::launch_decode_attn_latent(ctx->tm_latent_pairs, ctx->tm_latent, ctx->tm_latent_q, p,
+                                                          ctx->num_sms / p.groups * p.groups, static_cast<cudaStream_t>(stream));
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent decode launch", err);
     ctx->launches += 2;
     return PD_OK;

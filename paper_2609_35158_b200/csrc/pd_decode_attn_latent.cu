@@ -70,6 +70,13 @@ __device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int3
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar,
+                                            uint64_t l2_policy) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+                 " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(l2_policy) : "memory");
+}
+
 // Half a row's columns per thread: threads 0..15 of the warp get lanes 0..15 from column 0 on, threads 16..31 the same
 // lanes from column K on.
 template <int K>
@@ -193,7 +200,8 @@ __device__ __forceinline__ int reduced_index(int lane) { return K >= 16 ? (lane 
 
 template <int N>
 __global__ void __launch_bounds__(kThreads, 1)
-decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_q, const LatentAttnParams p) {
+decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_rope,
+                          const __grid_constant__ CUtensorMap tm_q, const LatentAttnParams p) {
     constexpr int kSlots = pair_slots<N>();
     constexpr int K = N / 2;                           // heads per softmax thread
     constexpr int kColS = 4 * N;                       // O^T in columns [0, 4 N), then two buffers of S^T
@@ -230,6 +238,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
         mbar_init(bar_drain, 1);
         mbar_init_fence();
         prefetch_tensormap(&tm_kv);
+        prefetch_tensormap(&tm_rope);
         prefetch_tensormap(&tm_q);
     }
     if (warp == 0) {
@@ -275,68 +284,73 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     bool ok = true;
 
     if (busy && warp == 4) {
-        // ================= TMA warp: one box of 64 columns x 16 rows per lane =================
-        const uint64_t policy = l2_policy_evict_first();
-        const int32_t oob_row = p.a.num_pages * kPageSize;  // a box that starts here is all zero fill
-        Walk w = w0;
-        Segment s;
-        int pc = 0, rc = 0, seg = 0;
-        while (ok && next_segment(w, s, pl, p)) {
-            const int32_t *row = p.a.page_table + static_cast<size_t>(s.b) * p.a.MP + s.page0;
-            auto ids = [&](int g) { return g * 32 + lane < s.pages ? __ldg(row + g * 32 + lane) : -1; };
-            int val = ids(0), nval = ids(1);
-            for (int i = 0; i * kTilePages < s.pages && ok; ++i) {
-                const int pg0 = i * kTilePages;
-                if (i > 0 && (pg0 & 31) == 0) {
-                    val = nval;
-                    nval = ids((pg0 >> 5) + 1);
-                }
-                const int pg = (lane >> 1) & (kTilePages - 1);
-                int pid = __shfl_sync(0xffffffffu, val, (pg0 + pg) & 31);
-                int32_t y = oob_row;
-                if (pg0 + pg < s.pages) {
-                    if (pid < 0 || pid >= p.a.num_pages) {
-                        if (lane < 2 * kTilePages && (lane & 1) == 0) latch_status(p.a.status, kDevBadPage, s.b, pid);
-                        pid = 0;
+        // ================= TMA warp: one elected thread =================
+        // A pair of column blocks of a page is one 4-D box, 8 rows x 2 blocks x 2 row groups: shared memory gets [row group][block][8 rows],
+        // in which row groups follow one another at the same distance (2 KB) across pages, as a product's operand needs them.
+        if (elect_one()) {
+            const uint64_t policy = l2_policy_evict_first();
+            const int32_t *row = nullptr;
+            Walk w = w0;
+            Segment s;
+            int pc = 0, rc = 0, seg = 0;
+            auto load_q = [&]() {
+                if (seg > 0) ok = mbar_wait(bar_qempty, (seg - 1) & 1);
+                if (!ok) return;
+                mbar_arrive_expect_tx(bar_qfull, kQBytes);
+#pragma unroll
+                for (int c = 0; c < kRowChunks; ++c) tma_load_3d(q_s + c * (N * 128), &tm_q, c * 64, h0, s.b, bar_qfull);
+                ++seg;
+            };
+            int32_t id[kTilePages];  // the next tile's pages
+            auto load_ids = [&](int pg0) {
+#pragma unroll
+                for (int g = 0; g < kTilePages; ++g) id[g] = pg0 + g < s.pages ? __ldg(row + pg0 + g) : p.a.num_pages;  // (a page of zero fill)
+            };
+            while (ok && next_segment(w, s, pl, p)) {
+                row = p.a.page_table + static_cast<size_t>(s.b) * p.a.MP + s.page0;
+                load_ids(0);
+                const bool first = seg == 0;  // later ones behind their first tile: Q has to wait for the last segment's logits
+                if (first) load_q();
+                for (int i = 0; i * kTilePages < s.pages && ok; ++i) {
+                    int32_t page[kTilePages];
+#pragma unroll
+                    for (int g = 0; g < kTilePages; ++g) {
+                        page[g] = id[g];
+                        if (i * kTilePages + g < s.pages && static_cast<uint32_t>(page[g]) >= static_cast<uint32_t>(p.a.num_pages)) {
+                            latch_status(p.a.status, kDevBadPage, s.b, page[g]);
+                            page[g] = 0;
+                        }
                     }
-                    y = pid * kPageSize;
-                }
-                {
-                    const int slot = rc % kRopeSlots, fill = rc / kRopeSlots;
-                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_rempty + slot * 8, (fill - 1) & 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_rfull + slot * 8, kChunkBytes);
-                    __syncwarp();
-                    if (lane < 2 * kTilePages && (lane & 1) == 0)
-                        tma_load_2d(rope_ring + slot * kChunkBytes + pg * (kPageSize * 128), &tm_kv, kLatentDim, y, bar_rfull + slot * 8, policy);
-                    ++rc;
-                }
-                for (int j = 0; j < kPairs; ++j) {
-                    const int slot = pc % kSlots, fill = pc / kSlots;
-                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_empty + slot * 8, (fill - 1) & 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_full + slot * 8, kPairBytes);
-                    __syncwarp();
-                    if (lane < 2 * kTilePages)
-                        tma_load_2d(ring + slot * kPairBytes + (lane & 1) * kChunkBytes + pg * (kPageSize * 128), &tm_kv,
-                                    (2 * j + (lane & 1)) * 64, y, bar_full + slot * 8, policy);
-                    ++pc;
-                }
-                if (i == 0 && ok) {  // Q behind the first tile: it has to wait for the last segment's logits
-                    if (seg > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_qempty, (seg - 1) & 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_qfull, kQBytes);
-                    __syncwarp();
-                    if (lane < kRowChunks) tma_load_3d(q_s + lane * (N * 128), &tm_q, lane * 64, h0, s.b, bar_qfull);
-                    ++seg;
+                    load_ids((i + 1) * kTilePages);
+                    {
+                        const int slot = rc % kRopeSlots, fill = rc / kRopeSlots;
+                        if (fill > 0) ok = mbar_wait(bar_rempty + slot * 8, (fill - 1) & 1);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(bar_rfull + slot * 8, kChunkBytes);
+#pragma unroll
+                        for (int g = 0; g < kTilePages; ++g)
+                            tma_load_2d(rope_ring + slot * kChunkBytes + g * (kPageSize * 128), &tm_rope, kLatentDim, page[g] * kPageSize, bar_rfull + slot * 8, policy);
+                        ++rc;
+                    }
+                    for (int j = 0; j < kPairs; ++j) {
+                        const int slot = pc % kSlots, fill = pc / kSlots;
+                        if (fill > 0) ok = mbar_wait(bar_empty + slot * 8, (fill - 1) & 1);
+                        if (!ok) break;
+                        mbar_arrive_expect_tx(bar_full + slot * 8, kPairBytes);
+#pragma unroll
+                        for (int g = 0; g < kTilePages; ++g)
+                            tma_load_4d(ring + slot * kPairBytes + g * (2 * kPageSize * 128), &tm_kv, 0, 0, 2 * j, 2 * page[g], bar_full + slot * 8, policy);
+                        ++pc;
+                    }
+                    if (i == 0 && ok && !first) load_q();
                 }
             }
-        }
-        if (!ok) {  // copies in flight have to land before the block's memory goes
-            if (lane == 0) latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
-            for (int i = max(0, pc - kSlots); i < pc; ++i) mbar_wait(bar_full + (i % kSlots) * 8, (i / kSlots) & 1);
-            for (int i = max(0, rc - kRopeSlots); i < rc; ++i) mbar_wait(bar_rfull + (i % kRopeSlots) * 8, (i / kRopeSlots) & 1);
-            if (seg > 0) mbar_wait(bar_qfull, (seg - 1) & 1);
+            if (!ok) {  // copies in flight have to land before the block's memory goes
+                latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
+                for (int i = max(0, pc - kSlots); i < pc; ++i) mbar_wait(bar_full + (i % kSlots) * 8, (i / kSlots) & 1);
+                for (int i = max(0, rc - kRopeSlots); i < rc; ++i) mbar_wait(bar_rfull + (i % kRopeSlots) * 8, (i / kRopeSlots) & 1);
+                if (seg > 0) mbar_wait(bar_qfull, (seg - 1) & 1);
+            }
         }
     } else if (busy && warp == 5) {
         // ================= MMA warp: one elected thread issues every product =================
@@ -344,7 +358,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             constexpr uint32_t idesc_s = umma_idesc_bf16(64, N, false);
             constexpr uint32_t idesc_o = umma_idesc_bf16(128, N, true) | (1u << 15);  // A M-major
             const uint64_t q_desc = umma_smem_desc(q_s, 16, 1024), p_desc = umma_smem_desc(p_s, 16, 1024);
-            const uint64_t ring_k = umma_smem_desc(ring, 16, 1024), ring_m = umma_smem_desc(ring, kChunkBytes, 1024);
+            const uint64_t ring_k = umma_smem_desc(ring, 16, 2048), ring_m = umma_smem_desc(ring, 1024, 2048);
             const uint64_t rope_k = umma_smem_desc(rope_ring, 16, 1024);
             int pv_tile = 0, pv_seg_first = 0;   // next tile whose output product is due; segments begun by them
             // one tile's output products
@@ -356,7 +370,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     const uint64_t a = ring_m + slot * (kPairBytes >> 4);
 #pragma unroll
                     for (int ks = 0; ks < kTile / 16; ++ks)
-                        umma_ss(tm + j * N, a + ks * (2048 >> 4), p_desc + ks * (2048 >> 4), idesc_o, !first || ks != 0);
+                        umma_ss(tm + j * N, a + ks * (4096 >> 4), p_desc + ks * (2048 >> 4), idesc_o, !first || ks != 0);
                     umma_commit(bar_empty + slot * 8);
                 }
                 umma_commit(bar_pv);
@@ -408,7 +422,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
                             for (int ks = 0; ks < 4; ++ks)
-                                umma_ss(d, ring_k + slot * (kPairBytes >> 4) + c * (kChunkBytes >> 4) + ks * 2,
+                                umma_ss(d, ring_k + slot * (kPairBytes >> 4) + c * (1024 >> 4) + ks * 2,
                                         q_desc + ((2 * j + c) * N * 128 >> 4) + ks * 2, idesc_s, true);
                     }
                     if (!ok) break;
@@ -461,7 +475,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     for (int x = tid; x < (last - valid) * (kLatentDim / 8); x += kSoftmaxThreads) {
                         const int r = valid + x / (kLatentDim / 8), c = x % (kLatentDim / 8);
                         const int slot = (t * kPairs + (c >> 4)) % kSlots;
-                        st_shared_zero16(ring + slot * kPairBytes + ((c >> 3) & 1) * kChunkBytes + r * 128 + (c & 7) * 16);
+                        st_shared_zero16(ring + slot * kPairBytes + (r >> 3) * 2048 + ((c >> 3) & 1) * 1024 + (r & 7) * 128 + (c & 7) * 16);
                     }
                 }
                 const bool dead = tok >= valid;
@@ -700,9 +714,9 @@ cudaError_t prepare_decode_attn_latent() {
     return e;
 }
 
-cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_q, const LatentAttnParams &p, int num_ctas,
-                                      cudaStream_t stream) {
-    auto go = [&](auto *k, size_t smem) { return launch_pdl(k, dim3(num_ctas), dim3(kThreads), smem, stream, p.a.pdl != 0, tm_kv, tm_q, p); };
+cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_rope, const CUtensorMap &tm_q, const LatentAttnParams &p,
+                                      int num_ctas, cudaStream_t stream) {
+    auto go = [&](auto *k, size_t smem) { return launch_pdl(k, dim3(num_ctas), dim3(kThreads), smem, stream, p.a.pdl != 0, tm_kv, tm_rope, tm_q, p); };
     const int n = latent_heads_per_cta(p.heads);
     const cudaError_t err = n == 16   ? go(decode_attn_latent_kernel<16>, smem_bytes<16>())
                             : n == 32 ? go(decode_attn_latent_kernel<32>, smem_bytes<32>())

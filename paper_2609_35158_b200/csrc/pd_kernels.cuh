@@ -291,8 +291,8 @@ cudaError_t launch_rope(const RopeParams &p, int append, int max_q_len, int num_
 // shared latent vectors
 int latent_heads_per_cta(int heads);         // heads the kernel is built for that takes `heads` (box height of the Q tensor map)
 cudaError_t prepare_decode_attn_latent();
-cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_q, const LatentAttnParams &p, int num_ctas,
-                                      cudaStream_t stream);
+cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_rope, const CUtensorMap &tm_q, const LatentAttnParams &p,
+                                      int num_ctas, cudaStream_t stream);
 cudaError_t prepare_kv_expand_latent();
 cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_sms,
                                     cudaStream_t stream);
