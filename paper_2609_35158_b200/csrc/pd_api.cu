@@ -1459,6 +1459,7 @@ int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, cons
     p.a.split_pages = split_pages;
     p.a.max_ranges = ctx->max_ranges;
     p.a.min_pages_auto = ctx->min_pages_auto;
+    p.extra = split_pages > 0 ? 0 : pd::kLatentSegmentPages;
     p.groups = latent_groups(ctx->cfg.num_q_heads);
     p.heads = latent_group_heads(ctx->cfg.num_q_heads);
     p.a.pdl = ctx->pdl;

@@ -15,9 +15,10 @@
 // The ring holds pairs of 64-column blocks (128 latents of a tile, 16 KB) and, apart, the rotated parts (8 KB): a tile's
 // pairs are handed back one by one as the output products pass over them, so nearly two tiles are in flight beside 72 KB of Q.
 //
-// Softmax: one thread holds half the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
+// Softmax: one thread holds a quarter of the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
 // tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
-// than 8 log2 units, so a tile needs one vote and no reduction over tokens. P is rounded to bf16 (2^-9 of itself: a second
+// than 32 log2 units (P and the sums keep fp32's exponent range, so 2^32 costs no accuracy): a tile needs one vote and no
+// reduction over tokens. P is rounded to bf16 (2^-9 of itself: a second
 // product for its remainder would make 128 heads a third slower); the sum that normalises the output adds the rounded
 // values, lse takes the unrounded sum.
 //
@@ -40,8 +41,9 @@ constexpr int kPairBytes = 2 * kChunkBytes;
 constexpr int kPairs = 4;                        // pairs of a tile: 512 latents
 constexpr int kRopeSlots = 2;
 constexpr int kRowChunks = kLatentRow / 64;      // 9
-constexpr int kSoftmaxThreads = 128;
+constexpr int kSoftmaxWarps = 8, kSoftmaxThreads = 32 * kSoftmaxWarps;
 constexpr int kThreads = kSoftmaxThreads + 64;   // + TMA warp + MMA warp
+constexpr float kRaise = 32.f;                   // log2 units a logit may exceed its head's reference
 constexpr int kPBytes = kTile * 128;
 constexpr int kSmemLimit = 232448;
 constexpr int kControlBytes = 512;
@@ -82,6 +84,11 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int3
 template <int K>
 __device__ __forceinline__ void tmem_ld_halves(uint32_t taddr, uint32_t (&r)[K]);
 template <>
+__device__ __forceinline__ void tmem_ld_halves<4>(uint32_t taddr, uint32_t (&r)[4]) {
+    asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x4.b32 {%0, %1, %2, %3}, [%4], 4;"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(taddr) : "memory");
+}
+template <>
 __device__ __forceinline__ void tmem_ld_halves<8>(uint32_t taddr, uint32_t (&r)[8]) {
     asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8], 8;"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(taddr) : "memory");
@@ -91,18 +98,6 @@ __device__ __forceinline__ void tmem_ld_halves<16>(uint32_t taddr, uint32_t (&r)
     asm volatile("tcgen05.ld.sync.aligned.16x32bx2.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16], 16;"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
                    "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]) : "r"(taddr) : "memory");
-}
-template <>
-__device__ __forceinline__ void tmem_ld_halves<32>(uint32_t taddr, uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.ld.sync.aligned.16x32bx2.x32.b32 "
-        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, "
-        "%16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32], 32;"
-        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
-        : "r"(taddr) : "memory");
 }
 __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
@@ -119,7 +114,8 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
 }
 
-// How the flattened list of (sequence, page) units is cut: ranges of `size` pages, `per_worker` consecutive ranges per worker.
+// How the work is cut: a sequence is its pages behind `extra` units for what a segment costs beside them (Q, the partial result),
+// and the list of all sequences' units is cut into ranges of `size`, `per_worker` consecutive ranges per worker.
 struct LatentPlan {
     int total, size, ranges, per_worker;
 };
@@ -133,6 +129,40 @@ __device__ __forceinline__ LatentPlan latent_plan(int total, int workers, const 
     pl.per_worker = (pl.ranges + workers - 1) / workers;
     return pl;
 }
+__device__ __forceinline__ int units_of(int pages, int extra) { return pages > 0 ? pages + extra : 0; }
+
+// Exclusive prefix sums of the sequences' units; cum[B] = all. Returns the pages of this thread's sequences.
+__device__ __forceinline__ int scan_units(const LatentAttnParams &p, int32_t *cum, int32_t *warp_sums) {
+    const int tid = threadIdx.x, items = (p.a.B + kThreads - 1) / kThreads;
+    const int begin = min(p.a.B, tid * items), end = min(p.a.B, begin + items);
+    int sum = 0, pages = 0;
+    for (int i = begin; i < end; ++i) {
+        const int L = __ldg(p.a.ctx_lens + i);
+        if (L < 0 || L > p.a.MP * kPageSize) latch_status(p.a.status, kDevBadLength, i, L);
+        const int np = (clamp_len(L, p.a.MP) + kPageSize - 1) / kPageSize;
+        cum[i] = units_of(np, p.extra);  // this thread's own entries, turned into sums below
+        sum += cum[i];
+        pages += np;
+    }
+    int incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int t = __shfl_up_sync(0xffffffffu, incl, o);
+        if ((tid & 31) >= o) incl += t;
+    }
+    if ((tid & 31) == 31) warp_sums[tid >> 5] = incl;
+    __syncthreads();
+    int run = incl - sum;
+    for (int w = 0; w < (tid >> 5); ++w) run += warp_sums[w];
+    for (int i = begin; i < end; ++i) {
+        const int units = cum[i];
+        cum[i] = run;
+        run += units;
+    }
+    if (tid == kThreads - 1) cum[p.a.B] = run;
+    __syncthreads();
+    return pages;
+}
 
 // The segments of one worker, in order; every role of the CTA walks them by itself.
 struct Segment {
@@ -140,51 +170,49 @@ struct Segment {
     bool whole;
 };
 struct Walk {
-    int b, page, np, len, r, r_end, left;
-    bool at_start;
+    int b, at, np, len, r, r_end, left;  // `at`: units of sequence b that lie behind
 };
 __device__ __forceinline__ bool next_segment(Walk &w, Segment &s, const LatentPlan &pl, const LatentAttnParams &p) {
-    if (w.left == 0) {
-        if (++w.r >= w.r_end) return false;
-        w.left = min(pl.size, pl.total - w.r * pl.size);
-        w.at_start = true;
+    for (;;) {
+        if (w.left == 0) {
+            if (++w.r >= w.r_end) return false;
+            w.left = min(pl.size, pl.total - w.r * pl.size);
+        }
+        const int units = units_of(w.np, p.extra);
+        if (w.at >= units) {  // units are left, so a sequence that has some follows
+            ++w.b;
+            w.at = 0;
+            w.len = clamp_len(__ldg(p.a.ctx_lens + w.b), p.a.MP);
+            w.np = (w.len + kPageSize - 1) / kPageSize;
+            continue;
+        }
+        const int take = min(units - w.at, w.left), from = max(w.at - p.extra, 0), to = max(w.at + take - p.extra, 0);
+        w.at += take;
+        w.left -= take;
+        if (from == to) continue;
+        s.b = w.b;
+        s.page0 = from;
+        s.pages = to - from;
+        s.tokens = min(w.len - from * kPageSize, s.pages * kPageSize);
+        s.whole = s.pages == w.np;
+        s.slot = 2 * w.r + (from == 0 ? 1 : 0);  // a range has at most one segment that is cut at its start, and one at its end alone
+        return true;
     }
-    while (w.page >= w.np) {  // units are left, so a sequence with pages follows
-        ++w.b;
-        w.page = 0;
-        w.len = clamp_len(__ldg(p.a.ctx_lens + w.b), p.a.MP);
-        w.np = (w.len + kPageSize - 1) / kPageSize;
-    }
-    s.b = w.b;
-    s.page0 = w.page;
-    s.pages = min(w.np - w.page, w.left);
-    s.tokens = min(w.len - w.page * kPageSize, s.pages * kPageSize);
-    s.whole = s.pages == w.np;
-    s.slot = 2 * w.r + (w.at_start ? 0 : 1);  // a cut segment begins its range or ends it
-    w.page += s.pages;
-    w.left -= s.pages;
-    w.at_start = false;
-    return true;
 }
 
-// Reduces K values per thread over the 16 lanes of a half warp: afterwards lane l (of 16) holds, in v[0..K/16), those of
-// index (l & 15) * (K / 16) + i for K >= 16; for K = 8 lanes l and l ^ 8 both hold index l & 7.
+// Reduces K (at most 16) values per thread over the 16 lanes of a half warp: afterwards v[0] of a lane is that of index lane % K.
 template <int K, bool MAX>
 __device__ __forceinline__ void reduce_half_warp(float (&v)[K], int lane) {
-    int n = K;
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) {
-        if (n > 1 && !(K == 8 && o == 8)) {
-            const int half = n / 2;
+        if (o < K) {  // halve the values: a lane keeps those of its side
             const bool upper = (lane & o) != 0;
 #pragma unroll
-            for (int i = 0; i < K / 2; ++i)
-                if (i < half) {
-                    const float send = upper ? v[i] : v[i + half], keep = upper ? v[i + half] : v[i];
-                    const float got = __shfl_xor_sync(0xffffffffu, send, o);
-                    v[i] = MAX ? fmaxf(keep, got) : keep + got;
-                }
-            n = half;
+            for (int i = 0; i < o; ++i) {
+                const float send = upper ? v[i] : v[i + o], keep = upper ? v[i + o] : v[i];
+                const float got = __shfl_xor_sync(0xffffffffu, send, o);
+                v[i] = MAX ? fmaxf(keep, got) : keep + got;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < K; ++i) {
@@ -194,16 +222,13 @@ __device__ __forceinline__ void reduce_half_warp(float (&v)[K], int lane) {
         }
     }
 }
-// Index of v[0] after reduce_half_warp (lanes with a duplicate excluded by `owner`).
-template <int K>
-__device__ __forceinline__ int reduced_index(int lane) { return K >= 16 ? (lane & 15) * (K / 16) : (lane & 7); }
 
 template <int N>
 __global__ void __launch_bounds__(kThreads, 1)
 decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_rope,
                           const __grid_constant__ CUtensorMap tm_q, const LatentAttnParams p) {
     constexpr int kSlots = pair_slots<N>();
-    constexpr int K = N / 2;                           // heads per softmax thread
+    constexpr int K = N / 4;                           // heads per softmax thread
     constexpr int kColS = 4 * N;                       // O^T in columns [0, 4 N), then two buffers of S^T
     constexpr int kQBytes = kRowChunks * N * 128;
     extern __shared__ uint8_t smem_raw[];
@@ -230,11 +255,11 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
 
     if (tid == 0) {
         for (int i = 0; i < 2 * kSlots + 2 * kRopeSlots + 4; ++i) mbar_init(bar_full + i * 8, 1);  // .. bar_s[2]
-        mbar_init(bar_sempty, 4);
-        mbar_init(bar_sempty + 8, 4);
-        mbar_init(bar_p, 4);
+        mbar_init(bar_sempty, kSoftmaxWarps);
+        mbar_init(bar_sempty + 8, kSoftmaxWarps);
+        mbar_init(bar_p, kSoftmaxWarps);
         mbar_init(bar_pv, 1);
-        mbar_init(bar_o, 4);
+        mbar_init(bar_o, kSoftmaxWarps);
         mbar_init(bar_drain, 1);
         mbar_init_fence();
         prefetch_tensormap(&tm_kv);
@@ -248,9 +273,9 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     grid_dependency_wait();
     launch_dependents();
 
-    // ---- the plan: page sums in the ring's memory, which no copy uses yet
+    // ---- the plan: prefix sums in the ring's memory, which no copy uses yet
     int32_t *cum = reinterpret_cast<int32_t *>(aligned);
-    scan_pages<kThreads>(p.a, cum, warp_sums);
+    const int pages = scan_units(p, cum, warp_sums);
     const LatentPlan pl = latent_plan(cum[p.a.B], workers, p);
     Walk w0{};
     w0.r = worker * pl.per_worker;
@@ -259,16 +284,21 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     if (busy) {
         const Cursor c = locate(cum, p.a.B, 1, static_cast<long long>(w0.r) * pl.size);
         w0.b = c.b;
-        w0.page = c.page;
-        w0.np = c.np;
+        w0.at = c.page;
+        w0.np = c.np - p.extra;
         w0.len = clamp_len(__ldg(p.a.ctx_lens + c.b), p.a.MP);
         w0.left = min(pl.size, pl.total - w0.r * pl.size);
-        w0.at_start = true;
     }
     if (blockIdx.x == 0) {
         for (int i = tid; i <= p.a.B; i += kThreads) p.a.cum_pages[i] = cum[i];
+        int sum = __reduce_add_sync(0xffffffffu, pages);
+        __syncthreads();
+        if (lane == 0) warp_sums[warp] = sum;
+        __syncthreads();
         if (tid == 0) {
-            p.a.plan[0] = pl.total;
+            sum = 0;
+            for (int i = 0; i < kThreads / 32; ++i) sum += warp_sums[i];
+            p.a.plan[0] = sum;
             p.a.plan[1] = 0;
             p.a.plan[2] = 1;
             p.a.plan[3] = pl.ranges;
@@ -283,7 +313,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     const uint32_t tm = tmem_slot;
     bool ok = true;
 
-    if (busy && warp == 4) {
+    if (busy && warp == kSoftmaxWarps) {
         // ================= TMA warp: one elected thread =================
         // A pair of column blocks of a page is one 4-D box, 8 rows x 2 blocks x 2 row groups: shared memory gets [row group][block][8 rows],
         // in which row groups follow one another at the same distance (2 KB) across pages, as a product's operand needs them.
@@ -352,7 +382,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 if (seg > 0) mbar_wait(bar_qfull, (seg - 1) & 1);
             }
         }
-    } else if (busy && warp == 5) {
+    } else if (busy && warp == kSoftmaxWarps + 1) {
         // ================= MMA warp: one elected thread issues every product =================
         if (elect_one()) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(64, N, false);
@@ -445,10 +475,13 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
             mbar_wait(bar_drain, 0);
         }
-    } else if (busy && warp < 4) {
-        // ================= softmax: thread = (token of the tile, half of the heads) =================
-        const int tok = warp * 16 + (lane & 15), hb = lane >> 4;
-        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
+    } else if (busy && warp < kSoftmaxWarps) {
+        // ================= softmax: thread = (token of the tile, a quarter of the heads) =================
+        // Warps w and w + 4 share 16 tokens (the tensor-memory lanes they can reach), warps 0..3 take the first half of the heads.
+        const int wg = warp >> 2, wq = warp & 3;
+        const int tok = wq * 16 + (lane & 15);
+        const int hq = 2 * wg + (lane >> 4), hb = hq * K;  // first head of this thread, within the group
+        const uint32_t lane_base = static_cast<uint32_t>(wq * 32) << 16;
         Walk w = w0;
         Segment s;
         int t = 0;
@@ -462,7 +495,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 if (!ok) break;
                 tc_fence_after_sync();
                 uint32_t sreg[K];
-                tmem_ld_halves<K>(tm + lane_base + kColS + (t & 1) * N, sreg);
+                tmem_ld_halves<K>(tm + lane_base + kColS + (t & 1) * N + wg * 2 * K, sreg);
                 tmem_wait_ld();
                 tc_fence_before_sync();
                 __syncwarp();
@@ -479,20 +512,17 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     }
                 }
                 const bool dead = tok >= valid;
-                float x[K];
-                // the reference of every head of this thread: the largest logit over all tokens of the tile
+                // the largest logit of this thread's heads over all tokens of the tile
                 auto tile_max = [&](float (&top)[K]) {
                     float v[K];
 #pragma unroll
                     for (int k = 0; k < K; ++k) v[k] = dead ? -INFINITY : __uint_as_float(sreg[k]) * p.a.scale_log2;
                     reduce_half_warp<K, true>(v, lane);
-                    const int at = reduced_index<K>(lane);
-#pragma unroll
-                    for (int k = 0; k < (K >= 16 ? K / 16 : 1); ++k) scratch[warp * 64 + hb * K + at + k] = v[k];
+                    scratch[wq * 64 + hb + lane % K] = v[0];
                     softmax_sync();
 #pragma unroll
                     for (int k = 0; k < K; ++k)
-                        top[k] = fmaxf(fmaxf(scratch[hb * K + k], scratch[64 + hb * K + k]), fmaxf(scratch[128 + hb * K + k], scratch[192 + hb * K + k]));
+                        top[k] = fmaxf(fmaxf(scratch[hb + k], scratch[64 + hb + k]), fmaxf(scratch[128 + hb + k], scratch[192 + hb + k]));
                     softmax_sync();
                 };
                 if (i == 0) {
@@ -500,15 +530,22 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
 #pragma unroll
                     for (int k = 0; k < K; ++k) m[k] = fmaxf(m[k], -1e30f);
                 }
-                float over = -INFINITY;
+                float x[K], e[K], over = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
                     x[k] = dead ? -INFINITY : fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]);
                     over = fmaxf(over, x[k]);
+                    e[k] = fast_exp2(x[k]);
                 }
+                uint32_t pk[K / 2];
+                auto pack = [&]() {
+#pragma unroll
+                    for (int k = 0; k < K; k += 2) pk[k / 2] = pack_bf16x2(e[k], e[k + 1]);
+                };
+                pack();
                 if (i > 0) {
-                    const bool raise = softmax_any(over > kRescaleSlack);
                     ok = mbar_wait(bar_pv, (t - 1) & 1);  // P's buffer is free and O^T holds every tile before this one
+                    const bool raise = softmax_any(over > kRaise);
                     if (!ok) break;
                     if (raise) {
                         tc_fence_after_sync();
@@ -517,18 +554,18 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
 #pragma unroll
                         for (int k = 0; k < K; ++k) {
                             float alpha = 1.f;
-                            if (top[k] - m[k] > kRescaleSlack) {
+                            if (top[k] - m[k] > kRaise) {
                                 alpha = fast_exp2(m[k] - top[k]);
-                                x[k] += m[k] - top[k];
+                                e[k] = fast_exp2(x[k] + (m[k] - top[k]));
                                 m[k] = top[k];
                             }
                             l[k] *= alpha;
                             lr[k] *= alpha;
-                            if ((lane & 15) == 0 && warp == 0) scratch[hb * K + k] = alpha;
+                            if ((lane & 15) == 0 && wq == 0) scratch[hb + k] = alpha;
                         }
                         softmax_sync();
 #pragma unroll 1
-                        for (int c = 0; c < 4 * N; c += 16) {
+                        for (int c = wg * 2 * N; c < (wg + 1) * 2 * N; c += 16) {
                             uint32_t o[16];
                             tmem_ld16(tm + lane_base + c, o);
                             tmem_wait_ld();
@@ -538,28 +575,31 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                         }
                         tmem_wait_st();
                         softmax_sync();
+                        pack();
                     }
                 }
-                uint32_t pk[K / 2];
+                if constexpr (K >= 8) {
 #pragma unroll
-                for (int k = 0; k < K; k += 2) {
-                    const float e0 = fast_exp2(x[k]), e1 = fast_exp2(x[k + 1]);
-                    pk[k / 2] = pack_bf16x2(e0, e1);
-                    l[k] += e0;
-                    l[k + 1] += e1;
-                    lr[k] += __uint_as_float(pk[k / 2] << 16);
-                    lr[k + 1] += __uint_as_float(pk[k / 2] & 0xffff0000u);
-                }
-#pragma unroll
-                for (int c = 0; c < K / 8; ++c) {
-                    const uint32_t a = p_s + sw128_offset(tok, hb * (K / 8) + c);
-                    asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(pk[4 * c]), "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]),
-                                 "r"(pk[4 * c + 3]) : "memory");
+                    for (int c = 0; c < K / 8; ++c) {
+                        const uint32_t a = p_s + sw128_offset(tok, hb / 8 + c);
+                        asm volatile("st.shared.v4.u32 [%0], {%1,%2,%3,%4};" ::"r"(a), "r"(pk[4 * c]), "r"(pk[4 * c + 1]), "r"(pk[4 * c + 2]),
+                                     "r"(pk[4 * c + 3]) : "memory");
+                    }
+                } else {
+                    const uint32_t a = p_s + sw128_offset(tok, hb / 8) + (hb % 8) * 2;
+                    asm volatile("st.shared.v2.u32 [%0], {%1,%2};" ::"r"(a), "r"(pk[0]), "r"(pk[1]) : "memory");
                 }
                 fence_proxy_async();
                 tc_fence_before_sync();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_p);
+#pragma unroll
+                for (int k = 0; k < K; k += 2) {
+                    l[k] += e[k];
+                    l[k + 1] += e[k + 1];
+                    lr[k] += __uint_as_float(pk[k / 2] << 16);
+                    lr[k + 1] += __uint_as_float(pk[k / 2] & 0xffff0000u);
+                }
             }
             if (!ok) break;
             // ---- the segment's end
@@ -567,18 +607,14 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             if (!ok) break;
             tc_fence_after_sync();
             float *sum_l = scratch, *sum_lr = scratch + 256, *ref = scratch + 512, *inv = scratch + 576;
-            if (warp == 0 && (lane & 15) == 0) {
+            if (wq == 0 && (lane & 15) == 0) {
 #pragma unroll
-                for (int k = 0; k < K; ++k) ref[hb * K + k] = m[k];
+                for (int k = 0; k < K; ++k) ref[hb + k] = m[k];
             }
             reduce_half_warp<K, false>(l, lane);
             reduce_half_warp<K, false>(lr, lane);
-            const int at = reduced_index<K>(lane);
-#pragma unroll
-            for (int k = 0; k < (K >= 16 ? K / 16 : 1); ++k) {
-                sum_l[warp * 64 + hb * K + at + k] = l[k];
-                sum_lr[warp * 64 + hb * K + at + k] = lr[k];
-            }
+            sum_l[wq * 64 + hb + lane % K] = l[0];
+            sum_lr[wq * 64 + hb + lane % K] = lr[0];
             softmax_sync();
             if (tid < nh) {
                 const float sl = (sum_l[tid] + sum_l[64 + tid]) + (sum_l[128 + tid] + sum_l[192 + tid]);
@@ -590,10 +626,10 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     p.part_ml[static_cast<size_t>(s.slot) * p.a.Hq + h0 + tid] = make_float4(ref[tid], sl, slr, 0.f);
                 }
             }
-            softmax_sync();
+            if (s.whole) softmax_sync();
 #pragma unroll 1
-            for (int j = 0; j < 4; ++j) {
-                const int latent = j * 128 + tid;
+            for (int j = 2 * wg; j < 2 * wg + 2; ++j) {
+                const int latent = j * 128 + wq * 32 + lane;
 #pragma unroll 1
                 for (int c = 0; c < N; c += 16) {
                     uint32_t o[16];
@@ -624,77 +660,101 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     if (warp == 0) tmem_dealloc(tm, kTmemCols);
 }
 
-// Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A group of
-// 128 threads holds 4 values each of a row; PARTS groups share a row's partials (few rows, many partials), or
-// each takes rows of its own.
-constexpr int kMergeGroups = 4;
-template <int PARTS>
-__global__ void __launch_bounds__(128 * kMergeGroups) latent_merge_kernel(const LatentAttnParams p) {
-    __shared__ float4 part_o[kMergeGroups][128];
-    __shared__ float part_m[kMergeGroups], part_l[kMergeGroups], part_lr[kMergeGroups];
+// The running sums of a merge: what a thread holds of a row and how a partial joins it.
+template <int VECS>
+struct Joined {
+    float m = -INFINITY, l = 0.f, lr = 0.f;
+    float4 o[VECS];
+    __device__ __forceinline__ Joined() {
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    __device__ __forceinline__ void raise(float top) {
+        const float keep = m == top ? 1.f : fast_exp2(m - top);
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) o[v].x *= keep, o[v].y *= keep, o[v].z *= keep, o[v].w *= keep;
+        l *= keep, lr *= keep;
+        m = top;
+    }
+    __device__ __forceinline__ void join(float pm, float pl, float plr, const float4 (&x)[VECS]) {
+        const float a = fast_exp2(pm - m);
+#pragma unroll
+        for (int v = 0; v < VECS; ++v)
+            o[v].x = fmaf(a, x[v].x, o[v].x), o[v].y = fmaf(a, x[v].y, o[v].y), o[v].z = fmaf(a, x[v].z, o[v].z), o[v].w = fmaf(a, x[v].w, o[v].w);
+        l = fmaf(a, pl, l);
+        lr = fmaf(a, plr, lr);
+    }
+};
+
+// Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A row is held by
+// LANES threads, 512 / LANES values each. Where rows are few and partials many, PARTS sets of threads share a row's partials;
+// where rows are many, a warp takes a row. (Measured, 64 sequences of 2K-16K with 128 heads: 8 us with a warp per row, 13
+// with four sets of 128 threads; 4 sequences of 32K-64K with 32 heads: 8 and 5.)
+template <int LANES, int PARTS>
+__global__ void __launch_bounds__(LANES == 32 ? 256 : LANES * PARTS) latent_merge_kernel(const LatentAttnParams p) {
+    constexpr int VECS = kLatentDim / 4 / LANES, U = 4;  // U partials in flight
+    __shared__ float4 part_o[PARTS > 1 ? PARTS : 1][LANES];
+    __shared__ float part_m[PARTS], part_l[PARTS], part_lr[PARTS];
+    const int set = threadIdx.x / LANES, lane = threadIdx.x % LANES, part = PARTS > 1 ? set : 0;
     grid_dependency_wait();
     launch_dependents();
-    const int b = blockIdx.y, g = threadIdx.x >> 7, col = threadIdx.x & 127;
-    const int c0 = p.a.cum_pages[b], c1 = p.a.cum_pages[b + 1], size = p.a.plan[kPlanHeaderWords + 2];
-    const int r0 = c0 / size, r1 = (c1 - 1) / size;
-    if (c0 != c1 && r0 == r1) return;  // written by the split kernel
-    const int first = 2 * r0 + (c0 > r0 * size ? 1 : 0);
-    auto slot = [&](int r) { return static_cast<size_t>(r == r0 ? first : 2 * r); };
-    const int h_end = min(static_cast<int>(blockIdx.x + 1) * p.merge_heads, p.a.Hq);
-    for (int h = blockIdx.x * p.merge_heads + g / PARTS; h < h_end; h += kMergeGroups / PARTS) {
-        const size_t row_out = static_cast<size_t>(b) * p.a.Hq + h;
-        __nv_bfloat16 *out = p.a.out + row_out * kLatentDim + col * 4;
+    const int size = p.a.plan[kPlanHeaderWords + 2], rows = p.a.B * p.a.Hq;
+    const int per_block = PARTS > 1 ? 1 : blockDim.x / LANES;
+    for (int row = blockIdx.x * per_block + (PARTS > 1 ? 0 : set); row < rows; row += gridDim.x * per_block) {
+        const int b = row / p.a.Hq, h = row - b * p.a.Hq;
+        const int c0 = p.a.cum_pages[b], c1 = p.a.cum_pages[b + 1];
+        uint2 *out = reinterpret_cast<uint2 *>(p.a.out + static_cast<size_t>(row) * kLatentDim);
         if (c0 == c1) {
-            if (g % PARTS == 0) *reinterpret_cast<uint2 *>(out) = make_uint2(0u, 0u);
-            if (g % PARTS == 0 && col == 0 && p.a.lse != nullptr) p.a.lse[row_out] = -INFINITY;
+#pragma unroll
+            for (int v = 0; v < VECS; ++v)
+                if (part == 0) out[v * LANES + lane] = make_uint2(0u, 0u);
+            if (part == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = -INFINITY;
             continue;
         }
-        float m = -INFINITY, l = 0.f, lr = 0.f;
-        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-        auto join = [&](float pm, float pl, float plr, const float4 &v) {
-            const float a = fast_exp2(pm - m);
-            o.x = fmaf(a, v.x, o.x), o.y = fmaf(a, v.y, o.y), o.z = fmaf(a, v.z, o.z), o.w = fmaf(a, v.w, o.w);
-            l = fmaf(a, pl, l);
-            lr = fmaf(a, plr, lr);
-        };
-        auto raise = [&](float top) {
-            const float keep = m == top ? 1.f : fast_exp2(m - top);
-            o.x *= keep, o.y *= keep, o.z *= keep, o.w *= keep, l *= keep, lr *= keep;
-            m = top;
-        };
-        constexpr int U = 4;  // partials in flight
-        for (int r = r0 + g % PARTS; r <= r1; r += PARTS * U) {
-            float4 v[U], ml[U];
+        const int r0 = (c0 + p.extra) / size, r1 = (c1 - 1) / size;  // ranges of its first and last page
+        if (r0 == r1) continue;  // written by the split kernel
+        Joined<VECS> sum;
+        for (int r = r0 + part; r <= r1; r += PARTS * U) {
+            float4 x[U][VECS], ml[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int x = r + u * PARTS;
-                if (x <= r1) {
-                    const size_t row = slot(x) * p.a.Hq + h;
-                    ml[u] = p.part_ml[row];
-                    v[u] = reinterpret_cast<const float4 *>(p.a.part_o + row * kLatentDim)[col];
+                const int y = r + u * PARTS;
+                if (y <= r1) {
+                    const size_t at = static_cast<size_t>(y == r0 ? 2 * y + 1 : 2 * y) * p.a.Hq + h;
+                    ml[u] = p.part_ml[at];
+#pragma unroll
+                    for (int v = 0; v < VECS; ++v) x[u][v] = reinterpret_cast<const float4 *>(p.a.part_o + at * kLatentDim)[v * LANES + lane];
                 } else {
                     ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-                    v[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int v = 0; v < VECS; ++v) x[u][v] = make_float4(0.f, 0.f, 0.f, 0.f);
                 }
             }
-            raise(fmaxf(fmaxf(m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)));  // finite: ml[0] is a partial's reference
+            sum.raise(fmaxf(fmaxf(sum.m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)));  // finite: ml[0] is a partial's reference
 #pragma unroll
-            for (int u = 0; u < U; ++u) join(ml[u].x, ml[u].y, ml[u].z, v[u]);
+            for (int u = 0; u < U; ++u) sum.join(ml[u].x, ml[u].y, ml[u].z, x[u]);
         }
-        if (PARTS > 1) {
-            part_o[g][col] = o;
-            if (col == 0) part_m[g] = m, part_l[g] = l, part_lr[g] = lr;
+        if constexpr (PARTS > 1) {
+            static_assert(VECS == 1, "one vector per thread");
+            part_o[set][lane] = sum.o[0];
+            if (lane == 0) part_m[set] = sum.m, part_l[set] = sum.l, part_lr[set] = sum.lr;
             __syncthreads();
-            if (g != 0) return;  // (one row per block)
+            if (part == 0) {  // it has a partial, so its reference is finite
 #pragma unroll
-            for (int i = 1; i < PARTS; ++i) {
-                raise(fmaxf(m, part_m[i]));  // the first group has a partial
-                join(part_m[i], part_l[i], part_lr[i], part_o[i][col]);
+                for (int i = 1; i < PARTS; ++i) {
+                    const float4 x[1] = {part_o[i][lane]};
+                    sum.raise(fmaxf(sum.m, part_m[i]));
+                    sum.join(part_m[i], part_l[i], part_lr[i], x);
+                }
             }
+            __syncthreads();
+            if (part != 0) continue;
         }
-        const float inv = 1.f / lr;
-        *reinterpret_cast<uint2 *>(out) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
-        if (col == 0 && p.a.lse != nullptr) p.a.lse[row_out] = (m + log2f(l)) * kLn2;
+        const float inv = 1.f / sum.lr;
+#pragma unroll
+        for (int v = 0; v < VECS; ++v)
+            out[v * LANES + lane] = make_uint2(pack_bf16x2(sum.o[v].x * inv, sum.o[v].y * inv), pack_bf16x2(sum.o[v].z * inv, sum.o[v].w * inv));
+        if (lane == 0 && p.a.lse != nullptr) p.a.lse[row] = (sum.m + log2f(sum.l)) * kLn2;
     }
 }
 
@@ -722,15 +782,9 @@ cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMa
                             : n == 32 ? go(decode_attn_latent_kernel<32>, smem_bytes<32>())
                                       : go(decode_attn_latent_kernel<64>, smem_bytes<64>());
     if (err != cudaSuccess) return err;
-    // Few rows are cut into many partials each: a block per row, its groups side by side. Otherwise a group per row, and as
-    // many rows per block as leave a few thousand blocks (most of which find nothing to do on large batches).
-    LatentAttnParams q = p;
-    const long long rows = static_cast<long long>(p.a.B) * p.a.Hq;
-    const bool few = rows <= 2048;
-    q.merge_heads = few ? 1 : kMergeGroups * static_cast<int>((rows + 16383) / 16384);
-    const dim3 grid((p.a.Hq + q.merge_heads - 1) / q.merge_heads, p.a.B);
-    return few ? launch_pdl(latent_merge_kernel<kMergeGroups>, grid, dim3(128 * kMergeGroups), 0, stream, p.a.pdl != 0, q)
-               : launch_pdl(latent_merge_kernel<1>, grid, dim3(128 * kMergeGroups), 0, stream, p.a.pdl != 0, q);
+    const int rows = p.a.B * p.a.Hq, warps = (rows + 7) / 8, most = num_ctas * 16;
+    return rows <= 4 * num_ctas ? launch_pdl(latent_merge_kernel<128, 4>, dim3(rows), dim3(512), 0, stream, p.a.pdl != 0, p)
+                                : launch_pdl(latent_merge_kernel<32, 1>, dim3(warps < most ? warps : most), dim3(256), 0, stream, p.a.pdl != 0, p);
 }
 
 }  // namespace pd

@@ -194,12 +194,13 @@ struct RopeParams {
 constexpr int kLatentDim = 512, kLatentRope = 64, kLatentRow = kLatentDim + kLatentRope;
 constexpr int kLatentHead = 128;             // width of a head's expanded K (beside the rotated part) and V
 constexpr int kLatentMaxHeads = 128;
+constexpr int kLatentSegmentPages = 8;       // what a segment of the decode kernel costs beside its pages, in pages
 
 struct LatentAttnParams {
     AttnParams a;                // q [B][Hq][576], out [B][Hq][512], part_o [slots][Hq][512]
     float4 *part_ml;             // [slots][Hq] reference (log2 units), sum, sum of the rounded weights
     int32_t groups, heads;       // groups of at most 64 heads, heads per group
-    int32_t merge_heads;         // heads per block of the merge kernel (set at its launch)
+    int32_t extra;               // units a sequence counts in the plan beside its pages
 };
 
 // New tokens' rows into the pages: latent normalised, key part and queries rotated.
