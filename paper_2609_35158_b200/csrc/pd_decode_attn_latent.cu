@@ -485,14 +485,14 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
         Walk w = w0;
         Segment s;
         int t = 0;
-        while (ok && next_segment(w, s, pl, p)) {
+        // (a warp whose wait ran out goes on without waiting: the others must not be left alone at the barriers they share)
+        while (next_segment(w, s, pl, p)) {
             float m[K], l[K], lr[K];
 #pragma unroll
             for (int i = 0; i < K; ++i) m[i] = l[i] = lr[i] = 0.f;
             const int tiles = (s.pages + kTilePages - 1) / kTilePages;
-            for (int i = 0; i < tiles && ok; ++i, ++t) {
-                ok = mbar_wait(bar_s + (t & 1) * 8, (t >> 1) & 1);
-                if (!ok) break;
+            for (int i = 0; i < tiles; ++i, ++t) {
+                ok = ok && mbar_wait(bar_s + (t & 1) * 8, (t >> 1) & 1);
                 tc_fence_after_sync();
                 uint32_t sreg[K];
                 tmem_ld_halves<K>(tm + lane_base + kColS + (t & 1) * N + wg * 2 * K, sreg);
@@ -544,9 +544,8 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 };
                 pack();
                 if (i > 0) {
-                    ok = mbar_wait(bar_pv, (t - 1) & 1);  // P's buffer is free and O^T holds every tile before this one
+                    ok = ok && mbar_wait(bar_pv, (t - 1) & 1);  // P's buffer is free and O^T holds every tile before this one
                     const bool raise = softmax_any(over > kRaise);
-                    if (!ok) break;
                     if (raise) {
                         tc_fence_after_sync();
                         float top[K];
@@ -601,10 +600,8 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     lr[k + 1] += __uint_as_float(pk[k / 2] & 0xffff0000u);
                 }
             }
-            if (!ok) break;
             // ---- the segment's end
-            ok = mbar_wait(bar_pv, (t - 1) & 1);
-            if (!ok) break;
+            ok = ok && mbar_wait(bar_pv, (t - 1) & 1);
             tc_fence_after_sync();
             float *sum_l = scratch, *sum_lr = scratch + 256, *ref = scratch + 512, *inv = scratch + 576;
             if (wq == 0 && (lane & 15) == 0) {

@@ -56,11 +56,6 @@ __device__ __forceinline__ void step(Walk &w, const LatentExpandParams &p) {
     } while (w.s.tiles == 0);
 }
 
-__device__ __forceinline__ void store32(void *dst, const uint32_t (&v)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(dst), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
-                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
-}
-
 __global__ void __launch_bounds__(kThreads, 1)
 kv_expand_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_constant__ CUtensorMap tm_w, const LatentExpandParams p) {
     extern __shared__ uint8_t smem_raw[];
