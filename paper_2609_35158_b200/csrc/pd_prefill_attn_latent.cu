@@ -26,7 +26,7 @@ namespace {
 
 constexpr float kLn2f = 0.6931471805599453f;
 constexpr float kRaise = 32.f;                  // log2 units a logit may exceed its row's reference
-constexpr int kRows = 128;                      // query rows per tile (MMA M), two softmax threads each
+constexpr int kRows = 128;                      // query rows per tile (MMA M), one softmax thread each
 constexpr int kTiles = 2;
 constexpr int kBlock = 128;                     // context tokens per step
 constexpr int kBlockPages = kBlock / kPageSize;
@@ -35,15 +35,13 @@ constexpr int kPiece = 16384;                   // 128 rows of 64 columns, or 64
 constexpr int kKPieces = kQDim / 64;            // per block
 constexpr int kKSlots = 5, kVSlots = 3;
 constexpr int kParts = 2, kPart = kBlock / kParts;  // P and the O product go in two parts of 64 tokens
-constexpr int kTileThreads = kParts * kRows;    // a thread per row and part
-constexpr int kSoftmaxWarps = kTiles * kTileThreads / 32;
+constexpr int kSoftmaxWarps = kTiles * kRows / 32;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);  // + MMA warp, K loader, V loader, one spare
 constexpr int kQTileBytes = kKPieces * kPiece;
 constexpr int kTmemCols = 512;
 constexpr int kColS = 0, kColO = 256;
-constexpr int kNumBars = 2 * kKSlots + 2 * kVSlots + 2 + 4 + 2 + 1 + 2;
-constexpr int kExchangeBytes = kTiles * kRows * 4;  // one value per row, between its two threads
-constexpr size_t kSmemBytes = 1024 + kTiles * kQTileBytes + (kKSlots + kVSlots) * kPiece + kNumBars * 8 + kExchangeBytes;
+constexpr int kNumBars = 2 * kKSlots + 2 * kVSlots + 2 + 4 + 4 + 1 + 2;
+constexpr size_t kSmemBytes = 1024 + kTiles * kQTileBytes + (kKSlots + kVSlots) * kPiece + kNumBars * 8;
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -74,14 +72,6 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]),
           "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
-}
-
-__device__ __forceinline__ void pair_sync(int id) { asm volatile("barrier.cta.sync %0, 64;" ::"r"(id) : "memory"); }
-__device__ __forceinline__ bool pair_any(int id, bool v) {
-    uint32_t r;
-    asm volatile("{\n.reg .pred p, q;\nsetp.ne.u32 p, %2, 0;\nbarrier.cta.red.or.pred q, %1, 64, p;\nselp.u32 %0, 1, 0, q;\n}"
-                 : "=r"(r) : "r"(id), "r"(static_cast<uint32_t>(v)) : "memory");
-    return r != 0;
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -122,15 +112,14 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
     const uint32_t bar_v = bar_kfree + kKSlots * 8, bar_vfree = bar_v + kVSlots * 8;
     const uint32_t bar_s = bar_vfree + kVSlots * 8;  // [2] S_t of the current block complete (and every product before it)
     const uint32_t bar_p = bar_s + 16;               // [2 tiles][2 parts] that part of P_t is written (4 warps each)
-    const uint32_t bar_o = bar_p + 32;               // [2] last O_t product complete
-    const uint32_t bar_drain = bar_o + 16;
-    const uint32_t bar_q = bar_drain + 8;            // [2] tile t's queries are in shared memory (8 warps each)
-    float *exchange = reinterpret_cast<float *>(bars + kNumBars);
+    const uint32_t bar_o = bar_p + 32;               // [2] last O_t product complete; [2] first part's O_t product of the block complete
+    const uint32_t bar_drain = bar_o + 32;
+    const uint32_t bar_q = bar_drain + 8;            // [2] tile t's queries are in shared memory (4 warps each)
 
     if (tid == 0) {
         for (int i = 0; i < kNumBars; ++i) {
             const uint32_t bar = bar_k + i * 8;
-            mbar_init(bar, bar >= bar_q ? kTileThreads / 32 : bar >= bar_p && bar < bar_o ? kRows / 32 : 1);
+            mbar_init(bar, bar >= bar_q || (bar >= bar_p && bar < bar_o) ? kRows / 32 : 1);
         }
         mbar_init_fence();
         prefetch_tensormap(&tm_k);
@@ -141,9 +130,9 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
         tmem_relinquish_alloc_permit();
     }
-    const int tile = tid / kTileThreads, part = (tid / kRows) % kParts, row = tid & (kRows - 1);  // of a softmax thread
+    const int tile = tid / kRows, row = tid & (kRows - 1);  // of a softmax thread
     const int tok = tile * kRows + row;                 // token index inside the CTA
-    const bool row_valid = tid < kTiles * kTileThreads && tok < n_tok;
+    const bool row_valid = tid < kTiles * kRows && tok < n_tok;
     const int my_pos = pos0 + min(tok, n_tok - 1);      // padding rows mirror the last token
     tc_fence_before_sync();
     __syncthreads();
@@ -186,7 +175,8 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     umma_ts(tm + kColO + t * kLatentHead, tm + kColS + t * kBlock + (part * (kPart / 16) + ks) * 8,
                             v_desc + slot * (kPiece >> 4) + ks * (2048 >> 4), idesc_o, (j | part | ks) != 0);
                 if (release) umma_commit(bar_vfree + slot * 8);
-                if (part == kParts - 1 && last) umma_commit(bar_o + t * 8);
+                if (part == 0) umma_commit(bar_o + (2 + t) * 8);  // lets a row thread rescale O_t between the two parts (rare)
+                else if (last) umma_commit(bar_o + t * 8);
             };
             ok = mbar_wait(bar_q, 0);
             if (ok) issue_s(0, 0, true, nb1 == 0);
@@ -271,31 +261,19 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait((is_k ? bar_k : bar_v) + (i % slots) * 8, (i / slots) & 1);
         }
     } else if (warp < kSoftmaxWarps && (tile == 0 || nb1 > 0)) {
-        // ================= softmax: eight warps per tile, a thread per row and part of the block =================
-        // A row's two threads share its reference m (O_t is one accumulator); the warps they sit in meet at a barrier of 64 threads.
+        // ================= softmax warpgroups: warpgroup t owns tile t, one thread per query row =================
         const int t = tile, my_nb = t == 0 ? nb0 : nb1;
-        const int pair = 1 + t * 4 + (warp & 3);
         const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
         const uint32_t s_buf = tm + lane_base + kColS + t * kBlock;
         const uint32_t o_buf = tm + lane_base + kColO + t * kLatentHead;
-        float *slot = exchange + t * kRows + row;
-        // combines the values of a row's two threads; both get the result
-        auto both = [&](float v, auto op) {
-            if (part == 1) *slot = v;
-            pair_sync(pair);
-            if (part == 0) *slot = v = op(v, *slot);
-            pair_sync(pair);
-            return part == 1 ? *slot : v;
-        };
-        auto larger = [](float a, float b) { return fmaxf(a, b); };
         // ---- the tile's queries: neighbouring threads copy neighbouring 16 bytes, all in flight at once
         {
-            constexpr int kChunks = kQDim / 8;  // 128 rows x 24 pieces
+            constexpr int kChunks = kQDim / 8;  // 128 rows x 24 pieces over 128 threads
             const __nv_bfloat16 *src = p.q + (static_cast<size_t>(q0 + cta_start + tile * kRows) * p.Hq + head) * kQDim;
             const int rows = min(kRows, n_tok - tile * kRows);
 #pragma unroll
-            for (int i = 0; i < kRows * kChunks / kTileThreads; ++i) {
-                const int x = i * kTileThreads + part * kRows + row, r = x / kChunks, c = x - r * kChunks;
+            for (int i = 0; i < kChunks; ++i) {
+                const int x = i * kRows + row, r = x / kChunks, c = x - r * kChunks;
                 const uint32_t a = q_s + tile * kQTileBytes + (c >> 3) * kPiece + sw128_offset(r, c & 7);
                 cp_async16(a, src + static_cast<size_t>(min(r, rows - 1)) * p.Hq * kQDim + c * 8, r < rows ? 16 : 0);  // rows past the last are zeros
             }
@@ -305,128 +283,130 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             if (lane == 0) mbar_arrive(bar_q + t * 8);
         }
         float m_run = 0.f, l_run = 0.f;
-        // (a warp whose wait ran out goes on without waiting: its partner must not be left alone at their barrier)
-        for (int j = 0; j < my_nb; ++j) {
-            ok = ok && mbar_wait(bar_s + t * 8, j & 1);
+        for (int j = 0; j < my_nb && ok; ++j) {
+            ok = mbar_wait(bar_s + t * 8, j & 1);
             tc_fence_after_sync();
-            const int t0 = j * kBlock + part * kPart;          // first token of this thread's part
-            const int visible = my_pos - t0 + 1;               // logits of the part the row may see
-            // V rows past the context inside the last page may hold NaN; 0 * NaN is NaN, so the warps whose products of
-            // this block come first clear them
+            if (!ok) break;
+            const int t0 = j * kBlock;
+            const bool masked = t0 + kBlock - 1 > my_pos;  // the block reaches past this row's position
+            // V rows past the context inside the last page may hold NaN; 0 * NaN is NaN, so the warpgroup whose products of
+            // this block come first clears them
             const int valid_rows = L - t0;
-            if (valid_rows > 0 && valid_rows < kPart && (t == 0 || j >= nb0)) {
-                const int i = j * kParts + part, last = (valid_rows + kPageSize - 1) / kPageSize * kPageSize;
-                ok = ok && mbar_wait(bar_v + (i % kVSlots) * 8, (i / kVSlots) & 1);  // the part must have landed
-                for (int x = row; x < (last - valid_rows) * (kLatentHead / 8); x += kRows) {
-                    const int r = valid_rows + x / (kLatentHead / 8), c = x % (kLatentHead / 8);
-                    st_shared_zero16(v_ring + (i % kVSlots) * kPiece + (c >> 3) * (kPart * 128) + r * 128 + (c & 7) * 16);
+            if (valid_rows < kBlock && (t == 0 || j >= nb0)) {
+                const int last = min(kBlock, (valid_rows + kPageSize - 1) / kPageSize * kPageSize);
+                for (int part = 0; part < kParts; ++part) {  // the parts must have landed
+                    const int i = j * kParts + part;
+                    ok = ok && mbar_wait(bar_v + (i % kVSlots) * 8, (i / kVSlots) & 1);
+                }
+                if (!ok) break;
+                for (int i = row; i < (last - valid_rows) * (kLatentHead / 8); i += kRows) {
+                    const int r = valid_rows + i / (kLatentHead / 8), c = i % (kLatentHead / 8);
+                    const int slot = (j * kParts + r / kPart) % kVSlots;
+                    st_shared_zero16(v_ring + slot * kPiece + (c >> 3) * (kPart * 128) + (r % kPart) * 128 + (c & 7) * 16);
                 }
                 fence_proxy_async();
             }
-            auto run = [&](auto masked_c) {
-                constexpr bool kMasked = decltype(masked_c)::value;
-                // the part's logits, `n` columns from `c0`; invisible ones as -inf
-                auto load = [&](int c0, uint32_t (&v)[32]) { tmem_ld32(s_buf + part * kPart + c0, v); };
-                auto hide = [&](int c0, uint32_t (&v)[32]) {
-                    if (kMasked) {
+            auto load = [&](int part, uint32_t (&v)[kPart]) {
 #pragma unroll
-                        for (int c = 0; c < 32; ++c)
-                            if (c0 + c >= visible) v[c] = 0xff800000u;
-                    }
-                };
-                uint32_t pk[kPart / 2];
-                float sum = 0.f;
-                // x = s * scale - m, P = 2^x in bf16, the unrounded sum; returns the largest x
-                auto weigh = [&]() {
-                    const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), nm2 = make_float2(-m_run, -m_run);
-                    float xm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-                    float2 a[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
-                    uint32_t v[2][32];
-                    load(0, v[0]);
-                    tmem_wait_ld();
-                    load(32, v[1]);
+                for (int c = 0; c < kPart; c += 32) tmem_ld32(s_buf + part * kPart + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
+            };
+            // one part of 64 tokens: x = s * scale - m against the reference as it stands, P = 2^x and its sum at once, so that the
+            // special-function unit starts with the first logits; the largest x is looked at behind them
+            auto weigh = [&](auto masked_c, int part, uint32_t (&v)[kPart], uint32_t (&pk)[kPart / 2], float &sum) {
+                if (decltype(masked_c)::value) {  // mask by select: masked logits become -inf, their exponentials exact zeros
+                    const int visible = my_pos - (t0 + part * kPart) + 1;
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (h == 1) tmem_wait_ld();
-                        hide(h * 32, v[h]);
-#pragma unroll
-                        for (int c = 0; c < 32; c += 4) {
-                            const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[h][c]), __uint_as_float(v[h][c + 1])), sc2, nm2);
-                            const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[h][c + 2]), __uint_as_float(v[h][c + 3])), sc2, nm2);
-                            xm[(c >> 2) & 1] = max3(xm[(c >> 2) & 1], x.x, x.y);
-                            xm[2 + ((c >> 2) & 1)] = max3(xm[2 + ((c >> 2) & 1)], y.x, y.y);
-                            const float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y)), f = make_float2(fast_exp2(y.x), fast_exp2(y.y));
-                            a[0] = __fadd2_rn(a[0], e);
-                            a[1] = __fadd2_rn(a[1], f);
-                            pk[(h * 32 + c) >> 1] = pack_bf16x2(e.x, e.y);
-                            pk[((h * 32 + c) >> 1) + 1] = pack_bf16x2(f.x, f.y);
-                        }
-                    }
-                    sum = (a[0].x + a[0].y) + (a[1].x + a[1].y);
-                    return fmaxf(fmaxf(xm[0], xm[1]), fmaxf(xm[2], xm[3]));
-                };
-                if (j == 0) {  // the reference: the row's largest logit of the first block, finite because position 0 is visible
-                    float top = -INFINITY;
-#pragma unroll 1
-                    for (int h = 0; h < 2; ++h) {
-                        uint32_t v[32];
-                        load(h * 32, v);
-                        tmem_wait_ld();
-                        hide(h * 32, v);
-#pragma unroll
-                        for (int c = 0; c < 32; c += 2) top = max3(top, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-                    }
-                    m_run = both(top, larger) * p.scale_log2;
+                    for (int c = 0; c < kPart; ++c)
+                        if (c >= visible) v[c] = 0xff800000u;
                 }
-                float xmax = weigh();
-                if (j > 0 && pair_any(pair, xmax > kRaise)) {
-                    // rare: the row's reference rises by its largest x, what it has accumulated is rescaled (the commit that announced
-                    // S_t(j) also covers O_t(j-1), and no product of this block is under way before both threads hand over P), and the
-                    // part is weighed again (its logits still stand in tensor memory)
-                    xmax = both(xmax, larger);
+                const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), nm2 = make_float2(-m_run, -m_run);
+                float xm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                float2 a[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
+#pragma unroll
+                for (int c = 0; c < kPart; c += 4) {
+                    const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, nm2);
+                    const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, nm2);
+                    xm[(c >> 2) & 1] = max3(xm[(c >> 2) & 1], x.x, x.y);
+                    xm[2 + ((c >> 2) & 1)] = max3(xm[2 + ((c >> 2) & 1)], y.x, y.y);
+                    const float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y)), f = make_float2(fast_exp2(y.x), fast_exp2(y.y));
+                    a[0] = __fadd2_rn(a[0], e);
+                    a[1] = __fadd2_rn(a[1], f);
+                    pk[c >> 1] = pack_bf16x2(e.x, e.y);
+                    pk[(c >> 1) + 1] = pack_bf16x2(f.x, f.y);
+                }
+                sum = (a[0].x + a[0].y) + (a[1].x + a[1].y);
+                return fmaxf(fmaxf(xm[0], xm[1]), fmaxf(xm[2], xm[3]));
+            };
+            auto hand_over = [&](auto masked_c, int part, float xmax, uint32_t (&pk)[kPart / 2], float sum) {
+                if (__any_sync(0xffffffffu, xmax > kRaise)) {
+                    // rare: the row's reference rises by its largest x, what it has accumulated is rescaled, and the part is weighed again
+                    // (its logits still stand in tensor memory)
                     const float shift = xmax > kRaise ? xmax : 0.f, alpha = fast_exp2(-shift);
                     m_run += shift;
+                    if (j > 0 || part > 0) {
+                        if (part > 0) {  // the first part's product of this block must be over before O_t is touched
+                            ok = ok && mbar_wait(bar_o + (2 + t) * 8, j & 1);
+                            tc_fence_after_sync();
+                        }  // (the commit that announced S_t(j) also covers O_t(j-1))
 #pragma unroll 1
-                    for (int c = part * (kLatentHead / 2); c < (part + 1) * (kLatentHead / 2); c += 16) {
-                        uint32_t o[16];
-                        tmem_ld16(o_buf + c, o);
-                        tmem_wait_ld();
+                        for (int c = 0; c < kLatentHead; c += 16) {
+                            uint32_t o[16];
+                            tmem_ld16(o_buf + c, o);
+                            tmem_wait_ld();
 #pragma unroll
-                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                        tmem_st16(o_buf + c, o);
+                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                            tmem_st16(o_buf + c, o);
+                        }
+                        tmem_wait_st();
+                        l_run *= alpha;
                     }
-                    tmem_wait_st();
-                    l_run *= alpha;
-                    weigh();
-                    pair_sync(pair);
+                    uint32_t v[kPart];
+                    load(part, v);
+                    tmem_wait_ld();
+                    weigh(masked_c, part, v, pk, sum);
                 }
-                // P over the first 64 columns of S_t. Part 1's P lies where part 0's logits were: the row's threads have met since they
-                // read them
-                if (j == 0) pair_sync(pair);
-                tmem_st16(s_buf + part * (kPart / 2), *reinterpret_cast<uint32_t(*)[16]>(pk));
-                tmem_st16(s_buf + part * (kPart / 2) + 16, *reinterpret_cast<uint32_t(*)[16]>(pk + 16));
                 l_run += sum;
+                // P over the first 64 columns of the tile's logit buffer (columns this thread has already consumed)
+#pragma unroll
+                for (int c = 0; c < kPart / 2; c += 16) tmem_st16(s_buf + part * (kPart / 2) + c, *reinterpret_cast<uint32_t(*)[16]>(pk + c));
+                tmem_wait_st();
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_p + (t * 2 + part) * 8);
             };
-            if (__any_sync(0xffffffffu, visible < kPart)) run(std::true_type{});
-            else run(std::false_type{});
-            tmem_wait_st();
-            tc_fence_before_sync();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_p + (t * 2 + part) * 8);
+            auto do_block = [&](auto masked_c) {
+                uint32_t va[kPart], vb[kPart], pk[kPart / 2];
+                float sum;
+                load(0, va);
+                tmem_wait_ld();
+                if (j == 0) {  // the reference: the row's largest logit of the first part, finite because position 0 is visible
+                    float top = -INFINITY;
+                    const int visible = my_pos + 1;
+#pragma unroll
+                    for (int c = 0; c < kPart; ++c) top = c < visible ? fmaxf(top, __uint_as_float(va[c])) : top;
+                    m_run = top * p.scale_log2;
+                }
+                load(1, vb);  // on their way while the first part's exponentials run
+                float xmax = weigh(masked_c, 0, va, pk, sum);
+                tmem_wait_ld();
+                hand_over(masked_c, 0, xmax, pk, sum);
+                xmax = weigh(masked_c, 1, vb, pk, sum);
+                hand_over(masked_c, 1, xmax, pk, sum);
+            };
+            if (__any_sync(0xffffffffu, masked)) do_block(std::true_type{});
+            else do_block(std::false_type{});
         }
 
-        // ---- epilogue: O_t / l -> bf16 rows, half a row per thread
+        // ---- epilogue: O_t / l -> bf16 rows
         ok = ok && mbar_wait(bar_o + t * 8, 0);
         tc_fence_after_sync();
-        l_run = both(l_run, [](float a, float b) { return a + b; });
         const float inv = 1.f / l_run;
         const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
         __nv_bfloat16 *orow = p.out + (static_cast<size_t>(q0 + cta_start + min(tok, n_tok - 1)) * p.Hq + head) * kLatentHead;
 #pragma unroll
-        for (int c = 0; c < kLatentHead / 2; c += 32) {
-            const int col = part * (kLatentHead / 2) + c;
+        for (int c = 0; c < kLatentHead; c += 32) {
             uint32_t o[32];
-            tmem_ld32(o_buf + col, o);
+            tmem_ld32(o_buf + c, o);
             tmem_wait_ld();
             if (row_valid && ok) {
 #pragma unroll
@@ -435,15 +415,15 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
 #pragma unroll
                     for (int k = 0; k < 8; ++k) v[k] = pack_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
                     if (wide) {
-                        store32(orow + col + i, v);
+                        store32(orow + c + i, v);
                     } else {
-                        *reinterpret_cast<uint4 *>(orow + col + i) = make_uint4(v[0], v[1], v[2], v[3]);
-                        *reinterpret_cast<uint4 *>(orow + col + i + 8) = make_uint4(v[4], v[5], v[6], v[7]);
+                        *reinterpret_cast<uint4 *>(orow + c + i) = make_uint4(v[0], v[1], v[2], v[3]);
+                        *reinterpret_cast<uint4 *>(orow + c + i + 8) = make_uint4(v[4], v[5], v[6], v[7]);
                     }
                 }
             }
         }
-        if (p.lse != nullptr && row_valid && ok && part == 0)
+        if (p.lse != nullptr && row_valid && ok)
             p.lse[static_cast<size_t>(q0 + cta_start + tok) * p.Hq + head] = (m_run + log2f(l_run)) * kLn2f;
         if (!ok && lane == 0) latch(p.status, kDevTimeout, b, blockIdx.x);
     }
