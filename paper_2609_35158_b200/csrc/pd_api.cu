@@ -189,22 +189,27 @@ int encode_rows_map(pd_ctx *ctx, const void *ptr, int width, int64_t rows, int b
     return PD_ERR_CUDA;
 }
 
-// A pool of shared latent vectors, twice: rows = (page, slot) with a box of 16 rows x 64 columns; and as [row group][block of 64
-// columns][8 rows][64], box = both row groups of a page x 2 blocks.
+// Rows of `blocks` x 64 bf16 columns, every 16 of them a page, as [8-row group][block of 64 columns][8 rows][64]; box = both groups
+// of a page x 2 blocks. In shared memory a tile's row groups then lie at one distance from one another, across its pages too.
+int encode_groups_map(pd_ctx *ctx, const void *ptr, int blocks, int64_t rows, CUtensorMap *out) {
+    const cuuint64_t dims[4] = {64, 8, static_cast<cuuint64_t>(blocks), static_cast<cuuint64_t>(rows) / 8};
+    const cuuint64_t strides[3] = {static_cast<cuuint64_t>(blocks) * 128, 128, static_cast<cuuint64_t>(blocks) * 1024};
+    const cuuint32_t box[4] = {64, 8, 2, 2}, elem_strides[4] = {1, 1, 1, 1};
+    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(ptr), dims, strides, box, elem_strides,
+                                   CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B,
+                                   CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    if (r == CUDA_SUCCESS) return PD_OK;
+    std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
+    return PD_ERR_CUDA;
+}
+
+// A pool of shared latent vectors, twice: boxes of 16 rows x 64 columns, and of a page's row groups.
 int latent_map(pd_ctx *ctx, const void *kv_pages) {
     if (ctx->map_latent_ptr == kv_pages) return PD_OK;
     ctx->map_latent_ptr = nullptr;
-    if (int rc = encode_rows_map(ctx, kv_pages, pd::kLatentRow, ctx->cfg.num_pages * pd::kPageSize, pd::kPageSize, &ctx->tm_latent)) return rc;
-    const cuuint64_t dims[4] = {64, 8, pd::kLatentRow / 64, static_cast<cuuint64_t>(ctx->cfg.num_pages) * 2};
-    const cuuint64_t strides[3] = {pd::kLatentRow * 2, 128, 8 * pd::kLatentRow * 2};
-    const cuuint32_t box[4] = {64, 8, 2, 2}, elem_strides[4] = {1, 1, 1, 1};
-    const CUresult r = ctx->encode(&ctx->tm_latent_pairs, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(kv_pages), dims, strides,
-                                   box, elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
-                                   CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
-    if (r != CUDA_SUCCESS) {
-        std::snprintf(ctx->last_error, sizeof ctx->last_error, "cuTensorMapEncodeTiled failed (%d)", static_cast<int>(r));
-        return PD_ERR_CUDA;
-    }
+    const int64_t rows = ctx->cfg.num_pages * pd::kPageSize;
+    if (int rc = encode_rows_map(ctx, kv_pages, pd::kLatentRow, rows, pd::kPageSize, &ctx->tm_latent)) return rc;
+    if (int rc = encode_groups_map(ctx, kv_pages, pd::kLatentRow / 64, rows, &ctx->tm_latent_pairs)) return rc;
     ctx->map_latent_ptr = kv_pages;
     return PD_OK;
 }
@@ -1542,8 +1547,8 @@ int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, 
     const int64_t rows = expanded_num_pages * ctx->cfg.num_q_heads * pd::kPageSize;
     if (ctx->map_expanded_k_ptr != k_pages || ctx->map_expanded_v_ptr != v_pages || ctx->map_expanded_pages != expanded_num_pages) {
         ctx->map_expanded_k_ptr = nullptr;
-        if (int rc = encode_rows_map(ctx, k_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_k)) return rc;
-        if (int rc = encode_rows_map(ctx, v_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_v)) return rc;
+        if (int rc = encode_groups_map(ctx, k_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_k)) return rc;
+        if (int rc = encode_groups_map(ctx, v_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_v)) return rc;
         ctx->map_expanded_k_ptr = k_pages;
         ctx->map_expanded_v_ptr = v_pages;
         ctx->map_expanded_pages = expanded_num_pages;

@@ -1,24 +1,23 @@
 // Append-prefill attention in the expanded form of a cache of shared latent vectors: queries of 192 values, 128 against the
 // head's own expanded keys, 64 against the rotated key part all heads share; values of 128.
 //
-// The scheme is that of pd_prefill_attn_d128.cu: one CTA per SM owns two tiles of 128 query rows (here 256 consecutive new
-// tokens of one head) that share every K and V tile, walks the context in blocks of 128 tokens, and issues
-// O0(j) S0(j+1) O1(j) S1(j+1) so that the tensor pipe runs one tile's products while the other tile's warpgroup does its softmax.
-// What differs and why:
-// - S is a product over 192: 12 MMAs of 128 x 128 x 16 a tile and block beside 8 of O, 2560 tensor cycles a block for both tiles,
-//   and 2048 cycles of exponentials (16 per clock): the tensor pipe is the bound, not the softmax.
-// - Q takes 96 KB, which leaves eight pieces of 16 KB. K goes in pieces of 64 columns (two from the head's own pages, one from
-//   the rotated part of the latent pages), five in flight; V in halves of 64 tokens, three in flight. A piece is handed
-//   back by its last product, not with its block, so the piece a block is short of is under way 1300-1500 cycles before it is needed.
-// - Each tile has its own number of blocks: the first skips those that only the second one sees, and a turn of at most 128 tokens
-//   runs one tile.
-// - The issuing thread is chosen by elect.sync: the products then issue in half the time they take to run.
-// Tensor memory: S0 | S1 | O0 | O1, 128 columns each; P_t as bf16 over the first 64 columns of S_t. Every wait is bounded.
+// One CTA per SM owns two tiles of 128 query rows (256 consecutive new tokens of one head) that share every K and V tile, as in
+// pd_prefill_attn_d128.cu, and walks the context in blocks of 80 tokens (5 pages):
+//   tcgen05  S_t = Q_t K^T (12 MMAs of 128 x 80 x 16, Q and K from shared memory), O_t += P_t V (5 of 128 x 128 x 16, P_t from
+//            tensor memory), in the order S0(j+1) O0(j) S1(j+1) O1(j)
+//   softmax  one warpgroup per tile, one thread per row
+// Why 80: tensor memory has 128 columns a tile beside its 128 of O. With blocks of 128 P has to lie where S lay, so S(j+1) waits
+// for the softmax of block j, for its O product and for four hand-overs: 3630 cycles per 128 tokens (both tiles), where the
+// products take 2560. With 80 columns of S and 40 of P beside them, S(j+1) waits only until the row threads hold the
+// logits of block j in registers, and runs during their softmax. What bounds it now is shared memory: an S product reads 4 KB of Q and 2.5 KB of
+// K in 51 cycles (128 bytes each), 1864 cycles a block with O, and the copies write 50 KB (400 cycles) beside that.
+// A page's 128 columns come as one box in the order [8-row group][64-column half][8 rows]: row groups follow one another
+// at the same distance across pages, as both operand forms want it.
+// Each tile has its own number of blocks: the first skips those that only the second one sees, and a turn of at most 128 tokens
+// runs one tile. Tensor memory: (S0 80, P0 40) (S1, P1) O0 O1, 128 columns each. Every wait is bounded.
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_tcgen05.cuh"
-
-#include <type_traits>
 
 namespace pd {
 
@@ -28,20 +27,20 @@ constexpr float kLn2f = 0.6931471805599453f;
 constexpr float kRaise = 32.f;                  // log2 units a logit may exceed its row's reference
 constexpr int kRows = 128;                      // query rows per tile (MMA M), one softmax thread each
 constexpr int kTiles = 2;
-constexpr int kBlock = 128;                     // context tokens per step
+constexpr int kBlock = 80;                      // context tokens per step
 constexpr int kBlockPages = kBlock / kPageSize;
 constexpr int kQDim = kLatentHead + kLatentRope;
-constexpr int kPiece = 16384;                   // 128 rows of 64 columns, or 64 tokens of 128 columns
-constexpr int kKPieces = kQDim / 64;            // per block
-constexpr int kKSlots = 5, kVSlots = 3;
-constexpr int kParts = 2, kPart = kBlock / kParts;  // P and the O product go in two parts of 64 tokens
+constexpr int kQPiece = kRows * 128;            // 64 columns of a Q tile
+constexpr int kQTileBytes = kQDim / 64 * kQPiece;
+constexpr int kKvBytes = kBlock * kLatentHead * 2;   // a block's K or V
+constexpr int kRopeBytes = kBlock * kLatentRope * 2;
+constexpr int kKSlots = 2, kVSlots = 3;
 constexpr int kSoftmaxWarps = kTiles * kRows / 32;
 constexpr int kThreads = 32 * (kSoftmaxWarps + 4);  // + MMA warp, K loader, V loader, one spare
-constexpr int kQTileBytes = kKPieces * kPiece;
 constexpr int kTmemCols = 512;
-constexpr int kColS = 0, kColO = 256;
-constexpr int kNumBars = 2 * kKSlots + 2 * kVSlots + 2 + 4 + 4 + 1 + 2;
-constexpr size_t kSmemBytes = 1024 + kTiles * kQTileBytes + (kKSlots + kVSlots) * kPiece + kNumBars * 8;
+constexpr int kColS = 0, kColP = kBlock, kColO = 256;  // S_t, P_t at 128 t + .., O_t at kColO + 128 t
+constexpr int kNumBars = 4 * kKSlots + 2 * kVSlots + 5 * kTiles + 1;
+constexpr size_t kSmemBytes = 1024 + kTiles * kQTileBytes + kKSlots * (kKvBytes + kRopeBytes) + kVSlots * kKvBytes + kNumBars * 8;
 
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float d;
@@ -64,6 +63,11 @@ __device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
           "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(taddr)
         : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t w, uint32_t bar, uint64_t l2_policy) {
+    asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
+                 " [%0], [%1, {%2, %2, %2, %3}], [%4], %5;"
+                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(0), "r"(w), "r"(bar), "l"(l2_policy) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
     asm volatile(
@@ -104,22 +108,22 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
     const int n_pages = (L + kPageSize - 1) / kPageSize;
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
-    uint8_t *aligned = smem_raw + (base - smem_u32(smem_raw));
-    const uint32_t q_s = base;
-    const uint32_t k_ring = base + kTiles * kQTileBytes, v_ring = k_ring + kKSlots * kPiece;
-    uint64_t *bars = reinterpret_cast<uint64_t *>(aligned + kTiles * kQTileBytes + (kKSlots + kVSlots) * kPiece);
-    const uint32_t bar_k = smem_u32(bars), bar_kfree = bar_k + kKSlots * 8;          // a piece of K landed / is free again
-    const uint32_t bar_v = bar_kfree + kKSlots * 8, bar_vfree = bar_v + kVSlots * 8;
-    const uint32_t bar_s = bar_vfree + kVSlots * 8;  // [2] S_t of the current block complete (and every product before it)
-    const uint32_t bar_p = bar_s + 16;               // [2 tiles][2 parts] that part of P_t is written (4 warps each)
-    const uint32_t bar_o = bar_p + 32;               // [2] last O_t product complete; [2] first part's O_t product of the block complete
-    const uint32_t bar_drain = bar_o + 32;
-    const uint32_t bar_q = bar_drain + 8;            // [2] tile t's queries are in shared memory (4 warps each)
+    const uint32_t q_s = base, k_ring = q_s + kTiles * kQTileBytes, r_ring = k_ring + kKSlots * kKvBytes;
+    const uint32_t v_ring = r_ring + kKSlots * kRopeBytes;
+    const uint32_t bar_k = v_ring + kVSlots * kKvBytes, bar_kfree = bar_k + kKSlots * 8;  // a block of K landed / is free again
+    const uint32_t bar_r = bar_kfree + kKSlots * 8, bar_rfree = bar_r + kKSlots * 8;      // the same of the rotated part
+    const uint32_t bar_v = bar_rfree + kKSlots * 8, bar_vfree = bar_v + kVSlots * 8;
+    const uint32_t bar_s = bar_vfree + kVSlots * 8;  // [2] S_t of the block complete
+    const uint32_t bar_o = bar_s + kTiles * 8;       // [2] O_t product of the block complete
+    const uint32_t bar_drain = bar_o + kTiles * 8;
+    const uint32_t bar_sfree = bar_drain + 8;        // [2] the rows hold S_t of the block in registers (4 warps each, like the next two)
+    const uint32_t bar_p = bar_sfree + kTiles * 8;   // [2] P_t is written
+    const uint32_t bar_q = bar_p + kTiles * 8;       // [2] tile t's queries are in shared memory
 
     if (tid == 0) {
         for (int i = 0; i < kNumBars; ++i) {
             const uint32_t bar = bar_k + i * 8;
-            mbar_init(bar, bar >= bar_q || (bar >= bar_p && bar < bar_o) ? kRows / 32 : 1);
+            mbar_init(bar, bar >= bar_sfree ? kRows / 32 : 1);
         }
         mbar_init_fence();
         prefetch_tensormap(&tm_k);
@@ -145,126 +149,122 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         if (elect_one()) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(kRows, kBlock, false);
             constexpr uint32_t idesc_o = umma_idesc_bf16(kRows, kLatentHead, true);
-            const uint64_t q_desc = umma_smem_desc(q_s, 16, 1024), k_desc = umma_smem_desc(k_ring, 16, 1024);
-            const uint64_t v_desc = umma_smem_desc(v_ring, kPart * 128, 1024);
+            const uint64_t q_desc = umma_smem_desc(q_s, 16, 1024), k_desc = umma_smem_desc(k_ring, 16, 2048);
+            const uint64_t r_desc = umma_smem_desc(r_ring, 16, 1024), v_desc = umma_smem_desc(v_ring, 1024, 2048);
             auto issue_s = [&](int t, int j, bool wait, bool release) {  // S_t(j) = Q_t K_j^T
-#pragma unroll
-                for (int c = 0; c < kKPieces; ++c) {
-                    const int i = j * kKPieces + c, slot = i % kKSlots;
-                    if (wait) {
-                        ok = ok && mbar_wait(bar_k + slot * 8, (i / kKSlots) & 1);
-                        if (!ok) return;
-                        tc_fence_after_sync();
-                    }
-#pragma unroll
-                    for (int ks = 0; ks < 4; ++ks)
-                        umma_ss(tm + kColS + t * kBlock, q_desc + ((t * kQTileBytes + c * kPiece) >> 4) + ks * 2,
-                                k_desc + slot * (kPiece >> 4) + ks * 2, idesc_s, (c | ks) != 0);
-                    if (release) umma_commit(bar_kfree + slot * 8);
-                }
-                umma_commit(bar_s + t * 8);
-            };
-            auto issue_o = [&](int t, int j, int part, bool wait, bool release, bool last) {  // O_t += P_t(j)[:, part] V_j[part]
-                const int i = j * kParts + part, slot = i % kVSlots;
-                ok = ok && mbar_wait(bar_p + (t * 2 + part) * 8, j & 1);
-                if (wait) ok = ok && mbar_wait(bar_v + slot * 8, (i / kVSlots) & 1);
+                const int slot = j % kKSlots;
+                const uint32_t d = tm + kColS + t * 128, parity = (j / kKSlots) & 1;
+                const uint64_t q = q_desc + (t * kQTileBytes >> 4);
+                if (wait) ok = ok && mbar_wait(bar_k + slot * 8, parity);
                 if (!ok) return;
                 tc_fence_after_sync();
 #pragma unroll
-                for (int ks = 0; ks < kPart / 16; ++ks)
-                    umma_ts(tm + kColO + t * kLatentHead, tm + kColS + t * kBlock + (part * (kPart / 16) + ks) * 8,
-                            v_desc + slot * (kPiece >> 4) + ks * (2048 >> 4), idesc_o, (j | part | ks) != 0);
+                for (int c = 0; c < 2; ++c)
+#pragma unroll
+                    for (int ks = 0; ks < 4; ++ks)
+                        umma_ss(d, q + (c * kQPiece >> 4) + ks * 2, k_desc + slot * (kKvBytes >> 4) + c * (1024 >> 4) + ks * 2, idesc_s, (c | ks) != 0);
+                if (release) umma_commit(bar_kfree + slot * 8);
+                if (wait) ok = mbar_wait(bar_r + slot * 8, parity);
+                if (!ok) return;
+                tc_fence_after_sync();
+#pragma unroll
+                for (int ks = 0; ks < 4; ++ks)
+                    umma_ss(d, q + (2 * kQPiece >> 4) + ks * 2, r_desc + slot * (kRopeBytes >> 4) + ks * 2, idesc_s, true);
+                if (release) umma_commit(bar_rfree + slot * 8);
+                umma_commit(bar_s + t * 8);
+            };
+            auto issue_o = [&](int t, int j, bool wait, bool release) {  // O_t += P_t(j) V_j
+                const int slot = j % kVSlots;
+                ok = mbar_wait(bar_p + t * 8, j & 1);
+                if (wait) ok = ok && mbar_wait(bar_v + slot * 8, (j / kVSlots) & 1);
+                if (!ok) return;
+                tc_fence_after_sync();
+#pragma unroll
+                for (int ks = 0; ks < kBlock / 16; ++ks)
+                    umma_ts(tm + kColO + t * kLatentHead, tm + t * 128 + kColP + ks * 8, v_desc + slot * (kKvBytes >> 4) + ks * (4096 >> 4), idesc_o,
+                            (j | ks) != 0);
                 if (release) umma_commit(bar_vfree + slot * 8);
-                if (part == 0) umma_commit(bar_o + (2 + t) * 8);  // lets a row thread rescale O_t between the two parts (rare)
-                else if (last) umma_commit(bar_o + t * 8);
+                umma_commit(bar_o + t * 8);
             };
             ok = mbar_wait(bar_q, 0);
             if (ok) issue_s(0, 0, true, nb1 == 0);
             if (nb1 > 0) ok = ok && mbar_wait(bar_q + 8, 0);
             if (ok && nb1 > 0) issue_s(1, 0, false, true);
-            // the tile that meets a piece first waits for it, the one that meets it last hands it back
+            // the tile that meets a block first waits for it, the one that meets it last hands it back
             for (int j = 0; j < nb && ok; ++j) {
                 const bool u0 = j < nb0, u1 = j < nb1, n0 = j + 1 < nb0, n1 = j + 1 < nb1;
-                if (u0) {
-                    issue_o(0, j, 0, true, !u1, j == nb0 - 1);
-                    if (ok) issue_o(0, j, 1, true, !u1, j == nb0 - 1);
-                }
+                if (n0) ok = mbar_wait(bar_sfree, j & 1);
                 if (ok && n0) issue_s(0, j + 1, true, !n1);
-                if (ok && u1) {
-                    issue_o(1, j, 0, !u0, true, j == nb1 - 1);
-                    if (ok) issue_o(1, j, 1, !u0, true, j == nb1 - 1);
-                }
+                if (ok && u0) issue_o(0, j, true, !u1);
+                if (ok && n1) ok = mbar_wait(bar_sfree + 8, j & 1);
                 if (ok && n1) issue_s(1, j + 1, !n0, true);
+                if (ok && u1) issue_o(1, j, !u0, true);
             }
             if (!ok) latch(p.status, kDevTimeout, b, blockIdx.x);
             umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
             mbar_wait(bar_drain, 0);
         }
     } else if (warp == kSoftmaxWarps + 1 || warp == kSoftmaxWarps + 2) {
-        // ================= two TMA warps (one streams K, the other V): one box per lane, eight per piece =================
-        const uint64_t policy = l2_policy_evict_first();
-        const bool is_k = warp == kSoftmaxWarps + 1;
-        const int32_t oob_kv = lp.kv_num_pages * p.Hq * kPageSize, oob_r = p.num_pages * kPageSize;  // boxes there are zero fill
-        const int32_t *kv_row = lp.kv_table + static_cast<size_t>(b) * p.MP, *r_row = p.page_table + static_cast<size_t>(b) * p.MP;
-        int issued = 0;
-        auto page_y = [&](const int32_t *table_row, int lp_page, int limit, int scale, int add, int32_t oob) {
-            if (lp_page >= n_pages) return oob;
-            int pid = __ldg(table_row + lp_page);
-            if (pid < 0 || pid >= limit) {
+        // ================= two TMA warps (K and the rotated part, V), one elected thread each =================
+        if (elect_one()) {
+            const uint64_t policy = l2_policy_evict_first();
+            const bool is_k = warp == kSoftmaxWarps + 1;
+            const int32_t *kv_row = lp.kv_table + static_cast<size_t>(b) * p.MP, *r_row = p.page_table + static_cast<size_t>(b) * p.MP;
+            int issued = 0, issued_r = 0;
+            int32_t kv_id[kBlockPages], r_id[kBlockPages];  // the next block's pages
+            auto load_ids = [&](int j) {
+#pragma unroll
+                for (int g = 0; g < kBlockPages; ++g) {
+                    const int page = j * kBlockPages + g;
+                    kv_id[g] = page < n_pages ? __ldg(kv_row + page) : 0;
+                    if (is_k) r_id[g] = page < n_pages ? __ldg(r_row + page) : 0;
+                }
+            };
+            auto checked = [&](int32_t pid, int page, int limit) {  // `limit`: a page past the pool is zero fill
+                if (page >= n_pages) return limit;
+                if (pid >= 0 && pid < limit) return pid;
                 latch(p.status, kDevBadPage, b, pid);
-                pid = 0;
-            }
-            return (pid * scale + add) * kPageSize;
-        };
-        if (is_k) {
-            int32_t y_next = lane < 16 ? (lane < 8 ? page_y(kv_row, lane, lp.kv_num_pages, p.Hq, head, oob_kv)
-                                                   : page_y(r_row, lane - 8, p.num_pages, 1, 0, oob_r)) : 0;
+                return 0;
+            };
+            load_ids(0);
             for (int j = 0; j < nb && ok; ++j) {
-                const int32_t y = y_next;  // lanes 0..7: the block's pages of K, lanes 8..15: of the rotated part
-                if (j + 1 < nb && lane < 16)
-                    y_next = lane < 8 ? page_y(kv_row, (j + 1) * kBlockPages + lane, lp.kv_num_pages, p.Hq, head, oob_kv)
-                                      : page_y(r_row, (j + 1) * kBlockPages + lane - 8, p.num_pages, 1, 0, oob_r);
-                for (int c = 0; c < kKPieces; ++c) {
-                    const int i = j * kKPieces + c, slot = i % kKSlots, fill = i / kKSlots;
-                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_kfree + slot * 8, (fill - 1) & 1));
+                int32_t kv_page[kBlockPages], r_page[kBlockPages];
+#pragma unroll
+                for (int g = 0; g < kBlockPages; ++g) {
+                    kv_page[g] = checked(kv_id[g], j * kBlockPages + g, lp.kv_num_pages);
+                    r_page[g] = is_k ? checked(r_id[g], j * kBlockPages + g, p.num_pages) : 0;
+                }
+                if (j + 1 < nb) load_ids(j + 1);
+                const int slots = is_k ? kKSlots : kVSlots, slot = j % slots, fill = j / slots;
+                const uint32_t full = (is_k ? bar_k : bar_v) + slot * 8, dst = (is_k ? k_ring : v_ring) + slot * kKvBytes;
+                if (fill > 0) ok = mbar_wait((is_k ? bar_kfree : bar_vfree) + slot * 8, (fill - 1) & 1);
+                if (!ok) break;
+                mbar_arrive_expect_tx(full, kKvBytes);
+#pragma unroll
+                for (int g = 0; g < kBlockPages; ++g) tma_load_4d(dst + g * 4096, is_k ? &tm_k : &tm_v, (kv_page[g] * p.Hq + (kv_page[g] < lp.kv_num_pages ? head : 0)) * 2, full, policy);
+                issued = j + 1;
+                if (is_k) {
+                    if (fill > 0) ok = mbar_wait(bar_rfree + slot * 8, (fill - 1) & 1);
                     if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_k + slot * 8, kPiece);
-                    __syncwarp();
-                    const uint32_t dst = k_ring + slot * kPiece + (lane & 7) * (kPageSize * 128);
-                    if (c < 2 && lane < 8) tma_load_2d(dst, &tm_k, c * 64, y, bar_k + slot * 8, policy);
-                    if (c == 2 && lane >= 8 && lane < 16) tma_load_2d(dst, &tm_r, kLatentDim, y, bar_k + slot * 8, policy);
-                    issued = i + 1;
+                    mbar_arrive_expect_tx(bar_r + slot * 8, kRopeBytes);
+#pragma unroll
+                    for (int g = 0; g < kBlockPages; ++g)
+                        tma_load_2d(r_ring + slot * kRopeBytes + g * (kPageSize * 128), &tm_r, kLatentDim, r_page[g] * kPageSize, bar_r + slot * 8, policy);
+                    issued_r = j + 1;
                 }
             }
-        } else {
-            int32_t y_next = lane < 8 ? page_y(kv_row, lane, lp.kv_num_pages, p.Hq, head, oob_kv) : 0;
-            for (int j = 0; j < nb && ok; ++j) {
-                const int32_t y = y_next;
-                if (j + 1 < nb && lane < 8) y_next = page_y(kv_row, (j + 1) * kBlockPages + lane, lp.kv_num_pages, p.Hq, head, oob_kv);
-                for (int part = 0; part < kParts; ++part) {
-                    const int i = j * kParts + part, slot = i % kVSlots, fill = i / kVSlots;
-                    if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_vfree + slot * 8, (fill - 1) & 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_v + slot * 8, kPiece);
-                    __syncwarp();
-                    const int32_t yy = __shfl_sync(0xffffffffu, y, part * 4 + ((lane >> 1) & 3));
-                    if (lane < 8)
-                        tma_load_2d(v_ring + slot * kPiece + (lane & 1) * (kPart * 128) + (lane >> 1) * (kPageSize * 128), &tm_v, (lane & 1) * 64, yy,
-                                    bar_v + slot * 8, policy);
-                    issued = i + 1;
-                }
+            if (!ok) {  // copies in flight have to land before the block's memory goes
+                latch(p.status, kDevTimeout, b, blockIdx.x);
+                const int slots = is_k ? kKSlots : kVSlots;
+                for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait((is_k ? bar_k : bar_v) + (i % slots) * 8, (i / slots) & 1);
+                for (int i = max(0, issued_r - kKSlots); i < issued_r; ++i) mbar_wait(bar_r + (i % kKSlots) * 8, (i / kKSlots) & 1);
             }
-        }
-        if (!ok) {  // copies in flight have to land before the block's memory goes
-            if (lane == 0) latch(p.status, kDevTimeout, b, blockIdx.x);
-            const int slots = is_k ? kKSlots : kVSlots;
-            for (int i = max(0, issued - slots); i < issued; ++i) mbar_wait((is_k ? bar_k : bar_v) + (i % slots) * 8, (i / slots) & 1);
         }
     } else if (warp < kSoftmaxWarps && (tile == 0 || nb1 > 0)) {
         // ================= softmax warpgroups: warpgroup t owns tile t, one thread per query row =================
         const int t = tile, my_nb = t == 0 ? nb0 : nb1;
         const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
-        const uint32_t s_buf = tm + lane_base + kColS + t * kBlock;
+        const uint32_t s_buf = tm + lane_base + kColS + t * 128, p_buf = tm + lane_base + kColP + t * 128;
         const uint32_t o_buf = tm + lane_base + kColO + t * kLatentHead;
         // ---- the tile's queries: neighbouring threads copy neighbouring 16 bytes, all in flight at once
         {
@@ -274,7 +274,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
 #pragma unroll
             for (int i = 0; i < kChunks; ++i) {
                 const int x = i * kRows + row, r = x / kChunks, c = x - r * kChunks;
-                const uint32_t a = q_s + tile * kQTileBytes + (c >> 3) * kPiece + sw128_offset(r, c & 7);
+                const uint32_t a = q_s + tile * kQTileBytes + (c >> 3) * kQPiece + sw128_offset(r, c & 7);
                 cp_async16(a, src + static_cast<size_t>(min(r, rows - 1)) * p.Hq * kQDim + c * 8, r < rows ? 16 : 0);  // rows past the last are zeros
             }
             cp_async_wait_all();
@@ -294,36 +294,31 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             const int valid_rows = L - t0;
             if (valid_rows < kBlock && (t == 0 || j >= nb0)) {
                 const int last = min(kBlock, (valid_rows + kPageSize - 1) / kPageSize * kPageSize);
-                for (int part = 0; part < kParts; ++part) {  // the parts must have landed
-                    const int i = j * kParts + part;
-                    ok = ok && mbar_wait(bar_v + (i % kVSlots) * 8, (i / kVSlots) & 1);
-                }
+                ok = mbar_wait(bar_v + (j % kVSlots) * 8, (j / kVSlots) & 1);  // it must have landed
                 if (!ok) break;
                 for (int i = row; i < (last - valid_rows) * (kLatentHead / 8); i += kRows) {
                     const int r = valid_rows + i / (kLatentHead / 8), c = i % (kLatentHead / 8);
-                    const int slot = (j * kParts + r / kPart) % kVSlots;
-                    st_shared_zero16(v_ring + slot * kPiece + (c >> 3) * (kPart * 128) + (r % kPart) * 128 + (c & 7) * 16);
+                    st_shared_zero16(v_ring + (j % kVSlots) * kKvBytes + (r >> 3) * 2048 + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16);
                 }
                 fence_proxy_async();
             }
-            auto load = [&](int part, uint32_t (&v)[kPart]) {
-#pragma unroll
-                for (int c = 0; c < kPart; c += 32) tmem_ld32(s_buf + part * kPart + c, *reinterpret_cast<uint32_t(*)[32]>(v + c));
-            };
-            // one part of 64 tokens: x = s * scale - m against the reference as it stands, P = 2^x and its sum at once, so that the
-            // special-function unit starts with the first logits; the largest x is looked at behind them
-            auto weigh = [&](auto masked_c, int part, uint32_t (&v)[kPart], uint32_t (&pk)[kPart / 2], float &sum) {
-                if (decltype(masked_c)::value) {  // mask by select: masked logits become -inf, their exponentials exact zeros
-                    const int visible = my_pos - (t0 + part * kPart) + 1;
-#pragma unroll
-                    for (int c = 0; c < kPart; ++c)
-                        if (c >= visible) v[c] = 0xff800000u;
-                }
+            uint32_t v[kBlock], pk[kBlock / 2];
+            tmem_ld32(s_buf, *reinterpret_cast<uint32_t(*)[32]>(v));
+            tmem_ld32(s_buf + 32, *reinterpret_cast<uint32_t(*)[32]>(v + 32));
+            tmem_ld16(s_buf + 64, *reinterpret_cast<uint32_t(*)[16]>(v + 64));
+            tmem_wait_ld();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_sfree + t * 8);  // S_t(j+1) may come
+            float sum = 0.f;
+            // x = s * scale - m against the reference as it stands, P = 2^x and its sum at once, so that the special-function unit
+            // starts with the first logits; the largest x is looked at behind them
+            auto weigh = [&]() {
                 const float2 sc2 = make_float2(p.scale_log2, p.scale_log2), nm2 = make_float2(-m_run, -m_run);
                 float xm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                 float2 a[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
-                for (int c = 0; c < kPart; c += 4) {
+                for (int c = 0; c < kBlock; c += 4) {
                     const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, nm2);
                     const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, nm2);
                     xm[(c >> 2) & 1] = max3(xm[(c >> 2) & 1], x.x, x.y);
@@ -337,68 +332,57 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 sum = (a[0].x + a[0].y) + (a[1].x + a[1].y);
                 return fmaxf(fmaxf(xm[0], xm[1]), fmaxf(xm[2], xm[3]));
             };
-            auto hand_over = [&](auto masked_c, int part, float xmax, uint32_t (&pk)[kPart / 2], float sum) {
-                if (__any_sync(0xffffffffu, xmax > kRaise)) {
-                    // rare: the row's reference rises by its largest x, what it has accumulated is rescaled, and the part is weighed again
-                    // (its logits still stand in tensor memory)
-                    const float shift = xmax > kRaise ? xmax : 0.f, alpha = fast_exp2(-shift);
-                    m_run += shift;
-                    if (j > 0 || part > 0) {
-                        if (part > 0) {  // the first part's product of this block must be over before O_t is touched
-                            ok = ok && mbar_wait(bar_o + (2 + t) * 8, j & 1);
-                            tc_fence_after_sync();
-                        }  // (the commit that announced S_t(j) also covers O_t(j-1))
+            if (__any_sync(0xffffffffu, masked)) {  // masked logits become -inf, their exponentials exact zeros
+                const int visible = my_pos - t0 + 1;
+#pragma unroll
+                for (int c = 0; c < kBlock; ++c)
+                    if (c >= visible) v[c] = 0xff800000u;
+            }
+            if (j == 0) {  // the reference: the row's largest logit of the block, finite because position 0 is visible
+                float top = -INFINITY;
+#pragma unroll
+                for (int c = 0; c < kBlock; c += 2) top = max3(top, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                m_run = top * p.scale_log2;
+            }
+            const float xmax = weigh();
+            if (__any_sync(0xffffffffu, xmax > kRaise)) {
+                // rare: the row's reference rises by its largest x, what it has accumulated is rescaled, and the block is weighed again
+                const float shift = xmax > kRaise ? xmax : 0.f, alpha = fast_exp2(-shift);
+                m_run += shift;
+                if (j > 0) {
+                    ok = mbar_wait(bar_o + t * 8, (j - 1) & 1);
+                    tc_fence_after_sync();
 #pragma unroll 1
-                        for (int c = 0; c < kLatentHead; c += 16) {
-                            uint32_t o[16];
-                            tmem_ld16(o_buf + c, o);
-                            tmem_wait_ld();
+                    for (int c = 0; c < kLatentHead; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(o_buf + c, o);
+                        tmem_wait_ld();
 #pragma unroll
-                            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
-                            tmem_st16(o_buf + c, o);
-                        }
-                        tmem_wait_st();
-                        l_run *= alpha;
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * alpha);
+                        tmem_st16(o_buf + c, o);
                     }
-                    uint32_t v[kPart];
-                    load(part, v);
-                    tmem_wait_ld();
-                    weigh(masked_c, part, v, pk, sum);
+                    tmem_wait_st();
+                    l_run *= alpha;
                 }
-                l_run += sum;
-                // P over the first 64 columns of the tile's logit buffer (columns this thread has already consumed)
-#pragma unroll
-                for (int c = 0; c < kPart / 2; c += 16) tmem_st16(s_buf + part * (kPart / 2) + c, *reinterpret_cast<uint32_t(*)[16]>(pk + c));
-                tmem_wait_st();
-                tc_fence_before_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_p + (t * 2 + part) * 8);
-            };
-            auto do_block = [&](auto masked_c) {
-                uint32_t va[kPart], vb[kPart], pk[kPart / 2];
-                float sum;
-                load(0, va);
-                tmem_wait_ld();
-                if (j == 0) {  // the reference: the row's largest logit of the first part, finite because position 0 is visible
-                    float top = -INFINITY;
-                    const int visible = my_pos + 1;
-#pragma unroll
-                    for (int c = 0; c < kPart; ++c) top = c < visible ? fmaxf(top, __uint_as_float(va[c])) : top;
-                    m_run = top * p.scale_log2;
-                }
-                load(1, vb);  // on their way while the first part's exponentials run
-                float xmax = weigh(masked_c, 0, va, pk, sum);
-                tmem_wait_ld();
-                hand_over(masked_c, 0, xmax, pk, sum);
-                xmax = weigh(masked_c, 1, vb, pk, sum);
-                hand_over(masked_c, 1, xmax, pk, sum);
-            };
-            if (__any_sync(0xffffffffu, masked)) do_block(std::true_type{});
-            else do_block(std::false_type{});
+                weigh();
+            }
+            l_run += sum;
+            if (j > 0) {  // P_t has been used by the last block's product
+                ok = ok && mbar_wait(bar_o + t * 8, (j - 1) & 1);
+                if (!ok) break;
+                tc_fence_after_sync();
+            }
+            tmem_st16(p_buf, *reinterpret_cast<uint32_t(*)[16]>(pk));
+            tmem_st16(p_buf + 16, *reinterpret_cast<uint32_t(*)[16]>(pk + 16));
+            tmem_st8(p_buf + 32, *reinterpret_cast<uint32_t(*)[8]>(pk + 32));
+            tmem_wait_st();
+            tc_fence_before_sync();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_p + t * 8);
         }
 
         // ---- epilogue: O_t / l -> bf16 rows
-        ok = ok && mbar_wait(bar_o + t * 8, 0);
+        ok = ok && mbar_wait(bar_o + t * 8, (my_nb - 1) & 1);
         tc_fence_after_sync();
         const float inv = 1.f / l_run;
         const bool wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
