@@ -79,7 +79,8 @@ struct pd_ctx {
     cudaEvent_t ev_before = nullptr, ev_after = nullptr;  // optional timing hook around the split kernel
     // a context for shared latent vectors (PD_FLAG_LATENT): its pool's and its queries' tensor maps
     bool latent = false;
-    bool latent_decode_ready = false, latent_expand_ready = false, latent_prefill_ready = false;
+    bool latent_decode_ready = false, latent_prefill_ready = false;
+    int latent_expand_pairs = 0;  // CTA pairs of the expansion's launch, once it is prepared
     const void *map_latent_ptr = nullptr, *map_latent_q_ptr = nullptr, *map_latent_w_ptr = nullptr;
     const void *map_expanded_k_ptr = nullptr, *map_expanded_v_ptr = nullptr;
     int64_t map_expanded_pages = 0;  // of both expanded pools' maps
@@ -1494,15 +1495,16 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
     if (batch == 0) return PD_OK;
     DeviceGuard guard(ctx->cfg.device);
     if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
-    if (!ctx->latent_expand_ready) {
-        const cudaError_t e = pd::prepare_kv_expand_latent();
+    if (ctx->latent_expand_pairs == 0) {
+        int n = 0;
+        const cudaError_t e = pd::prepare_kv_expand_latent(ctx->num_sms, &n);
         if (e != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent expansion kernel attribute", e);
-        ctx->latent_expand_ready = true;
+        ctx->latent_expand_pairs = n;
     }
     if (int rc = latent_map(ctx, kv_pages)) return rc;
     if (ctx->map_latent_w_ptr != w_kv) {
         const int rows = 2 * pd::kLatentHead;
-        if (int rc = encode_rows_map(ctx, w_kv, pd::kLatentDim, static_cast<int64_t>(ctx->cfg.num_q_heads) * rows, rows, &ctx->tm_latent_w)) return rc;
+        if (int rc = encode_rows_map(ctx, w_kv, pd::kLatentDim, static_cast<int64_t>(ctx->cfg.num_q_heads) * rows, pd::kLatentHead, &ctx->tm_latent_w)) return rc;
         ctx->map_latent_w_ptr = w_kv;
     }
     pd::LatentExpandParams p{};
@@ -1519,7 +1521,7 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
     p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
     p.dst_num_pages = static_cast<int32_t>(expanded_num_pages);
     p.pdl = ctx->pdl;
-    const cudaError_t err = pd::launch_kv_expand_latent(ctx->tm_latent, ctx->tm_latent_w, p, ctx->num_sms, static_cast<cudaStream_t>(stream));
+    const cudaError_t err = pd::launch_kv_expand_latent(ctx->tm_latent, ctx->tm_latent_w, p, ctx->latent_expand_pairs, static_cast<cudaStream_t>(stream));
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent expansion launch", err);
     ctx->launches += 1;
     return PD_OK;

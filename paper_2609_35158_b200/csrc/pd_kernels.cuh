@@ -294,8 +294,8 @@ int latent_heads_per_cta(int heads);         // heads the kernel is built for th
 cudaError_t prepare_decode_attn_latent();
 cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_rope, const CUtensorMap &tm_q, const LatentAttnParams &p,
                                       int num_ctas, cudaStream_t stream);
-cudaError_t prepare_kv_expand_latent();
-cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_sms,
+cudaError_t prepare_kv_expand_latent(int num_sms, int *num_pairs);  // *num_pairs: clusters of two CTAs to launch
+cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_pairs,
                                     cudaStream_t stream);
 cudaError_t prepare_prefill_attn_latent();
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,

@@ -2,11 +2,15 @@
 // from latent pages into pages of bf16 K and V. A matrix product [tokens x 512] x [512 x 256 per head] whose rows are gathered
 // by page and whose results are scattered by page.
 //
-// A unit is (tile of 128 tokens, head): 32 MMAs of 128 x 256 x 16, 4096 cycles, for 128 KB of latents, 256 KB of W (from L2)
-// and 64 KB of results. A CTA per SM walks a run of units, heads innermost: the tile's latents (8 blocks of 64 columns) stay in
-// shared memory over its heads, W streams through a ring of three 32 KB blocks, and each block of the next tile is
-// fetched as soon as the last head's product has passed it. Two accumulators of 256 columns fill tensor memory, so the products
-// of one unit run while the results of the last are stored: a thread holds a token's row and stores 32 bytes at a time.
+// A unit is (two tiles of 128 tokens, head): 32 MMAs of 256 x 256 x 16 over a pair of CTAs (a cluster), a tile in each, 4096
+// cycles, for 256 KB of latents, 256 KB of W (from L2) and 128 KB of results. Each CTA holds half of W_h, K's rows in the first
+// and V's in the second, so W crosses from L2 once per 256 tokens. With a product per CTA (128 tokens) it crosses twice as often: 64 bytes
+// a cycle into each SM, and 82K tokens x 32 heads took 579 us, 393 of them without the stores of the results.
+// A pair walks a run of units, heads innermost: a tile's latents (8 blocks of 64 columns) stay in shared memory over its heads, W
+// streams through a ring of 16 KB blocks, and each block of the next tile is fetched as soon as the last head's product has
+// passed it. Two accumulators of 256 columns fill tensor memory, so the products of one unit run while the results of the last
+// are stored: a thread holds a token's row and stores 32 bytes at a time.
+// The first CTA issues the products; the copies of both complete on its barriers.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
@@ -20,9 +24,10 @@ constexpr int kTile = 128, kTilePages = kTile / kPageSize;
 constexpr int kCols = 2 * kLatentHead;           // K and V of a head
 constexpr int kChunks = kLatentDim / 64;
 constexpr int kABytes = kTile * 128;             // 64 columns of the tile
-constexpr int kBBytes = kCols * 128;
-constexpr int kStages = 3;
-constexpr int kThreads = 128 + 64;               // store warps + TMA warp + MMA warp
+constexpr int kBBytes = kLatentHead * 128;       // 64 columns of a CTA's half of W_h
+constexpr int kStages = 5;
+constexpr int kStoreWarps = 8;                   // four for K, four for V
+constexpr int kThreads = 32 * kStoreWarps + 64;  // + TMA warp + MMA warp (idle in the second CTA)
 constexpr int kTmemCols = 512;
 constexpr int kNumBars = 2 * kChunks + 2 * kStages + 4 + 1;
 constexpr size_t kSmemBytes = 1024 + kChunks * kABytes + kStages * kBBytes + kNumBars * 8;
@@ -41,19 +46,25 @@ __device__ __forceinline__ Span span_of(const LatentExpandParams &p, int b) {
     return s;
 }
 
+// Where a CTA stands: its tile (none behind the last one) and the head.
 struct Walk {
     int b, tile, head;
     Span s;
 };
+__device__ __forceinline__ void next_tile(Walk &w, const LatentExpandParams &p) {
+    if (w.b >= p.B || ++w.tile < w.s.tiles) return;
+    w.tile = 0;
+    do {
+        w.s.first = w.s.len = w.s.page0 = w.s.tiles = 0;
+        if (++w.b >= p.B) return;
+        w.s = span_of(p, w.b);
+    } while (w.s.tiles == 0);
+}
 __device__ __forceinline__ void step(Walk &w, const LatentExpandParams &p) {
     if (++w.head < p.Hq) return;
     w.head = 0;
-    if (++w.tile < w.s.tiles) return;
-    w.tile = 0;
-    do {
-        if (++w.b >= p.B) return;  // behind the last unit
-        w.s = span_of(p, w.b);
-    } while (w.s.tiles == 0);
+    next_tile(w, p);  // the pair's other tile
+    next_tile(w, p);
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -69,15 +80,16 @@ kv_expand_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_
     const uint32_t bar_a = smem_u32(bars), bar_afree = bar_a + kChunks * 8;
     const uint32_t bar_b = bar_afree + kChunks * 8, bar_bfree = bar_b + kStages * 8;
     const uint32_t bar_d = bar_bfree + kStages * 8, bar_dfree = bar_d + 16, bar_drain = bar_dfree + 16;
+    const uint32_t rank = cluster_rank(), pairs = gridDim.x / 2, pair = blockIdx.x / 2;
     if (tid == 0) {
-        for (int i = 0; i < kNumBars; ++i) mbar_init(bar_a + i * 8, bar_a + i * 8 == bar_dfree || bar_a + i * 8 == bar_dfree + 8 ? 4 : 1);
+        for (int i = 0; i < kNumBars; ++i) mbar_init(bar_a + i * 8, bar_a + i * 8 == bar_dfree || bar_a + i * 8 == bar_dfree + 8 ? 2 * kStoreWarps : 1);
         mbar_init_fence();
         prefetch_tensormap(&tm_kv);
         prefetch_tensormap(&tm_w);
     }
     if (warp == 0) {
-        tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
-        tmem_relinquish_alloc_permit();
+        tmem_alloc_pair(smem_u32(&tmem_slot), kTmemCols);
+        tmem_relinquish_alloc_permit_pair();
     }
     grid_dependency_wait();
     launch_dependents();
@@ -112,160 +124,195 @@ kv_expand_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __grid_
         if (tid == kThreads - 1) cum[p.B] = run;
         __syncthreads();
     }
-    const long long total = static_cast<long long>(cum[p.B]) * p.Hq;
-    const long long u0 = total * blockIdx.x / gridDim.x;
-    const int units = static_cast<int>(total * (blockIdx.x + 1) / gridDim.x - u0);
+    const int n_tiles = cum[p.B];
+    const long long total = static_cast<long long>((n_tiles + 1) / 2) * p.Hq;
+    const long long u0 = total * pair / pairs;
+    const int units = static_cast<int>(total * (pair + 1) / pairs - u0);
     Walk w{};
     if (units > 0) {
-        const Cursor c = locate(cum, p.B, 1, div_positive(u0, p.Hq));
-        w.b = c.b;
-        w.tile = c.page;
-        w.head = static_cast<int>(u0 - div_positive(u0, p.Hq) * p.Hq);
-        w.s = span_of(p, c.b);
+        const long long tile_pair = div_positive(u0, p.Hq);
+        const int tile = static_cast<int>(2 * tile_pair) + static_cast<int>(rank);
+        w.head = static_cast<int>(u0 - tile_pair * p.Hq);
+        w.b = p.B;
+        if (tile < n_tiles) {
+            const Cursor c = locate(cum, p.B, 1, tile);
+            w.b = c.b;
+            w.tile = c.page;
+            w.s = span_of(p, c.b);
+        }
     }
     fence_proxy_async();  // the copies that follow overwrite what was read here
     tc_fence_before_sync();
-    __syncthreads();
+    cluster_sync();  // (the other CTA's barriers are initialised too)
     tc_fence_after_sync();
     const uint32_t tm = tmem_slot;
     bool ok = true;
 
-    if (units > 0 && warp == 4) {
-        // ================= TMA warp =================
-        const uint64_t policy = l2_policy_evict_first();
-        const int32_t oob_row = p.num_pages * kPageSize;
-        int ac = 0, bc = 0;  // blocks of latents and of W issued
-        for (int u = 0; u < units && ok; ++u) {
-            const bool new_tile = u == 0 || w.head == 0;
-            int32_t y = oob_row;
-            if (new_tile && lane < kTilePages) {
-                const int page = w.s.page0 + w.tile * kTilePages + lane;
-                if (page * kPageSize < w.s.len) {
-                    const int pid = __ldg(p.page_table + static_cast<size_t>(w.b) * p.MP + page);
-                    if (pid >= 0 && pid < p.num_pages) y = pid * kPageSize;  // (the store warps latch the others)
-                }
-            }
-            for (int c = 0; c < kChunks && ok; ++c) {
-                if (new_tile) {
-                    if (ac >= kChunks) ok = __all_sync(0xffffffffu, mbar_wait(bar_afree + c * 8, (ac / kChunks - 1) & 1));
-                    if (!ok) break;
-                    if (lane == 0) mbar_arrive_expect_tx(bar_a + c * 8, kABytes);
-                    __syncwarp();
-                    if (lane < kTilePages) tma_load_2d(a_s + c * kABytes + lane * (kPageSize * 128), &tm_kv, c * 64, y, bar_a + c * 8, policy);
-                    ++ac;
-                }
-                const int slot = bc % kStages, fill = bc / kStages;
-                if (fill > 0) ok = __all_sync(0xffffffffu, mbar_wait(bar_bfree + slot * 8, (fill - 1) & 1));
-                if (!ok) break;
-                if (lane == 0) {
-                    mbar_arrive_expect_tx(bar_b + slot * 8, kBBytes);
-                    tma_load_2d(b_ring + slot * kBBytes, &tm_w, c * 64, w.head * kCols, bar_b + slot * 8, l2_policy_evict_last());
-                }
-                __syncwarp();
-                ++bc;
-            }
-            step(w, p);
-        }
-        if (!ok) {  // copies in flight have to land before the block's memory goes
-            if (lane == 0) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
-            for (int i = max(0, bc - kStages); i < bc; ++i) mbar_wait(bar_b + (i % kStages) * 8, (i / kStages) & 1);
-            for (int i = max(0, ac - kChunks); i < ac; ++i) mbar_wait(bar_a + (i % kChunks) * 8, (i / kChunks) & 1);
-        }
-    } else if (units > 0 && warp == 5) {
-        // ================= MMA warp: one elected thread =================
+    if (units > 0 && warp == kStoreWarps) {
+        // ================= TMA warp: one elected thread =================
         if (elect_one()) {
-            constexpr uint32_t idesc = umma_idesc_bf16(kTile, kCols, false);
+            const uint64_t policy = l2_policy_evict_first(), keep = l2_policy_evict_last();
+            const int32_t oob_row = p.num_pages * kPageSize;  // a box that starts here is all zero fill
+            const uint32_t a_full = cluster_address(bar_a, 0), b_full = cluster_address(bar_b, 0);
+            int ac = 0, bc = 0;  // blocks of latents and of W issued
+            for (int u = 0; u < units && ok; ++u) {
+                const bool new_tile = u == 0 || w.head == 0;
+                int32_t y[kTilePages];
+                if (new_tile) {
+#pragma unroll
+                    for (int g = 0; g < kTilePages; ++g) {
+                        const int page = w.s.page0 + w.tile * kTilePages + g;
+                        const int pid = w.b < p.B && page * kPageSize < w.s.len ? __ldg(p.page_table + static_cast<size_t>(w.b) * p.MP + page) : -1;
+                        y[g] = pid >= 0 && pid < p.num_pages ? pid * kPageSize : oob_row;  // (the store warps latch bad ids)
+                    }
+                }
+                for (int c = 0; c < kChunks && ok; ++c) {
+                    if (new_tile) {
+                        if (ac >= kChunks) ok = mbar_wait(bar_afree + c * 8, (ac / kChunks - 1) & 1);
+                        if (!ok) break;
+                        if (rank == 0) mbar_arrive_expect_tx(bar_a + c * 8, 2 * kABytes);
+#pragma unroll
+                        for (int g = 0; g < kTilePages; ++g)
+                            tma_load_2d_pair(a_s + c * kABytes + g * (kPageSize * 128), &tm_kv, c * 64, y[g], a_full + c * 8, policy);
+                        ++ac;
+                    }
+                    const int slot = bc % kStages, fill = bc / kStages;
+                    if (fill > 0) ok = mbar_wait(bar_bfree + slot * 8, (fill - 1) & 1);
+                    if (!ok) break;
+                    if (rank == 0) mbar_arrive_expect_tx(bar_b + slot * 8, 2 * kBBytes);
+                    tma_load_2d_pair(b_ring + slot * kBBytes, &tm_w, c * 64, w.head * kCols + static_cast<int>(rank) * kLatentHead, b_full + slot * 8, keep);
+                    ++bc;
+                }
+                step(w, p);
+            }
+            if (!ok) {
+                latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
+                if (rank == 0) {  // copies in flight, the other CTA's among them, have to land before the pair's memory goes
+                    for (int i = max(0, bc - kStages); i < bc; ++i) mbar_wait(bar_b + (i % kStages) * 8, (i / kStages) & 1);
+                    for (int i = max(0, ac - kChunks); i < ac; ++i) mbar_wait(bar_a + (i % kChunks) * 8, (i / kChunks) & 1);
+                }
+            }
+        }
+    } else if (units > 0 && warp == kStoreWarps + 1 && rank == 0) {
+        // ================= MMA warp of the first CTA: one elected thread =================
+        if (elect_one()) {
+            constexpr uint32_t idesc = umma_idesc_bf16(2 * kTile, kCols, false);
             const uint64_t a_desc = umma_smem_desc(a_s, 16, 1024), b_desc = umma_smem_desc(b_ring, 16, 1024);
             int tiles = 0, bc = 0;
             for (int u = 0; u < units && ok; ++u) {
                 const bool new_tile = u == 0 || w.head == 0, last_head = u == units - 1 || w.head == p.Hq - 1;
                 if (new_tile) ++tiles;
-                if (u >= 2) ok = mbar_wait(bar_dfree + (u & 1) * 8, ((u >> 1) - 1) & 1);
+                if (u >= 2) ok = mbar_wait_cluster(bar_dfree + (u & 1) * 8, ((u >> 1) - 1) & 1);
                 const uint32_t d = tm + (u & 1) * kCols;
 #pragma unroll
                 for (int c = 0; c < kChunks; ++c) {
                     const int slot = bc % kStages;
-                    if (new_tile) ok = ok && mbar_wait(bar_a + c * 8, (tiles - 1) & 1);
-                    ok = ok && mbar_wait(bar_b + slot * 8, (bc / kStages) & 1);
+                    if (new_tile) ok = ok && mbar_wait_cluster(bar_a + c * 8, (tiles - 1) & 1);
+                    ok = ok && mbar_wait_cluster(bar_b + slot * 8, (bc / kStages) & 1);
                     if (!ok) break;
                     tc_fence_after_sync();
 #pragma unroll
                     for (int ks = 0; ks < 4; ++ks)
-                        umma_ss(d, a_desc + (c * kABytes >> 4) + ks * 2, b_desc + slot * (kBBytes >> 4) + ks * 2, idesc, (c | ks) != 0);
-                    umma_commit(bar_bfree + slot * 8);
-                    if (last_head) umma_commit(bar_afree + c * 8);
+                        umma_ss_pair(d, a_desc + (c * kABytes >> 4) + ks * 2, b_desc + slot * (kBBytes >> 4) + ks * 2, idesc, (c | ks) != 0);
+                    umma_commit_pair(bar_bfree + slot * 8);
+                    if (last_head) umma_commit_pair(bar_afree + c * 8);
                     ++bc;
                 }
                 if (!ok) break;
-                umma_commit(bar_d + (u & 1) * 8);
+                umma_commit_pair(bar_d + (u & 1) * 8);
                 step(w, p);
             }
             if (!ok) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
-            umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
+            umma_commit_pair(bar_drain);  // nothing may be in flight when the tensor memory is freed
             mbar_wait(bar_drain, 0);
         }
-    } else if (units > 0 && warp < 4) {
-        // ================= store warps: thread = token of the tile =================
-        const uint32_t lane_base = static_cast<uint32_t>(warp * 32) << 16;
-        __nv_bfloat16 *k_dst = nullptr, *v_dst = nullptr;
+    } else if (units > 0 && warp < kStoreWarps) {
+        // ================= store warps: thread = token of the tile, K (first four warps) or V =================
+        const uint32_t lane_base = static_cast<uint32_t>((warp & 3) * 32) << 16;
+        const int half = warp >> 2, row = tid & (kTile - 1);
+        const uint32_t dfree = cluster_address(bar_dfree, 0);
+        __nv_bfloat16 *dst0 = nullptr;
         for (int u = 0; u < units && ok; ++u) {
-            if (u == 0 || w.head == 0) {  // where this token's rows of head 0 go, if anywhere
-                const int tok = (w.s.page0 + w.tile * kTilePages) * kPageSize + tid, page = tok / kPageSize;
-                k_dst = v_dst = nullptr;
-                if (tok >= w.s.first && tok < w.s.len) {
+            if (u == 0 || w.head == 0) {  // where this token's row of head 0 goes, if anywhere
+                const int tok = (w.s.page0 + w.tile * kTilePages) * kPageSize + row, page = tok / kPageSize;
+                dst0 = nullptr;
+                if (w.b < p.B && tok >= w.s.first && tok < w.s.len) {
                     const int from = __ldg(p.page_table + static_cast<size_t>(w.b) * p.MP + page);
                     const int to = __ldg(p.dst_table + static_cast<size_t>(w.b) * p.MP + page);
                     if (from < 0 || from >= p.num_pages) latch_status(p.status, kDevBadPage, w.b, from);
                     else if (to < 0 || to >= p.dst_num_pages) latch_status(p.status, kDevBadPage, w.b, to);
-                    else {
-                        const size_t at = (static_cast<size_t>(to) * p.Hq * kPageSize + tok % kPageSize) * kLatentHead;
-                        k_dst = p.k_pages + at;
-                        v_dst = p.v_pages + at;
-                    }
+                    else dst0 = (half == 0 ? p.k_pages : p.v_pages) + (static_cast<size_t>(to) * p.Hq * kPageSize + tok % kPageSize) * kLatentHead;
                 }
             }
             ok = mbar_wait(bar_d + (u & 1) * 8, (u >> 1) & 1);
             if (!ok) break;
             tc_fence_after_sync();
+            __nv_bfloat16 *dst = dst0 + static_cast<size_t>(w.head) * kPageSize * kLatentHead;
 #pragma unroll
-            for (int c = 0; c < kCols / 32; ++c) {
+            for (int c = 0; c < kLatentHead / 32; ++c) {
                 uint32_t o[32];
-                tmem_ld32(tm + lane_base + (u & 1) * kCols + c * 32, o);
+                tmem_ld32(tm + lane_base + (u & 1) * kCols + half * kLatentHead + c * 32, o);
                 tmem_wait_ld();
-                if (k_dst != nullptr) {
-                    __nv_bfloat16 *dst = (c < kLatentHead / 32 ? k_dst : v_dst) + static_cast<size_t>(w.head) * kPageSize * kLatentHead + (c % (kLatentHead / 32)) * 32;
+                if (dst0 != nullptr) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         uint32_t v[8];
 #pragma unroll
                         for (int i = 0; i < 8; ++i)
                             v[i] = pack_bf16x2(__uint_as_float(o[h * 16 + 2 * i]), __uint_as_float(o[h * 16 + 2 * i + 1]));
-                        store32(dst + h * 16, v);
+                        store32(dst + c * 32 + h * 16, v);
                     }
                 }
             }
             tc_fence_before_sync();
             __syncwarp();
-            if (lane == 0) mbar_arrive(bar_dfree + (u & 1) * 8);
+            if (lane == 0) mbar_arrive_relaxed(dfree + (u & 1) * 8);
             step(w, p);
         }
         if (!ok && lane == 0) latch_status(p.status, kDevTimeout, w.b, blockIdx.x);
     }
     __syncwarp();
     tc_fence_before_sync();
-    __syncthreads();
-    if (warp == 0) tmem_dealloc(tm, kTmemCols);
+    cluster_sync();  // neither CTA leaves while the other may still use its memory and barriers
+    if (warp == 0) tmem_dealloc_pair(tm, kTmemCols);
 }
 
 }  // namespace
 
-cudaError_t prepare_kv_expand_latent() {
-    return cudaFuncSetAttribute(kv_expand_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+// The pairs that fit the device at once (a cluster needs two free SMs of one GPC); the launch is that many.
+cudaError_t prepare_kv_expand_latent(int num_sms, int *num_pairs) {
+    cudaError_t e = cudaFuncSetAttribute(kv_expand_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+    cfg.gridDim = dim3(num_sms / 2 * 2);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaOccupancyMaxActiveClusters(num_pairs, kv_expand_latent_kernel, &cfg);
+    if (e == cudaSuccess && *num_pairs < 1) e = cudaErrorInvalidConfiguration;
+    if (e == cudaSuccess && *num_pairs > num_sms / 2) *num_pairs = num_sms / 2;
+    return e;
 }
 
-cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_sms,
+cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_pairs,
                                     cudaStream_t stream) {
-    return launch_pdl(kv_expand_latent_kernel, dim3(num_sms), dim3(kThreads), kSmemBytes, stream, p.pdl != 0, tm_kv, tm_w, p);
+    cudaLaunchConfig_t cfg{};
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 2, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+    attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[1].val.programmaticStreamSerializationAllowed = 1;
+    cfg.gridDim = dim3(2 * num_pairs);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = kSmemBytes;
+    cfg.stream = stream;
+    cfg.attrs = attr;
+    cfg.numAttrs = p.pdl != 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kv_expand_latent_kernel, tm_kv, tm_w, p);
 }
 
 }  // namespace pd
