@@ -426,10 +426,11 @@ def _row_strides(t, name: str):
     """(token stride, head stride) of rows [tokens, heads, 64] that may lie inside wider ones."""
     if t is None:
         return 0, 0
-    if t.dim() != 3 or t.shape[-1] != 64 or t.stride(-1) != 1:
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[2] != 64 or stride[2] != 1:
         raise ValueError(f"{name}: [tokens, heads, 64] with neighbouring values is needed")
-    head = t.stride(1) if t.shape[1] > 1 else 64                      # the stride of an axis of one means nothing
-    return (t.stride(0) if t.shape[0] > 1 else t.shape[1] * head), head
+    head = stride[1] if shape[1] > 1 else 64                      # the stride of an axis of one means nothing
+    return (stride[0] if shape[0] > 1 else shape[1] * head), head
 
 
 def pd_rope_append_tokens_latent(ctx, rope, positions, q_rope, kv_new, norm_weight, norm_eps, q_indptr, q_out, kv_pages, page_table,
@@ -438,9 +439,10 @@ def pd_rope_append_tokens_latent(ctx, rope, positions, q_rope, kv_new, norm_weig
     [tokens, 576], possibly inside wider rows; ``norm_weight`` [512] and ``positions`` may be None."""
     batch = q_indptr.shape[0] - 1 if batch is None else batch
     needed = batch > 0 and max_q_len > 0
-    if kv_new.dim() != 2 or kv_new.shape[-1] != 576 or kv_new.stride(-1) != 1:
+    shape, stride = kv_new.shape, kv_new.stride()
+    if len(shape) != 2 or shape[1] != 576 or stride[1] != 1:
         raise ValueError("kv_new: [tokens, 576] with neighbouring values is needed")
-    kv_stride = kv_new.stride(0) if kv_new.shape[0] > 1 else 576
+    kv_stride = stride[0] if shape[0] > 1 else 576
     _check(_lib.pd_rope_append_tokens_latent(
         ctx, ctypes.byref(rope), _optional_ptr(positions, needed, "positions"), _position_stride(positions, rope),
         _optional_ptr(q_rope, needed, "q_rope"), *_row_strides(q_rope, "q_rope"), _ptr(kv_new), kv_stride,

@@ -20,32 +20,40 @@ __device__ __forceinline__ void latch(int32_t *status, int code, int seq, int de
 }
 
 constexpr int kThreads = 256;
-constexpr int kMaxTile = 8;
+constexpr int kMaxTile = kThreads / 32;  // tokens a CTA takes at a time: a warp per latent
+constexpr int kFlight = 2;               // rotated rows of a lane group in flight
 constexpr int kPairs = kLatentRope / 2;
 
-// eight values of a row that rotate against eight others (halves), pairs 8 j ..
-__device__ __forceinline__ void rotate_halves(uint4 &x, uint4 &y, const float2 *cs) {
+// (cos, sin) of a token, two pairs per entry, so that the lanes of a row read neighbouring entries. Halves: entry 4 k + u holds pairs
+// 8 u + 2 k and 8 u + 2 k + 1 (lane u's); adjacent: entry 8 k + u pairs 4 u + 2 k and 4 u + 2 k + 1 (piece u's).
+__device__ __forceinline__ int turns_at(int i, bool adjacent) {  // where pair i lies, as an index of float2
+    return adjacent ? (8 * ((i & 3) >> 1) + (i >> 2)) * 2 + (i & 1) : (4 * ((i & 7) >> 1) + (i >> 3)) * 2 + (i & 1);
+}
+// eight values of a row that rotate against eight others (halves), lane u
+__device__ __forceinline__ void rotate_halves(uint4 &x, uint4 &y, const float4 *cs) {
     uint32_t *a = &x.x, *b = &y.x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float a0 = bf16_lo(a[k]), a1 = bf16_hi(a[k]), b0 = bf16_lo(b[k]), b1 = bf16_hi(b[k]);
-        const float2 u = cs[2 * k], v = cs[2 * k + 1];
-        a[k] = pack_bf16x2(a0 * u.x - b0 * u.y, a1 * v.x - b1 * v.y);
-        b[k] = pack_bf16x2(a0 * u.y + b0 * u.x, a1 * v.y + b1 * v.x);
+        const float4 t = cs[4 * k];
+        a[k] = pack_bf16x2(a0 * t.x - b0 * t.y, a1 * t.z - b1 * t.w);
+        b[k] = pack_bf16x2(a0 * t.y + b0 * t.x, a1 * t.w + b1 * t.z);
     }
 }
-// eight values that are four adjacent pairs
-__device__ __forceinline__ void rotate_adjacent(uint4 &x, const float2 *cs) {
+// eight values that are four adjacent pairs, piece u
+__device__ __forceinline__ void rotate_adjacent(uint4 &x, const float4 *cs) {
     uint32_t *a = &x.x;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float u = bf16_lo(a[k]), v = bf16_hi(a[k]);
-        a[k] = pack_bf16x2(u * cs[k].x - v * cs[k].y, u * cs[k].y + v * cs[k].x);
+        const float4 t = cs[8 * (k >> 1)];
+        const float c = (k & 1) ? t.z : t.x, s = (k & 1) ? t.w : t.y;
+        a[k] = pack_bf16x2(u * c - v * s, u * s + v * c);
     }
 }
 
-__global__ void __launch_bounds__(kThreads) rope_append_latent_kernel(const __grid_constant__ LatentAppendParams p) {
-    __shared__ float2 turns[kMaxTile][kPairs];
+__global__ void __launch_bounds__(kThreads, 4) rope_append_latent_kernel(const __grid_constant__ LatentAppendParams p) {
+    __shared__ float4 turns[kMaxTile][kPairs / 2];
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 31;
     grid_dependency_wait();
     launch_dependents();
@@ -68,78 +76,102 @@ __global__ void __launch_bounds__(kThreads) rope_append_latent_kernel(const __gr
         }
         return p.kv_pages + (static_cast<size_t>(page) * kPageSize + pos % kPageSize) * kLatentRow;
     };
+    const int rows = 1 + (p.q != nullptr ? p.Hq : 0), j = tid & 3;
+    // halves: pieces of 8 values c0 and c1 = c0 + rot_dim / 16 rotate against each other, then the rest is copied
+    const int pieces = p.rot_dim / 16;
+    const int c0 = p.adjacent ? j : (j < pieces ? j : pieces + j), c1 = p.adjacent ? j + 4 : (j < pieces ? j + pieces : j + 4);
     for (int i0 = blockIdx.x * p.tile; i0 < n; i0 += gridDim.x * p.tile) {
         const int nt = min(p.tile, n - i0);
-        for (int x = tid; x < nt * kPairs; x += kThreads) {
-            const int u = x / kPairs, i = x % kPairs;
-            float sn = 0.f, c = 1.f, mag = 1.f;
+        // ---- this lane group's first rotated rows (the key's is row 0 of a token) and this warp's latent are on their way while the
+        // sines are computed
+        int x = tid >> 2, at_u[kFlight];
+        uint4 a[kFlight], c[kFlight];
+        __nv_bfloat16 *to[kFlight];
+        auto fetch = [&]() {
+#pragma unroll
+            for (int f = 0; f < kFlight; ++f, x += kThreads / 4) {
+                to[f] = nullptr;
+                if (x >= nt * rows) continue;
+                const int u = x / rows, r = x - u * rows;
+                const long long row = r0 + i0 + u;
+                const __nv_bfloat16 *from;
+                at_u[f] = u;
+                if (r == 0) {
+                    from = p.kv_new + row * p.kv_stride + kLatentDim;
+                    to[f] = row_of(i0 + u);
+                    if (to[f] == nullptr) continue;
+                    to[f] += kLatentDim;
+                } else {
+                    from = p.q + row * p.q_token_stride + (r - 1) * p.q_head_stride;
+                    to[f] = p.q_out + row * p.q_out_token_stride + (r - 1) * p.q_out_head_stride;
+                }
+                a[f] = reinterpret_cast<const uint4 *>(from)[c0];
+                c[f] = reinterpret_cast<const uint4 *>(from)[c1];
+            }
+        };
+        fetch();
+        const int lt = tid >> 5;  // the token whose latent this warp takes
+        uint4 v[2];
+        __nv_bfloat16 *latent_to = nullptr;
+        if (lt < nt) {
+            const uint4 *src = reinterpret_cast<const uint4 *>(p.kv_new + (r0 + i0 + lt) * p.kv_stride);
+            v[0] = src[lane], v[1] = src[lane + 32];
+            latent_to = row_of(i0 + lt);
+        }
+        for (int y = tid; y < nt * kPairs; y += kThreads) {
+            const int u = y / kPairs, i = y % kPairs;
+            float sn = 0.f, cs = 1.f, mag = 1.f;
             if (i < half) {
                 const long long pos = p.positions != nullptr ? p.positions[p.axis_of_pair[i] * p.position_stride + r0 + i0 + u] : L + i0 + u;
                 const uint64_t turn = static_cast<uint64_t>(pos) * p.freq[i];
-                sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 4.656612873077393e-10f, &sn, &c);  // 2^-31: half turns
+                sincospif(static_cast<float>(static_cast<int32_t>(turn >> 32)) * 4.656612873077393e-10f, &sn, &cs);  // 2^-31: half turns
                 mag = p.magnitude;
             }
-            turns[u][i] = make_float2(c * mag, sn * mag);
+            reinterpret_cast<float2 *>(turns[u])[turns_at(i, p.adjacent != 0)] = make_float2(cs * mag, sn * mag);
         }
         // ---- latents: a warp per token
-        for (int u = tid >> 5; u < nt; u += kThreads / 32) {
-            __nv_bfloat16 *dst = row_of(i0 + u);
-            const uint4 *src = reinterpret_cast<const uint4 *>(p.kv_new + (r0 + i0 + u) * p.kv_stride);
-            uint4 v[2] = {src[lane], src[lane + 32]};
-            if (p.norm_weight != nullptr) {
-                float f[16], ss = 0.f;
+        if (lt < nt && p.norm_weight != nullptr) {
+            float f[16], ss = 0.f;
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint32_t w = (&v[k >> 2].x)[k & 3];
-                    f[2 * k] = bf16_lo(w), f[2 * k + 1] = bf16_hi(w);
-                    ss = fmaf(f[2 * k], f[2 * k], ss);
-                    ss = fmaf(f[2 * k + 1], f[2 * k + 1], ss);
-                }
-#pragma unroll
-                for (int o = 16; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
-                const float inv = rsqrtf(ss * (1.f / kLatentDim) + p.norm_eps);
-                const uint4 *wt = reinterpret_cast<const uint4 *>(p.norm_weight);
-                const uint4 g[2] = {wt[lane], wt[lane + 32]};
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint32_t w = (&g[k >> 2].x)[k & 3];
-                    (&v[k >> 2].x)[k & 3] = pack_bf16x2(f[2 * k] * inv * bf16_lo(w), f[2 * k + 1] * inv * bf16_hi(w));
-                }
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t w = (&v[k >> 2].x)[k & 3];
+                f[2 * k] = bf16_lo(w), f[2 * k + 1] = bf16_hi(w);
+                ss = fmaf(f[2 * k], f[2 * k], ss);
+                ss = fmaf(f[2 * k + 1], f[2 * k + 1], ss);
             }
-            if (dst != nullptr) {
-                reinterpret_cast<uint4 *>(dst)[lane] = v[0];
-                reinterpret_cast<uint4 *>(dst)[lane + 32] = v[1];
+#pragma unroll
+            for (int o = 16; o >= 1; o >>= 1) ss += __shfl_xor_sync(0xffffffffu, ss, o);
+            const float inv = rsqrtf(ss * (1.f / kLatentDim) + p.norm_eps);
+            const uint4 *wt = reinterpret_cast<const uint4 *>(p.norm_weight);
+            const uint4 g[2] = {wt[lane], wt[lane + 32]};
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const uint32_t w = (&g[k >> 2].x)[k & 3];
+                (&v[k >> 2].x)[k & 3] = pack_bf16x2(f[2 * k] * inv * bf16_lo(w), f[2 * k + 1] * inv * bf16_hi(w));
             }
         }
+        if (latent_to != nullptr) {
+            reinterpret_cast<uint4 *>(latent_to)[lane] = v[0];
+            reinterpret_cast<uint4 *>(latent_to)[lane + 32] = v[1];
+        }
         __syncthreads();  // the sines
-        // ---- rotated rows: the key part (row 0 of a token) and the queries, four lanes each
-        const int rows = 1 + (p.q != nullptr ? p.Hq : 0), j = tid & 3;
-        for (int x = tid >> 2; x < nt * rows; x += kThreads / 4) {
-            const int u = x / rows, r = x - u * rows;
-            const long long row = r0 + i0 + u;
-            const __nv_bfloat16 *from;
-            __nv_bfloat16 *to;
-            if (r == 0) {
-                from = p.kv_new + row * p.kv_stride + kLatentDim;
-                to = row_of(i0 + u);
-                if (to == nullptr) continue;
-                to += kLatentDim;
-            } else {
-                from = p.q + row * p.q_token_stride + (r - 1) * p.q_head_stride;
-                to = p.q_out + row * p.q_out_token_stride + (r - 1) * p.q_out_head_stride;
+        // ---- rotated rows, four lanes each
+        for (;;) {
+#pragma unroll
+            for (int f = 0; f < kFlight; ++f) {
+                if (to[f] == nullptr) continue;
+                const float4 *cs = turns[at_u[f]];
+                if (p.adjacent) {
+                    if (8 * c0 < p.rot_dim) rotate_adjacent(a[f], cs + c0);
+                    if (8 * c1 < p.rot_dim) rotate_adjacent(c[f], cs + c1);
+                } else if (j < pieces) {
+                    rotate_halves(a[f], c[f], cs + j);
+                }
+                reinterpret_cast<uint4 *>(to[f])[c0] = a[f];
+                reinterpret_cast<uint4 *>(to[f])[c1] = c[f];
             }
-            // halves: pieces of 8 values c0 and c1 = c0 + rot_dim / 16 rotate against each other, then the rest is copied
-            const int pieces = p.rot_dim / 16;
-            const int c0 = p.adjacent ? j : (j < pieces ? j : pieces + j), c1 = p.adjacent ? j + 4 : (j < pieces ? j + pieces : j + 4);
-            uint4 a = reinterpret_cast<const uint4 *>(from)[c0], c = reinterpret_cast<const uint4 *>(from)[c1];
-            if (p.adjacent) {
-                if (8 * c0 < p.rot_dim) rotate_adjacent(a, &turns[u][4 * c0]);
-                if (8 * c1 < p.rot_dim) rotate_adjacent(c, &turns[u][4 * c1]);
-            } else if (j < pieces) {
-                rotate_halves(a, c, &turns[u][8 * j]);
-            }
-            reinterpret_cast<uint4 *>(to)[c0] = a;
-            reinterpret_cast<uint4 *>(to)[c1] = c;
+            if (x >= nt * rows) break;
+            fetch();
         }
         __syncthreads();
     }
