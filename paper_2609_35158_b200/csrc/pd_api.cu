@@ -1574,10 +1574,11 @@ int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, 
     p.a.order = ctx->cum_pages;  // the decode kernel's prefix-sum buffer is free here
     p.kv_table = expanded_table;
     p.kv_num_pages = static_cast<int32_t>(expanded_num_pages);
-    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len,
+    int launched = 0;
+    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len, &launched,
                                                            static_cast<cudaStream_t>(stream));
+    ctx->launches += launched;
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent prefill launch", err);
-    ctx->launches += 2;
     return PD_OK;
 }
 

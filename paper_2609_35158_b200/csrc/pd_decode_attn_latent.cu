@@ -124,7 +124,7 @@ __device__ __forceinline__ LatentPlan latent_plan(int total, int workers, const 
     pl.total = total;
     int size = p.a.split_pages > 0 ? p.a.split_pages : max((total + workers - 1) / workers, p.a.min_pages_auto);
     size = max(size, (total + p.a.max_ranges - 1) / p.a.max_ranges);
-    pl.size = max(size, 1);
+    pl.size = max(min(size, total), 1);  // (total + size stays in 32 bits whatever split_pages is)
     pl.ranges = (total + pl.size - 1) / pl.size;
     pl.per_worker = (pl.ranges + workers - 1) / workers;
     return pl;
@@ -270,35 +270,86 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
         tmem_alloc(smem_u32(&tmem_slot), kTmemCols);
         tmem_relinquish_alloc_permit();
     }
+    tc_fence_before_sync();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tm = tmem_slot;
     grid_dependency_wait();
     launch_dependents();
 
-    // ---- the plan: prefix sums in the ring's memory, which no copy uses yet
-    int32_t *cum = reinterpret_cast<int32_t *>(aligned);
-    const int pages = scan_units(p, cum, warp_sums);
-    const LatentPlan pl = latent_plan(cum[p.a.B], workers, p);
+    // ---- the plan. Up to 128 sequences every warp derives it by itself; beyond that the block does, with prefix sums in the
+    // ring's memory, which no copy uses yet (1 us more).
+    LatentPlan pl;
     Walk w0{};
-    w0.r = worker * pl.per_worker;
+    w0.b = -1;
+    const bool warp_plan = p.a.B <= 128;
+    int32_t *cum = reinterpret_cast<int32_t *>(aligned);
+    int pages = 0;
+    if (warp_plan) {
+        int units[4], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int b = lane * 4 + i, L = b < p.a.B ? __ldg(p.a.ctx_lens + b) : 0;
+            if (blockIdx.x == 0 && warp == 0 && (L < 0 || L > p.a.MP * kPageSize)) latch_status(p.a.status, kDevBadLength, b, L);
+            const int np = (clamp_len(L, p.a.MP) + kPageSize - 1) / kPageSize;
+            units[i] = units_of(np, p.extra);
+            sum += units[i];
+            pages += np;
+        }
+        int incl = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        pl = latent_plan(__shfl_sync(0xffffffffu, incl, 31), workers, p);
+        w0.r = worker * pl.per_worker;
+        const int x = min(w0.r, pl.ranges) * pl.size;  // the worker's first unit: in this lane's sequences where it lies in [incl - sum, incl)
+        int at = incl - sum, mine = -1, off = 0, in = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (x >= at && x < at + units[i]) mine = lane * 4 + i, off = x - at, in = units[i];
+            if (blockIdx.x == 0 && warp == 0 && lane * 4 + i <= p.a.B) p.a.cum_pages[lane * 4 + i] = at;
+            at += units[i];
+        }
+        if (blockIdx.x == 0 && warp == 0 && lane == 31 && p.a.B == 128) p.a.cum_pages[128] = at;
+        const uint32_t owner = __ballot_sync(0xffffffffu, mine >= 0);
+        if (owner != 0) {
+            const int src = __ffs(owner) - 1;
+            w0.b = __shfl_sync(0xffffffffu, mine, src);
+            w0.at = __shfl_sync(0xffffffffu, off, src);
+            w0.np = __shfl_sync(0xffffffffu, in, src) - p.extra;
+        }
+    } else {
+        pages = scan_units(p, cum, warp_sums);
+        pl = latent_plan(cum[p.a.B], workers, p);
+        w0.r = worker * pl.per_worker;
+        if (w0.r < pl.ranges) {
+            const Cursor c = locate(cum, p.a.B, 1, static_cast<long long>(w0.r) * pl.size);
+            w0.b = c.b;
+            w0.at = c.page;
+            w0.np = c.np - p.extra;
+        }
+        if (blockIdx.x == 0)
+            for (int i = tid; i <= p.a.B; i += kThreads) p.a.cum_pages[i] = cum[i];
+    }
     w0.r_end = min(w0.r + pl.per_worker, pl.ranges);
     const bool busy = w0.r < w0.r_end;
     if (busy) {
-        const Cursor c = locate(cum, p.a.B, 1, static_cast<long long>(w0.r) * pl.size);
-        w0.b = c.b;
-        w0.at = c.page;
-        w0.np = c.np - p.extra;
-        w0.len = clamp_len(__ldg(p.a.ctx_lens + c.b), p.a.MP);
+        w0.len = clamp_len(__ldg(p.a.ctx_lens + w0.b), p.a.MP);
         w0.left = min(pl.size, pl.total - w0.r * pl.size);
     }
     if (blockIdx.x == 0) {
-        for (int i = tid; i <= p.a.B; i += kThreads) p.a.cum_pages[i] = cum[i];
-        int sum = __reduce_add_sync(0xffffffffu, pages);
-        __syncthreads();
-        if (lane == 0) warp_sums[warp] = sum;
-        __syncthreads();
+        const int sum = __reduce_add_sync(0xffffffffu, pages);
+        if (!warp_plan) {
+            __syncthreads();
+            if (lane == 0) warp_sums[warp] = sum;
+            __syncthreads();
+        }
         if (tid == 0) {
-            sum = 0;
-            for (int i = 0; i < kThreads / 32; ++i) sum += warp_sums[i];
-            p.a.plan[0] = sum;
+            int all = sum;
+            for (int i = 1; i < kThreads / 32 && !warp_plan; ++i) all += warp_sums[i];
+            p.a.plan[0] = all;
             p.a.plan[1] = 0;
             p.a.plan[2] = 1;
             p.a.plan[3] = pl.ranges;
@@ -306,11 +357,10 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             p.a.plan[kPlanHeaderWords + 2] = pl.size;
         }
     }
-    fence_proxy_async();  // the copies that follow overwrite what was read here
-    tc_fence_before_sync();
-    __syncthreads();
-    tc_fence_after_sync();
-    const uint32_t tm = tmem_slot;
+    if (!warp_plan) {
+        fence_proxy_async();  // the copies that follow overwrite what was read here
+        __syncthreads();
+    }
     bool ok = true;
 
     if (busy && warp == kSoftmaxWarps) {
@@ -657,101 +707,95 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     if (warp == 0) tmem_dealloc(tm, kTmemCols);
 }
 
-// The running sums of a merge: what a thread holds of a row and how a partial joins it.
-template <int VECS>
-struct Joined {
-    float m = -INFINITY, l = 0.f, lr = 0.f;
-    float4 o[VECS];
-    __device__ __forceinline__ Joined() {
-#pragma unroll
-        for (int v = 0; v < VECS; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    }
-    __device__ __forceinline__ void raise(float top) {
-        const float keep = m == top ? 1.f : fast_exp2(m - top);
-#pragma unroll
-        for (int v = 0; v < VECS; ++v) o[v].x *= keep, o[v].y *= keep, o[v].z *= keep, o[v].w *= keep;
-        l *= keep, lr *= keep;
-        m = top;
-    }
-    __device__ __forceinline__ void join(float pm, float pl, float plr, const float4 (&x)[VECS]) {
-        const float a = fast_exp2(pm - m);
-#pragma unroll
-        for (int v = 0; v < VECS; ++v)
-            o[v].x = fmaf(a, x[v].x, o[v].x), o[v].y = fmaf(a, x[v].y, o[v].y), o[v].z = fmaf(a, x[v].z, o[v].z), o[v].w = fmaf(a, x[v].w, o[v].w);
-        l = fmaf(a, pl, l);
-        lr = fmaf(a, plr, lr);
-    }
-};
-
-// Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A row is held by
-// LANES threads, 512 / LANES values each. Where rows are few and partials many, PARTS sets of threads share a row's partials;
-// where rows are many, a warp takes a row. (Measured, 64 sequences of 2K-16K with 128 heads: 8 us with a warp per row, 13
-// with four sets of 128 threads; 4 sequences of 32K-64K with 32 heads: 8 and 5.)
-template <int LANES, int PARTS>
-__global__ void __launch_bounds__(LANES == 32 ? 256 : LANES * PARTS) latent_merge_kernel(const LatentAttnParams p) {
-    constexpr int VECS = kLatentDim / 4 / LANES, U = 4;  // U partials in flight
-    __shared__ float4 part_o[PARTS > 1 ? PARTS : 1][LANES];
-    __shared__ float part_m[PARTS], part_l[PARTS], part_lr[PARTS];
-    const int set = threadIdx.x / LANES, lane = threadIdx.x % LANES, part = PARTS > 1 ? set : 0;
+// Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A warp takes
+// VECS * 128 / GROUPS columns of a row: 32 / GROUPS lanes of VECS times 4 values each. Where rows are few and partials many, GROUPS sets of
+// lanes share the row's partials and join by shuffles. No shared memory and few registers, so that its blocks stand beside the
+// split kernel's on the same SM and wait there for its end.
+constexpr int kMergeThreads = 128;
+template <int GROUPS, int VECS>
+__global__ void __launch_bounds__(kMergeThreads) latent_merge_kernel(const LatentAttnParams p) {
+    constexpr int LANES = 32 / GROUPS, PIECES = kLatentDim / 4 / LANES / VECS, U = VECS == 1 ? 6 : 4;  // U partials in flight
+    const int lane = threadIdx.x & 31, group = lane / LANES;
     grid_dependency_wait();
     launch_dependents();
-    const int size = p.a.plan[kPlanHeaderWords + 2], rows = p.a.B * p.a.Hq;
-    const int per_block = PARTS > 1 ? 1 : blockDim.x / LANES;
-    for (int row = blockIdx.x * per_block + (PARTS > 1 ? 0 : set); row < rows; row += gridDim.x * per_block) {
+    const int size = p.a.plan[kPlanHeaderWords + 2];
+    const int warps = gridDim.x * (kMergeThreads / 32), items = p.a.B * p.a.Hq * PIECES;
+    for (int item = blockIdx.x * (kMergeThreads / 32) + (threadIdx.x >> 5); item < items; item += warps) {
+        const int row = item / PIECES, piece = item - row * PIECES, col = piece * LANES * VECS + lane % LANES;  // col: in units of 4 values
         const int b = row / p.a.Hq, h = row - b * p.a.Hq;
         const int c0 = p.a.cum_pages[b], c1 = p.a.cum_pages[b + 1];
-        uint2 *out = reinterpret_cast<uint2 *>(p.a.out + static_cast<size_t>(row) * kLatentDim);
+        uint2 *out = reinterpret_cast<uint2 *>(p.a.out + static_cast<size_t>(row) * kLatentDim) + col;
         if (c0 == c1) {
 #pragma unroll
             for (int v = 0; v < VECS; ++v)
-                if (part == 0) out[v * LANES + lane] = make_uint2(0u, 0u);
-            if (part == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = -INFINITY;
+                if (group == 0) out[v * LANES] = make_uint2(0u, 0u);
+            if (piece == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = -INFINITY;
             continue;
         }
         const int r0 = (c0 + p.extra) / size, r1 = (c1 - 1) / size;  // ranges of its first and last page
         if (r0 == r1) continue;  // written by the split kernel
-        Joined<VECS> sum;
-        for (int r = r0 + part; r <= r1; r += PARTS * U) {
+        float m = -INFINITY, l = 0.f, lr = 0.f;
+        float4 o[VECS];
+#pragma unroll
+        for (int v = 0; v < VECS; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+        auto raise = [&](float top) {
+            const float keep = m == top ? 1.f : fast_exp2(m - top);
+#pragma unroll
+            for (int v = 0; v < VECS; ++v) o[v].x *= keep, o[v].y *= keep, o[v].z *= keep, o[v].w *= keep;
+            l *= keep, lr *= keep;
+            m = top;
+        };
+        auto join = [&](float pm, float pl, float plr, const float4 (&x)[VECS]) {  // pm <= m
+            const float a = pm == -INFINITY ? 0.f : fast_exp2(pm - m);
+#pragma unroll
+            for (int v = 0; v < VECS; ++v)
+                o[v].x = fmaf(a, x[v].x, o[v].x), o[v].y = fmaf(a, x[v].y, o[v].y), o[v].z = fmaf(a, x[v].z, o[v].z), o[v].w = fmaf(a, x[v].w, o[v].w);
+            l = fmaf(a, pl, l);
+            lr = fmaf(a, plr, lr);
+        };
+        for (int r = r0 + group; r <= r1; r += GROUPS * U) {
             float4 x[U][VECS], ml[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int y = r + u * PARTS;
+                const int y = r + u * GROUPS;
+                ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
+#pragma unroll
+                for (int v = 0; v < VECS; ++v) x[u][v] = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (y <= r1) {
                     const size_t at = static_cast<size_t>(y == r0 ? 2 * y + 1 : 2 * y) * p.a.Hq + h;
                     ml[u] = p.part_ml[at];
 #pragma unroll
-                    for (int v = 0; v < VECS; ++v) x[u][v] = reinterpret_cast<const float4 *>(p.a.part_o + at * kLatentDim)[v * LANES + lane];
-                } else {
-                    ml[u] = make_float4(-INFINITY, 0.f, 0.f, 0.f);
-#pragma unroll
-                    for (int v = 0; v < VECS; ++v) x[u][v] = make_float4(0.f, 0.f, 0.f, 0.f);
+                    for (int v = 0; v < VECS; ++v) x[u][v] = reinterpret_cast<const float4 *>(p.a.part_o + at * kLatentDim)[col + v * LANES];
                 }
             }
-            sum.raise(fmaxf(fmaxf(sum.m, fmaxf(ml[0].x, ml[1].x)), fmaxf(ml[2].x, ml[3].x)));  // finite: ml[0] is a partial's reference
+            float top = m;
 #pragma unroll
-            for (int u = 0; u < U; ++u) sum.join(ml[u].x, ml[u].y, ml[u].z, x[u]);
+            for (int u = 0; u < U; ++u) top = fmaxf(top, ml[u].x);  // finite: ml[0] is a partial's reference
+            raise(top);
+#pragma unroll
+            for (int u = 0; u < U; ++u) join(ml[u].x, ml[u].y, ml[u].z, x[u]);
         }
-        if constexpr (PARTS > 1) {
-            static_assert(VECS == 1, "one vector per thread");
-            part_o[set][lane] = sum.o[0];
-            if (lane == 0) part_m[set] = sum.m, part_l[set] = sum.l, part_lr[set] = sum.lr;
-            __syncthreads();
-            if (part == 0) {  // it has a partial, so its reference is finite
+        if (GROUPS > 1) {
+            __syncwarp();
 #pragma unroll
-                for (int i = 1; i < PARTS; ++i) {
-                    const float4 x[1] = {part_o[i][lane]};
-                    sum.raise(fmaxf(sum.m, part_m[i]));
-                    sum.join(part_m[i], part_l[i], part_lr[i], x);
+            for (int d = LANES; d < 32; d <<= 1) {
+                const float pm = __shfl_xor_sync(0xffffffffu, m, d), pl = __shfl_xor_sync(0xffffffffu, l, d), plr = __shfl_xor_sync(0xffffffffu, lr, d);
+                float4 x[VECS];
+#pragma unroll
+                for (int v = 0; v < VECS; ++v)
+                    x[v] = make_float4(__shfl_xor_sync(0xffffffffu, o[v].x, d), __shfl_xor_sync(0xffffffffu, o[v].y, d),
+                                       __shfl_xor_sync(0xffffffffu, o[v].z, d), __shfl_xor_sync(0xffffffffu, o[v].w, d));
+                if (fmaxf(m, pm) > -INFINITY) {  // (a set without partials holds none)
+                    raise(fmaxf(m, pm));
+                    join(pm, pl, plr, x);
                 }
             }
-            __syncthreads();
-            if (part != 0) continue;
         }
-        const float inv = 1.f / sum.lr;
+        const float inv = 1.f / lr;
 #pragma unroll
         for (int v = 0; v < VECS; ++v)
-            out[v * LANES + lane] = make_uint2(pack_bf16x2(sum.o[v].x * inv, sum.o[v].y * inv), pack_bf16x2(sum.o[v].z * inv, sum.o[v].w * inv));
-        if (lane == 0 && p.a.lse != nullptr) p.a.lse[row] = (sum.m + log2f(sum.l)) * kLn2;
+            if (group == 0) out[v * LANES] = make_uint2(pack_bf16x2(o[v].x * inv, o[v].y * inv), pack_bf16x2(o[v].z * inv, o[v].w * inv));
+        if (piece == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = (m + log2f(l)) * kLn2;
     }
 }
 
@@ -779,9 +823,13 @@ cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMa
                             : n == 32 ? go(decode_attn_latent_kernel<32>, smem_bytes<32>())
                                       : go(decode_attn_latent_kernel<64>, smem_bytes<64>());
     if (err != cudaSuccess) return err;
-    const int rows = p.a.B * p.a.Hq, warps = (rows + 7) / 8, most = num_ctas * 16;
-    return rows <= 4 * num_ctas ? launch_pdl(latent_merge_kernel<128, 4>, dim3(rows), dim3(512), 0, stream, p.a.pdl != 0, p)
-                                : launch_pdl(latent_merge_kernel<32, 1>, dim3(warps < most ? warps : most), dim3(256), 0, stream, p.a.pdl != 0, p);
+    // few rows are cut into many partials each: four sets of lanes share them
+    const int rows = p.a.B * p.a.Hq;
+    auto merge = [&](auto *k, int warps_per_row) {
+        const int blocks = (rows * warps_per_row + kMergeThreads / 32 - 1) / (kMergeThreads / 32), most = num_ctas * 32;
+        return launch_pdl(k, dim3(blocks < most ? blocks : most), dim3(kMergeThreads), 0, stream, p.a.pdl != 0, p);
+    };
+    return rows <= 4 * num_ctas ? merge(latent_merge_kernel<4, 1>, 16) : merge(latent_merge_kernel<1, 4>, 1);
 }
 
 }  // namespace pd

@@ -90,12 +90,31 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
 
     grid_dependency_wait();
     launch_dependents();
-    const int b = p.order != nullptr ? p.order[blockIdx.z] : static_cast<int>(blockIdx.z);  // heaviest sequences first
-    const int q0 = p.q_indptr[b], q_len = p.q_indptr[b + 1] - q0;
+    // heaviest sequences first: up to 32 sequences every warp ranks them by itself, beyond that a small kernel did
+    int b, q0, q_len, len;
+    if (p.order == nullptr) {
+        const int mine = min(lane, p.B - 1);
+        const int from = p.q_indptr[mine], n = p.q_indptr[mine + 1] - from, L0 = p.ctx_lens[mine];
+        const long long work = static_cast<long long>(n) * (2ll * L0 - n);
+        int rank = 0;
+        for (int i = 0; i < p.B; ++i) {
+            const long long w = __shfl_sync(0xffffffffu, work, i);
+            rank += w > work || (w == work && i < lane) ? 1 : 0;
+        }
+        b = __ffs(__ballot_sync(0xffffffffu, lane < p.B && rank == static_cast<int>(blockIdx.z))) - 1;
+        q0 = __shfl_sync(0xffffffffu, from, b);
+        q_len = __shfl_sync(0xffffffffu, n, b);
+        len = __shfl_sync(0xffffffffu, L0, b);
+    } else {
+        b = p.order[blockIdx.z];
+        q0 = p.q_indptr[b];
+        q_len = p.q_indptr[b + 1] - q0;
+        len = p.ctx_lens[b];
+    }
     // CTAs are scheduled in index order: start a sequence's last tokens (the longest contexts) first
     const int cta_start = static_cast<int>(gridDim.x - 1 - blockIdx.x) * CTA_TOK;
     if (cta_start >= q_len) return;  // before any allocation
-    const int L = min(max(p.ctx_lens[b], 0), p.MP * kPageSize);
+    const int L = min(max(len, 0), p.MP * kPageSize);
     if (L < q_len) {  // the cache must already hold the new tokens
         if (tid == 0) latch(p.status, kDevBadLength, b, L);
         return;
@@ -424,11 +443,16 @@ cudaError_t prepare_prefill_attn_latent() {
 }
 
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
-                                       const LatentPrefillParams &p, int max_q_len, cudaStream_t stream) {
+                                       const LatentPrefillParams &base, int max_q_len, int *launched, cudaStream_t stream) {
+    LatentPrefillParams p = base;
+    *launched = 0;
+    if (p.a.B <= 32) p.a.order = nullptr;
     if (p.a.order != nullptr) {
         const cudaError_t e = launch_prefill_order(p.a, stream);
         if (e != cudaSuccess) return e;
+        *launched = 1;
     }
+    *launched += 1;
     const dim3 grid((max_q_len + kTiles * kRows - 1) / (kTiles * kRows), p.a.Hq, p.a.B);
     return launch_pdl(prefill_attn_latent_kernel, grid, dim3(kThreads), kSmemBytes, stream, p.a.pdl != 0, tm_k, tm_v, tm_r, p);
 }

@@ -159,6 +159,47 @@ def test_many_sequences():
             check(out, lse, ol.decode(f64(q), np.nan_to_num(f64(pages)), table, lens, float(np.float32(SCALE))))
 
 
+@pytest.mark.parametrize("batch", [31, 128, 129, 300])
+def test_batches_around_the_plan_by_one_warp(batch):
+    """Up to 128 sequences every warp derives the ranges, beyond that the block: empty sequences first, last and between."""
+    rng = np.random.default_rng(batch)
+    lens = rng.integers(1, 400, batch)
+    lens[[0, 1, batch // 2, batch - 1]] = 0
+    pages, table = cache_for(lens, batch)
+    q = queries((batch, 9, 576), batch + 1)
+    with Latent(9, batch, table.shape[1], pages.shape[0]) as ctx:
+        ref = ol.decode(f64(q), np.nan_to_num(f64(pages)), table, lens, float(np.float32(SCALE)))
+        for split in (0, 17, 2 ** 31 - 1):
+            out, lse = decode(ctx, q, pages, table, lens, split=split)
+            check(out, lse, ref)
+        plan = ctx.pd.pd_last_plan(ctx.h)
+        assert plan["total_units"] == int(((lens + P - 1) // P).sum()) and plan["num_ranges"] == 1
+
+
+def test_rows_behind_the_last_sequence_stay():
+    import paper_2609_35158_b200 as pd
+
+    lens = [70, 9, 300]
+    pages, table = cache_for(lens, 27, poison=False)
+    q = queries((3, 20, 576), 28)
+    out = torch.full((3, 20, 512), 5.0, dtype=torch.bfloat16, device=DEV)
+    lse = torch.full((3, 20), 5.0, device=DEV)
+    with Latent(20, 8, table.shape[1], pages.shape[0]) as ctx:
+        want, _ = decode(ctx, q[:2].contiguous(), pages, table[:2], lens[:2])
+        pd.pd_decode_attn_latent(ctx.h, q, pages, dev(table), dev(np.asarray(lens, np.int32)), out, lse, batch=2, sm_scale=SCALE)
+        torch.cuda.synchronize()
+        assert torch.equal(out[:2], want) and torch.all(out[2] == 5.0) and torch.all(lse[2] == 5.0) and torch.isfinite(lse[:2]).all()
+        # an append of the first two sequences' rows: the third one's, its length and its queries stay
+        kv_new, q_rope = wl.random_bf16((6, 576), 29, DEV), wl.random_bf16((6, 20, 64), 30, DEV)
+        q_out, before, n = torch.full_like(q_rope, 5.0), pages.clone(), dev(np.array([60, 3, 290], np.int32))
+        pd.pd_rope_append_tokens_latent(ctx.h, pd.rope_config(64, frequencies(64)), None, q_rope, kv_new, None, 0.0, dev(indptr_of([2, 1, 3])), q_out,
+                                        pages, dev(table), n, 2, batch=2)
+        torch.cuda.synchronize()
+        assert n.cpu().tolist() == [62, 4, 290] and torch.all(q_out[3:] == 5.0) and not torch.any(q_out[:3] == 5.0)
+        used = torch.from_numpy(table[2][table[2] >= 0].astype(np.int64)).to(DEV)
+        assert torch.equal(pages[used], before[used])
+
+
 def test_all_empty_and_no_lse():
     pages, table = cache_for([0, 0], 15)
     q = queries((2, 33, 576), 16)

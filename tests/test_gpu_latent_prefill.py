@@ -143,6 +143,22 @@ def test_prefill_ragged(heads, before, new):
     check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
 
 
+@pytest.mark.parametrize("batch", [32, 33, 70])
+def test_prefill_many_sequences(batch):
+    """Up to 32 sequences the blocks rank them by themselves, beyond that a small kernel does; rows behind the last one stay."""
+    rng = np.random.default_rng(batch)
+    before, new = rng.integers(0, 90, batch), rng.integers(0, 60, batch)
+    new[0] = 200
+    lens, pages, table, to, k, v, q = turn(before, new, 2, batch)
+    used = batch - 3
+    with Latent(2, batch, table.shape[1], pages.shape[0]) as ctx:
+        out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens)
+        part, _ = prefill(ctx, q, new[:used], k, v, to, pages, table, lens)
+    n = int(new[:used].sum())
+    assert torch.equal(part[:n], out[:n]) and torch.isnan(part[n:]).all()
+    check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
+
+
 def test_prefill_logits_that_rise_and_jump():
     new, before = [300], [500]
     for name in ("rise", "jump"):
