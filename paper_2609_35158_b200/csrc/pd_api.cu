@@ -85,8 +85,8 @@ struct pd_ctx {
     const void *map_expanded_k_ptr = nullptr, *map_expanded_v_ptr = nullptr;
     int64_t map_expanded_pages = 0;  // of both expanded pools' maps
     alignas(64) CUtensorMap tm_latent_w{};
-    alignas(64) CUtensorMap tm_expanded_k{};
-    alignas(64) CUtensorMap tm_expanded_v{};
+    alignas(64) CUtensorMap tm_expanded_k{}, tm_expanded_k_rows{};  // boxes of a page's row groups (loads), of 16 rows (stores)
+    alignas(64) CUtensorMap tm_expanded_v{}, tm_expanded_v_rows{};
     alignas(64) CUtensorMap tm_latent{}, tm_latent_pairs{};
     alignas(64) CUtensorMap tm_latent_q{};
     float4 *part_ml4 = nullptr;
@@ -1476,6 +1476,21 @@ int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, cons
     return PD_OK;
 }
 
+// The expanded pools' tensor maps, cached for one pair of pools.
+static int expanded_maps(pd_ctx *ctx, const void *k_pages, const void *v_pages, int64_t num_pages) {
+    if (ctx->map_expanded_k_ptr == k_pages && ctx->map_expanded_v_ptr == v_pages && ctx->map_expanded_pages == num_pages) return PD_OK;
+    ctx->map_expanded_k_ptr = nullptr;
+    const int64_t rows = num_pages * ctx->cfg.num_q_heads * pd::kPageSize;
+    if (int rc = encode_groups_map(ctx, k_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_k)) return rc;
+    if (int rc = encode_groups_map(ctx, v_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_v)) return rc;
+    if (int rc = encode_rows_map(ctx, k_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_k_rows)) return rc;
+    if (int rc = encode_rows_map(ctx, v_pages, pd::kLatentHead, rows, pd::kPageSize, &ctx->tm_expanded_v_rows)) return rc;
+    ctx->map_expanded_k_ptr = k_pages;
+    ctx->map_expanded_v_ptr = v_pages;
+    ctx->map_expanded_pages = num_pages;
+    return PD_OK;
+}
+
 // Pages of the expanded pools: ids and tensor-map rows are 32-bit.
 static int check_expanded_pages(pd_ctx *ctx, int64_t n) {
     if (n < 1) return fail(ctx, PD_ERR_INVALID_ARG, "expanded_num_pages must be positive");
@@ -1507,6 +1522,7 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
         if (int rc = encode_rows_map(ctx, w_kv, pd::kLatentDim, static_cast<int64_t>(ctx->cfg.num_q_heads) * rows, pd::kLatentHead, &ctx->tm_latent_w)) return rc;
         ctx->map_latent_w_ptr = w_kv;
     }
+    if (int rc = expanded_maps(ctx, k_pages, v_pages, expanded_num_pages)) return rc;
     pd::LatentExpandParams p{};
     p.page_table = page_table;
     p.dst_table = expanded_table;
@@ -1521,7 +1537,8 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
     p.num_pages = static_cast<int32_t>(ctx->cfg.num_pages);
     p.dst_num_pages = static_cast<int32_t>(expanded_num_pages);
     p.pdl = ctx->pdl;
-    const cudaError_t err = pd::launch_kv_expand_latent(ctx->tm_latent, ctx->tm_latent_w, p, ctx->latent_expand_pairs, static_cast<cudaStream_t>(stream));
+    const cudaError_t err = pd::launch_kv_expand_latent(ctx->tm_latent, ctx->tm_latent_w, ctx->tm_expanded_k_rows, ctx->tm_expanded_v_rows, p,
+                                                        ctx->latent_expand_pairs, static_cast<cudaStream_t>(stream));
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent expansion launch", err);
     ctx->launches += 1;
     return PD_OK;
@@ -1546,15 +1563,7 @@ int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, 
         ctx->latent_prefill_ready = true;
     }
     if (int rc = latent_map(ctx, kv_pages)) return rc;
-    const int64_t rows = expanded_num_pages * ctx->cfg.num_q_heads * pd::kPageSize;
-    if (ctx->map_expanded_k_ptr != k_pages || ctx->map_expanded_v_ptr != v_pages || ctx->map_expanded_pages != expanded_num_pages) {
-        ctx->map_expanded_k_ptr = nullptr;
-        if (int rc = encode_groups_map(ctx, k_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_k)) return rc;
-        if (int rc = encode_groups_map(ctx, v_pages, pd::kLatentHead / 64, rows, &ctx->tm_expanded_v)) return rc;
-        ctx->map_expanded_k_ptr = k_pages;
-        ctx->map_expanded_v_ptr = v_pages;
-        ctx->map_expanded_pages = expanded_num_pages;
-    }
+    if (int rc = expanded_maps(ctx, k_pages, v_pages, expanded_num_pages)) return rc;
     pd::LatentPrefillParams p{};
     p.a.q = static_cast<const __nv_bfloat16 *>(q);
     p.a.q_indptr = q_indptr;

@@ -295,8 +295,8 @@ cudaError_t prepare_decode_attn_latent();
 cudaError_t launch_decode_attn_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_rope, const CUtensorMap &tm_q, const LatentAttnParams &p,
                                       int num_ctas, cudaStream_t stream);
 cudaError_t prepare_kv_expand_latent(int num_sms, int *num_pairs);  // *num_pairs: clusters of two CTAs to launch
-cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const LatentExpandParams &p, int num_pairs,
-                                    cudaStream_t stream);
+cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap &tm_w, const CUtensorMap &tm_k, const CUtensorMap &tm_v,
+                                    const LatentExpandParams &p, int num_pairs, cudaStream_t stream);
 cudaError_t prepare_prefill_attn_latent();
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
                                        const LatentPrefillParams &p, int max_q_len, int *launched, cudaStream_t stream);

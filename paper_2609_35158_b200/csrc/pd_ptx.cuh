@@ -212,6 +212,12 @@ __device__ __forceinline__ void bulk_store(void *dst, uint32_t src, uint32_t byt
                  "r"(src), "r"(bytes)
                  : "memory");
 }
+// Tiled TMA store shared -> global, tracked by bulk groups; x * sizeof(element) must be a multiple of 16 B, coordinates in range.
+__device__ __forceinline__ void tma_store_2d(const void *tmap, int32_t x, int32_t y, uint32_t src) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(reinterpret_cast<uint64_t>(tmap)),
+                 "r"(x), "r"(y), "r"(src)
+                 : "memory");
+}
 __device__ __forceinline__ void bulk_commit_group() { asm volatile("cp.async.bulk.commit_group;" ::: "memory"); }
 // Returns once all but the N most recent bulk groups have finished READING their shared-memory source.
 template <int N>
