@@ -162,14 +162,16 @@ int encode_pool_map_fp8(pd_ctx *ctx, const void *pool, CUtensorMap *out) {
 int latent_groups(int heads) { return (heads + 63) / 64; }
 int latent_group_heads(int heads) { return (heads + latent_groups(heads) - 1) / latent_groups(heads); }
 
-// Absorbed queries [batch][heads][576]: box = 64 columns of the heads one block takes; heads past the last are zero fill.
+// Absorbed queries [batch][heads][576] as [batch][block of 64 columns][head][64]; box = all nine blocks of the heads one CTA takes.
+// Heads past the last are zero fill.
 int encode_latent_q_map(pd_ctx *ctx, const void *q, CUtensorMap *out) {
     const cuuint64_t heads = static_cast<cuuint64_t>(ctx->cfg.num_q_heads);
-    const cuuint64_t dims[3] = {pd::kLatentRow, heads, static_cast<cuuint64_t>(ctx->cfg.max_batch)};
-    const cuuint64_t strides[2] = {pd::kLatentRow * 2, heads * pd::kLatentRow * 2};
-    const cuuint32_t box[3] = {64, static_cast<cuuint32_t>(pd::latent_heads_per_cta(latent_group_heads(ctx->cfg.num_q_heads))), 1};
-    const cuuint32_t elem_strides[3] = {1, 1, 1};
-    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void *>(q), dims, strides, box,
+    const cuuint64_t dims[4] = {64, heads, pd::kLatentRow / 64, static_cast<cuuint64_t>(ctx->cfg.max_batch)};
+    const cuuint64_t strides[3] = {pd::kLatentRow * 2, 128, heads * pd::kLatentRow * 2};
+    const cuuint32_t box[4] = {64, static_cast<cuuint32_t>(pd::latent_heads_per_cta(latent_group_heads(ctx->cfg.num_q_heads))),
+                               pd::kLatentRow / 64, 1};
+    const cuuint32_t elem_strides[4] = {1, 1, 1, 1};
+    const CUresult r = ctx->encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void *>(q), dims, strides, box,
                                    elem_strides, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                                    CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r == CUDA_SUCCESS) return PD_OK;

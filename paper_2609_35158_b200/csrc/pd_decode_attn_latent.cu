@@ -67,10 +67,6 @@ __device__ __forceinline__ bool softmax_any(bool v) {
     return r != 0;
 }
 
-__device__ __forceinline__ void tma_load_3d(uint32_t dst, const void *tmap, int32_t x, int32_t y, int32_t z, uint32_t bar) {
-    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];"
-                 ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
-}
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar,
                                             uint64_t l2_policy) {
@@ -78,7 +74,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int3
                  " [%0], [%1, {%2, %3, %4, %5}], [%6], %7;"
                  ::"r"(dst), "l"(reinterpret_cast<uint64_t>(tmap)), "r"(x), "r"(y), "r"(z), "r"(w), "r"(bar), "l"(l2_policy) : "memory");
 }
-
 // Half a row's columns per thread: threads 0..15 of the warp get lanes 0..15 from column 0 on, threads 16..31 the same
 // lanes from column K on.
 template <int K>
@@ -122,11 +117,12 @@ struct LatentPlan {
 __device__ __forceinline__ LatentPlan latent_plan(int total, int workers, const LatentAttnParams &p) {
     LatentPlan pl;
     pl.total = total;
-    int size = p.a.split_pages > 0 ? p.a.split_pages : max((total + workers - 1) / workers, p.a.min_pages_auto);
-    size = max(size, (total + p.a.max_ranges - 1) / p.a.max_ranges);
+    int size = max((total + workers - 1) / workers, p.a.min_pages_auto);  // at most one range per worker
+    pl.per_worker = 1;
+    if (p.a.split_pages > 0) size = max(p.a.split_pages, (total + p.a.max_ranges - 1) / p.a.max_ranges);
     pl.size = max(min(size, total), 1);  // (total + size stays in 32 bits whatever split_pages is)
     pl.ranges = (total + pl.size - 1) / pl.size;
-    pl.per_worker = (pl.ranges + workers - 1) / workers;
+    if (p.a.split_pages > 0) pl.per_worker = (pl.ranges + workers - 1) / workers;
     return pl;
 }
 __device__ __forceinline__ int units_of(int pages, int extra) { return pages > 0 ? pages + extra : 0; }
@@ -235,7 +231,8 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     __shared__ uint32_t tmem_slot;
     __shared__ int32_t warp_sums[kThreads / 32];
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int group = blockIdx.x % p.groups, worker = blockIdx.x / p.groups, workers = gridDim.x / p.groups;
+    const int pairs = p.groups - 1;  // one or two groups of heads: neighbouring CTAs take the same ranges for both
+    const int group = blockIdx.x & pairs, worker = blockIdx.x >> pairs, workers = gridDim.x >> pairs;
     const int h0 = group * p.heads, nh = min(p.heads, p.a.Hq - h0);
 
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
@@ -282,14 +279,15 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
     LatentPlan pl;
     Walk w0{};
     w0.b = -1;
-    const bool warp_plan = p.a.B <= 128;
+    constexpr int kPer = 4;  // sequences per lane
+    const bool warp_plan = p.a.B <= 32 * kPer;
     int32_t *cum = reinterpret_cast<int32_t *>(aligned);
     int pages = 0;
     if (warp_plan) {
-        int units[4], sum = 0;
+        int units[kPer], sum = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int b = lane * 4 + i, L = b < p.a.B ? __ldg(p.a.ctx_lens + b) : 0;
+        for (int i = 0; i < kPer; ++i) {
+            const int b = lane * kPer + i, L = b < p.a.B ? __ldg(p.a.ctx_lens + b) : 0;
             if (blockIdx.x == 0 && warp == 0 && (L < 0 || L > p.a.MP * kPageSize)) latch_status(p.a.status, kDevBadLength, b, L);
             const int np = (clamp_len(L, p.a.MP) + kPageSize - 1) / kPageSize;
             units[i] = units_of(np, p.extra);
@@ -307,12 +305,12 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
         const int x = min(w0.r, pl.ranges) * pl.size;  // the worker's first unit: in this lane's sequences where it lies in [incl - sum, incl)
         int at = incl - sum, mine = -1, off = 0, in = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (x >= at && x < at + units[i]) mine = lane * 4 + i, off = x - at, in = units[i];
-            if (blockIdx.x == 0 && warp == 0 && lane * 4 + i <= p.a.B) p.a.cum_pages[lane * 4 + i] = at;
+        for (int i = 0; i < kPer; ++i) {
+            if (x >= at && x < at + units[i]) mine = lane * kPer + i, off = x - at, in = units[i];
+            if (blockIdx.x == 0 && warp == 0 && lane * kPer + i <= p.a.B) p.a.cum_pages[lane * kPer + i] = at;
             at += units[i];
         }
-        if (blockIdx.x == 0 && warp == 0 && lane == 31 && p.a.B == 128) p.a.cum_pages[128] = at;
+        if (blockIdx.x == 0 && warp == 0 && lane == 31 && p.a.B == 32 * kPer) p.a.cum_pages[32 * kPer] = at;
         const uint32_t owner = __ballot_sync(0xffffffffu, mine >= 0);
         if (owner != 0) {
             const int src = __ffs(owner) - 1;
@@ -377,8 +375,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 if (seg > 0) ok = mbar_wait(bar_qempty, (seg - 1) & 1);
                 if (!ok) return;
                 mbar_arrive_expect_tx(bar_qfull, kQBytes);
-#pragma unroll
-                for (int c = 0; c < kRowChunks; ++c) tma_load_3d(q_s + c * (N * 128), &tm_q, c * 64, h0, s.b, bar_qfull);
+                tma_load_4d(q_s, &tm_q, 0, h0, 0, s.b, bar_qfull, policy);  // [9 blocks of 64 columns][N heads]
                 ++seg;
             };
             int32_t id[kTilePages];  // the next tile's pages
@@ -683,10 +680,16 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                     tmem_ld16(tm + lane_base + j * N + c, o);
                     tmem_wait_ld();
                     if (s.whole) {
-                        __nv_bfloat16 *dst = p.a.out + (static_cast<size_t>(s.b) * p.a.Hq + h0 + c) * kLatentDim + latent;
+                        // neighbouring lanes trade, so that each stores two neighbouring latents of one head: even lanes the even heads
+                        const int odd = lane & 1;
+                        __nv_bfloat16 *dst = p.a.out + (static_cast<size_t>(s.b) * p.a.Hq + h0 + c + odd) * kLatentDim + (latent - odd);
 #pragma unroll
-                        for (int k = 0; k < 16; ++k)
-                            if (c + k < nh) dst[static_cast<size_t>(k) * kLatentDim] = __float2bfloat16_rn(__uint_as_float(o[k]) * inv[c + k]);
+                        for (int k = 0; k < 16; k += 2) {
+                            const float a = __uint_as_float(o[k]) * inv[c + k], b = __uint_as_float(o[k + 1]) * inv[c + k + 1];
+                            const float got = __shfl_xor_sync(0xffffffffu, odd ? a : b, 1);
+                            const uint32_t both = odd ? pack_bf16x2(got, b) : pack_bf16x2(a, got);
+                            if (c + k + odd < nh) *reinterpret_cast<uint32_t *>(dst + static_cast<size_t>(k) * kLatentDim) = both;
+                        }
                     } else {
                         float *dst = p.a.part_o + (static_cast<size_t>(s.slot) * p.a.Hq + h0 + c) * kLatentDim + latent;
 #pragma unroll
