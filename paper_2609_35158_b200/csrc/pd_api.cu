@@ -1586,7 +1586,7 @@ int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, 
     p.kv_table = expanded_table;
     p.kv_num_pages = static_cast<int32_t>(expanded_num_pages);
     int launched = 0;
-    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len, &launched,
+    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len, ctx->num_sms, &launched,
                                                            static_cast<cudaStream_t>(stream));
     ctx->launches += launched;
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent prefill launch", err);

@@ -299,7 +299,7 @@ cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap 
                                     const LatentExpandParams &p, int num_pairs, cudaStream_t stream);
 cudaError_t prepare_prefill_attn_latent();
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
-                                       const LatentPrefillParams &p, int max_q_len, int *launched, cudaStream_t stream);
+                                       const LatentPrefillParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_rope_append_latent(const LatentAppendParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_transfer(const TransferParams &p, bool scatter, int num_sms, cudaStream_t stream);
 

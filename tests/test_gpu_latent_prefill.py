@@ -159,6 +159,22 @@ def test_prefill_many_sequences(batch):
     check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
 
 
+@pytest.mark.parametrize("batch", [20, 45])
+def test_prefill_more_items_than_blocks(batch):
+    """Long turns among single tokens and sequences without any; calls of other shapes of the same context in between."""
+    rng = np.random.default_rng(batch)
+    before, new = rng.integers(0, 200, batch), rng.integers(0, 3, batch)
+    new[[3, 11]] = 600, 257
+    lens, pages, table, to, k, v, q = turn(before, new, 40, batch)
+    with Latent(40, batch, table.shape[1], pages.shape[0]) as ctx:
+        out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens)
+        one, _ = prefill(ctx, q, new[:1], k, v, to, pages, table, lens)
+        again, _ = prefill(ctx, q, new, k, v, to, pages, table, lens)
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+    assert torch.equal(out, again) and torch.equal(one[:new[0]], out[:new[0]])
+    check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
+
+
 def test_prefill_logits_that_rise_and_jump():
     new, before = [300], [500]
     for name in ("rise", "jump"):
