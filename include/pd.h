@@ -539,7 +539,8 @@ int pd_rope_append_tokens_q4(pd_ctx *ctx, const pd_rope_config *rope, const int3
  * These calls need a context of their own: pd_create with PD_FLAG_LATENT, num_q_heads in [1, 128], num_kv_heads 1,
  * head_dim 512, page_size 16; the other calls on caches and rotations refuse such a context, and these any other, with
  * PD_ERR_UNSUPPORTED. Calls of one context share its workspace: enqueue them on one stream or order them with events. None of
- * them allocates or synchronises, so all can be captured in CUDA graphs after one eager call with the same pointers.
+ * them allocates or synchronises, so all can be captured in CUDA graphs after one eager call with the same pointers. The
+ * workspace holds partial results: 1.2 MB per query head (pd_workspace_bytes).
  */
 
 /*

@@ -10,21 +10,25 @@
 //   S^T [64 tokens][N heads]   = rows (K-major) x Q^T             36 MMAs 64 x N x 16
 //   O^T [4][128 latents][N]   += latents^T (M-major) x P^T        16 MMAs 128 x N x 16
 // The operands' bytes bound the tensor pipe, (A + B) / 128 per clock: measured 32 cycles for a 64 x 64 x 16 product, 48 for
-// 128 x 64 x 16 (23 and 39 at N = 16); 1936 cycles a tile at N = 64, beside 3200 for its 73,728 bytes at the measured copy
-// bandwidth. These rates need the issuing thread to be chosen by elect.sync: under `lane == 0` one MMA takes 46 cycles to issue.
+// 128 x 64 x 16 (23 and 39 at N = 16), 1936 cycles a tile at N = 64; its 73,728 bytes take 3200 at the measured copy bandwidth.
+// These rates need the issuing thread to be chosen by elect.sync: under `lane == 0` one MMA takes 46 cycles to issue.
 // The ring holds pairs of 64-column blocks (128 latents of a tile, 16 KB) and, apart, the rotated parts (8 KB): a tile's
 // pairs are handed back one by one as the output products pass over them, so nearly two tiles are in flight beside 72 KB of Q.
 //
 // Softmax: one thread holds a quarter of the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
 // tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
 // than 32 log2 units (P and the sums keep fp32's exponent range, so 2^32 costs no accuracy): a tile needs one vote and no
-// reduction over tokens. P is rounded to bf16 (2^-9 of itself: a second
-// product for its remainder would make 128 heads a third slower); the sum that normalises the output adds the rounded
-// values, lse takes the unrounded sum.
+// reduction over tokens. P is rounded to bf16 (off by at most 2^-8 of itself: a second product for its remainder would make 128
+// heads a third slower); the sum that normalises the output adds the rounded values, lse takes the unrounded sum.
 //
 // More than 64 heads go in groups: neighbouring CTAs read the same pages for different heads, the second one from L2.
 // A segment (the part of a range inside one sequence) that covers its sequence writes the result, any other an fp32 partial;
 // latent_merge_kernel joins them. Every wait is bounded.
+//
+// Bounds. 16 heads: memory, 64 contexts of 2K-16K in 110 us, 0.93 of the measured copy bandwidth (0.89 under load). 64 heads: a tile
+// keeps shared memory busy for 2612 cycles (1936 of operands, 576 of the copies' writes, P) and takes 2950; 64 contexts around 8K
+// take 149 us in a burst, 173 under load, where the power limit lowers the clock; 128 heads on 2K-16K 221 and 267 us, 795 and
+// 656 TFLOP/s.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
@@ -66,7 +70,6 @@ __device__ __forceinline__ bool softmax_any(bool v) {
                  : "=r"(r) : "r"(static_cast<uint32_t>(v)), "n"(kSoftmaxThreads) : "memory");
     return r != 0;
 }
-
 
 __device__ __forceinline__ void tma_load_4d(uint32_t dst, const void *tmap, int32_t x, int32_t y, int32_t z, int32_t w, uint32_t bar,
                                             uint64_t l2_policy) {

@@ -230,6 +230,23 @@ def test_prefill_capture():
         assert torch.equal(out, want)
 
 
+def test_expanded_pages_past_4_gb():
+    """The last pages of pools of 5.2 GB each give what the first ones do."""
+    H, NP = 64, 20000
+    lens, new = np.asarray([70, 300], np.int32), [20, 260]
+    pages, table = cache_for(lens, 31)
+    w, q = weights(H, 32), queries((280, H, 192), 33)
+    k, v = (torch.empty((NP, H, P, 128), dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    got = []
+    with Latent(H, 2, table.shape[1], pages.shape[0]) as ctx:
+        for at in (0, NP - 2 * table.shape[1]):
+            to = (at + np.arange(2 * table.shape[1], dtype=np.int32)).reshape(2, -1)
+            expand(ctx, w, pages, table, None, lens, k, v, to)
+            got.append(prefill(ctx, q, new, k, v, to, pages, table, lens))
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+    assert torch.equal(got[0][0], got[1][0]) and torch.equal(got[0][1], got[1][1]) and torch.isfinite(got[0][0]).all()
+
+
 def test_refusals():
     import paper_2609_35158_b200 as pd
 
