@@ -540,7 +540,7 @@ int pd_rope_append_tokens_q4(pd_ctx *ctx, const pd_rope_config *rope, const int3
  * head_dim 512, page_size 16; the other calls on caches and rotations refuse such a context, and these any other, with
  * PD_ERR_UNSUPPORTED. Calls of one context share its workspace: enqueue them on one stream or order them with events. None of
  * them allocates or synchronises, so all can be captured in CUDA graphs after one eager call with the same pointers. The
- * workspace holds partial results: 1.2 MB per query head (pd_workspace_bytes).
+ * workspace holds partial results: 1.2 MB per query head, at least 40 MB (pd_workspace_bytes).
  */
 
 /*
@@ -584,7 +584,8 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
 /*
  * Append-prefill attention in the expanded form: as pd_prefill_attn with q [total][num_q_heads][192], out
  * [total][num_q_heads][128] bf16, logits sm_scale * (q[0:128] . K_h + q[128:192] . r) with K_h and V_h from the expanded
- * pages and r from the latent pages, all of which hold the new tokens already (ctx_lens counts them).
+ * pages and r from the latent pages, all of which hold the new tokens already (ctx_lens counts them). Results are
+ * bit-reproducible; where a batch has few new tokens, long contexts are cut and the order of a row's sums depends on the whole batch.
  */
 int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, const void *k_pages, const void *v_pages,
                            const int32_t *expanded_table, int64_t expanded_num_pages, const void *kv_pages, const int32_t *page_table,

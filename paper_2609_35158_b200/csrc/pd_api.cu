@@ -90,6 +90,8 @@ struct pd_ctx {
     alignas(64) CUtensorMap tm_latent{}, tm_latent_pairs{};
     alignas(64) CUtensorMap tm_latent_q{};
     float4 *part_ml4 = nullptr;
+    int32_t *arrived = nullptr;  // latent prefill: stretches of 32 rows that are done, zero between calls
+    int32_t max_parts = 0;       // ... and the partial results there is room for
     bool prefill_ready = false;
     bool fp8_ready = false;
     bool q4_ready = false;
@@ -324,7 +326,12 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
         ctx->slots = 2 * static_cast<size_t>(ctx->max_ranges);
     }
     auto round256 = [](size_t n) { return (n + 255) & ~size_t(255); };
-    const size_t b_part_o = round256(ctx->slots * group * cfg->head_dim * sizeof(float));
+    size_t b_part_o = round256(ctx->slots * group * cfg->head_dim * sizeof(float)), b_arrived = 0;
+    if (latent) {  // prefill's partial results share the space: two per SM
+        ctx->max_parts = 2 * ctx->num_sms;
+        b_part_o = std::max(b_part_o, round256(ctx->max_parts * pd::kLatentPrefillPartBytes));
+        b_arrived = round256(static_cast<size_t>(ctx->max_parts) * 8 * sizeof(int32_t));
+    }
     const size_t b_part_ml = round256(ctx->slots * group * (latent ? sizeof(float4) : sizeof(float2)));
     const size_t b_cum = round256((static_cast<size_t>(cfg->max_batch) + 1) * sizeof(int32_t));
     const size_t b_plan = round256(pd::kPlanWords * sizeof(int32_t));
@@ -333,7 +340,7 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
     const size_t b_q = latent ? 0 : round256(static_cast<size_t>(cfg->max_batch) * cfg->num_q_heads * cfg->head_dim * 2);
     const size_t b_kv = latent ? 0 : round256(static_cast<size_t>(cfg->max_batch) * cfg->num_kv_heads * cfg->head_dim * 2);
     const size_t b_trace = tune_int("PD_TRACE_WORKERS", 0) ? round256(static_cast<size_t>(n_workers) * 4 * 8) : 0;
-    ctx->workspace_bytes = b_part_o + b_part_ml + b_cum + b_plan + b_status + 2 * b_q + 2 * b_kv + b_trace;
+    ctx->workspace_bytes = b_part_o + b_part_ml + b_cum + b_plan + b_status + b_arrived + 2 * b_q + 2 * b_kv + b_trace;
     err = cudaMalloc(&ctx->workspace, ctx->workspace_bytes);
     if (err != cudaSuccess) {
         delete ctx;
@@ -346,6 +353,7 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
     ctx->cum_pages = reinterpret_cast<int32_t *>(w); w += b_cum;
     ctx->plan = reinterpret_cast<int32_t *>(w); w += b_plan;
     ctx->status = reinterpret_cast<int32_t *>(w); w += b_status;
+    ctx->arrived = reinterpret_cast<int32_t *>(w); w += b_arrived;
     ctx->stage_q = reinterpret_cast<__nv_bfloat16 *>(w); w += b_q;  // q, k_new, v_new are adjacent: one copy can fill them
     ctx->stage_k = reinterpret_cast<__nv_bfloat16 *>(w); w += b_kv;
     ctx->stage_v = reinterpret_cast<__nv_bfloat16 *>(w); w += b_kv;
@@ -1248,6 +1256,10 @@ int pd_device_status(pd_ctx *ctx, void *stream, int32_t *code, int32_t *seq, int
     if (err == cudaSuccess) err = cudaMemsetAsync(ctx->status, 0, sizeof host, s);
     if (err == cudaSuccess) err = cudaStreamSynchronize(s);
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "status read", err);
+    if (host[0] == pd::kDevTimeout && ctx->max_parts > 0) {  // a latent prefill that gave up may have left counts behind
+        err = cudaMemsetAsync(ctx->arrived, 0, static_cast<size_t>(ctx->max_parts) * 8 * sizeof(int32_t), s);
+        if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "status read", err);
+    }
     int rc = PD_OK;
     if (host[0] == pd::kDevBadPage || host[0] == pd::kDevBadLength) rc = PD_ERR_DEVICE_FAULT;
     else if (host[0] == pd::kDevTimeout) rc = PD_ERR_TIMEOUT;
@@ -1585,8 +1597,12 @@ int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, 
     p.a.order = ctx->cum_pages;  // the decode kernel's prefix-sum buffer is free here
     p.kv_table = expanded_table;
     p.kv_num_pages = static_cast<int32_t>(expanded_num_pages);
+    p.num_sms = ctx->num_sms;
+    p.part = ctx->part_o;
+    p.arrived = ctx->arrived;
+    p.max_parts = ctx->max_parts;
     int launched = 0;
-    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len, ctx->num_sms, &launched,
+    const cudaError_t err = pd::launch_prefill_attn_latent(ctx->tm_expanded_k, ctx->tm_expanded_v, ctx->tm_latent, p, max_q_len, &launched,
                                                            static_cast<cudaStream_t>(stream));
     ctx->launches += launched;
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "latent prefill launch", err);

@@ -237,7 +237,12 @@ struct LatentPrefillParams {
     PrefillParams a;             // q [total][Hq][192], out [total][Hq][128]; page_table, num_pages: the latent pages
     const int32_t *kv_table;     // [B][MP] pages of the expanded K and V
     int32_t kv_num_pages;
+    int32_t num_sms;
+    int32_t max_parts;           // partial results there is room for
+    float *part;                 // [max_parts] of kLatentPrefillPartBytes
+    int32_t *arrived;            // [max_parts][8] stretches of a group of 32 rows that are done; zero between calls
 };
+constexpr size_t kLatentPrefillPartBytes = 2 * (128 * 128 + 2 * 128) * sizeof(float);
 
 struct AttnVariant {
     int head_dim, warps, stages, hilo;
@@ -299,7 +304,7 @@ cudaError_t launch_kv_expand_latent(const CUtensorMap &tm_kv, const CUtensorMap 
                                     const LatentExpandParams &p, int num_pairs, cudaStream_t stream);
 cudaError_t prepare_prefill_attn_latent();
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
-                                       const LatentPrefillParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
+                                       const LatentPrefillParams &p, int max_q_len, int *launched, cudaStream_t stream);
 cudaError_t launch_rope_append_latent(const LatentAppendParams &p, int max_q_len, int num_sms, int *launched, cudaStream_t stream);
 cudaError_t launch_kv_transfer(const TransferParams &p, bool scatter, int num_sms, cudaStream_t stream);
 

@@ -19,8 +19,11 @@
 // runs one tile. Tensor memory: (S0 80, P0 40) (S1, P1) O0 O1, 128 columns each. Every wait is bounded.
 // Why a counter and not a block per item: the grid would have to be as wide as the longest turn for every sequence, and the next
 // item's queries, keys and values come in during the last one's softmax and stores. Two turns of 2048 among 62 single tokens, 32
-// heads: 223 us, 329 with a block per item; nine odd turns 34.0 from 36.6. The few more instructions of the walk cost long
+// heads: 235 us, 329 with a block per item; nine odd turns 34.0 from 36.6. The few more instructions of the walk cost long
 // turns 2 %.
+// Few tokens on a long context are few items: then an item is a stretch of the context, its unnormalised outputs go to the workspace in
+// fp32, and the warp that counts the last stretch of its 32 rows joins them in their order (the same bits in every call). 128 tokens on
+// 8000, 32 heads: 42 us, 95 whole; 512 on 30000, 8 heads: 90 and 464.
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_tcgen05.cuh"
@@ -98,12 +101,19 @@ __device__ __forceinline__ uint32_t fills(int nb) {
     return mask;
 }
 
-// Two tiles of one head.
+// Two tiles of one head over a stretch of their context.
 struct Item {
-    int row0, n_tok, pos0, len;  // first packed row, rows, position of the first one, tokens of the context
-    int b, head, nb0, nb1;       // blocks each tile's last token can see (nb1 = 0: one tile; nb0 = 0: no more items)
+    int row0, n_tok, pos0, len;  // first packed row, rows (0: no more items), position of the first one, tokens of the context
+    int b, head, nb0, nb1;       // blocks of each tile in the stretch, as far as its last token sees
+    int j0, parts, part, first;  // first block; stretches of these tiles, the partial result this one writes, the first one's
 };
+// A partial result: per tile [column / 4][row][4] unnormalised outputs, then [row] (reference, sum).
+constexpr int kPartTile = kRows * kLatentHead;
+constexpr size_t kPartFloats = kTiles * (kPartTile + 2 * kRows);
+static_assert(kPartFloats * sizeof(float) == kLatentPrefillPartBytes, "the workspace is sized by it");
 
+// SPLITS: contexts may be cut. A kernel of its own, as the code of that costs every item 0.4 us.
+template <bool SPLITS>
 __global__ void __launch_bounds__(kThreads, 1)
 prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
                            const __grid_constant__ CUtensorMap tm_r, const LatentPrefillParams lp) {
@@ -154,7 +164,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
     bool ok = true;
 
     int taken = 0;  // items this thread has come to
-    // The slot of the next item; the item behind the last one has no blocks.
+    // The slot of the next item; the item behind the last one has no rows.
     auto next_item = [&]() -> const Item & {
         const int slot = taken % kItemSlots;
         ok = ok && mbar_wait(bar_item + slot * 8, (taken / kItemSlots) & 1);
@@ -167,7 +177,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         if (!ok) return false;
         it = next;
         mbar_arrive(bar_taken + (taken - 1) % kItemSlots * 8);
-        return it.nb0 > 0;
+        return it.n_tok > 0;
     };
 
     if (warp >= kSoftmaxWarps) {
@@ -175,7 +185,15 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
         if (warp == kSoftmaxWarps + 3) {
             // ================= hands out items: sequences by falling work, one head after the other, last tokens first =================
             // Lanes hold 32 sequences at a time and count their items up. Up to 32 are ranked here, more by a small kernel before.
-            int b = 0, from = 0, n = 0, L = 0, count = 0, incl = 0;
+            int b = 0, from = 0, n = 0, L = 0, per_head = 0, count = 0, incl = 0, chunk = 0;  // chunk: most blocks of a stretch, 0: any
+            // blocks the two tiles from token `start` of a sequence's m new ones see, and the stretches they are cut into
+            auto blocks_of = [&](int m, int len, int start) { return (len - m + min(start + kItemTok, m) - 1) / kBlock + 1; };
+            auto parts_of = [&](int nb, int c) { return static_cast<int>((static_cast<float>(nb + c) - 0.5f) * (1.f / static_cast<float>(c))); };
+            auto pieces_of = [&](int c) {
+                int sum = 0;
+                for (int start = 0; start < n; start += kItemTok) sum += parts_of(blocks_of(n, L, start), c);
+                return sum;
+            };
             auto window = [&](int w) {
                 const int z = w * 32 + lane;
                 if (p.order == nullptr) {
@@ -202,7 +220,31 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 const bool real = z < p.B && n > 0;
                 L = min(max(L, 0), p.MP * kPageSize);
                 if (real && L < n && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);  // the cache must hold the new tokens
-                count = real && L >= n ? (n + kItemTok - 1) / kItemTok * p.Hq : 0;
+                if (!real || L < n) n = 0;
+                if (SPLITS) {
+                    // Few items: a context is cut where whole ones would leave SMs idle. In blocks of 1.0 to 1.5 us: a stretch costs about 4
+                    // more, joining one about 1, and where there are more stretches than SMs the last ones end half a stretch late.
+                    int sum = 0, longest = 0;
+                    for (int start = 0; start < n; start += kItemTok) {
+                        const int nb = blocks_of(n, L, start);
+                        sum += nb;
+                        longest = max(longest, nb);
+                    }
+                    longest = __reduce_max_sync(0xffffffffu, longest);
+                    if (longest >= 16) {
+                        const int sms = lp.num_sms, fair = (__reduce_add_sync(0xffffffffu, sum) * p.Hq + sms - 1) / sms;
+                        const int whole = __reduce_add_sync(0xffffffffu, (n + kItemTok - 1) / kItemTok) * p.Hq;
+                        int best = whole <= sms ? longest : max(longest, fair + longest / 2);
+                        for (int c = max(fair, 8); c < longest; c += (c + 3) / 4) {
+                            const int pieces = __reduce_add_sync(0xffffffffu, pieces_of(c)) * p.Hq;
+                            const int est = max(c, pieces <= sms ? 0 : fair + c / 2 + 4) + 4 + longest / c;
+                            if (pieces <= lp.max_parts && est < best) best = est, chunk = c;
+                            if (c > best) break;
+                        }
+                    }
+                }
+                per_head = !SPLITS || chunk == 0 ? (n + kItemTok - 1) / kItemTok : pieces_of(chunk);
+                count = per_head * p.Hq;
                 incl = count;
 #pragma unroll
                 for (int o = 1; o < 32; o <<= 1) {
@@ -222,16 +264,33 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 if (more) {
                     const int src = __ffs(__ballot_sync(0xffffffffu, idx - before < incl)) - 1;
                     const int rel = idx - before - __shfl_sync(0xffffffffu, incl - count, src);
-                    const int q_len = __shfl_sync(0xffffffffu, n, src), tiles = (q_len + kItemTok - 1) / kItemTok;
-                    const int head = rel / tiles, start = (tiles - 1 - (rel - head * tiles)) * kItemTok;
+                    const int q_len = __shfl_sync(0xffffffffu, n, src);
                     it.b = __shfl_sync(0xffffffffu, b, src);
-                    it.head = head;
                     it.len = __shfl_sync(0xffffffffu, L, src);
+                    int left, start = (q_len - 1) / kItemTok * kItemTok, parts = 1, nb;
+                    if (!SPLITS || chunk == 0) {  // the tiles of one head after those of another: they read the same keys and values
+                        const int tiles = __shfl_sync(0xffffffffu, per_head, src);
+                        it.head = rel / tiles;
+                        start -= (rel - it.head * tiles) * kItemTok;
+                        left = 0;
+                        nb = blocks_of(q_len, it.len, start);
+                    } else {  // the longest contexts of all heads first
+                        left = rel / p.Hq;
+                        it.head = rel - left * p.Hq;
+                        for (;; start -= kItemTok) {
+                            nb = blocks_of(q_len, it.len, start);
+                            parts = parts_of(nb, chunk);
+                            if (left < parts || start == 0) break;
+                            left -= parts;
+                        }
+                    }
+                    const int size = parts == 1 ? nb : (nb + parts - 1) / parts;
                     it.row0 = __shfl_sync(0xffffffffu, from, src) + start;
                     it.n_tok = min(kItemTok, q_len - start);
                     it.pos0 = it.len - q_len + start;
-                    it.nb0 = (it.pos0 + min(it.n_tok, kRows) - 1) / kBlock + 1;
-                    it.nb1 = it.n_tok > kRows ? (it.pos0 + it.n_tok - 1) / kBlock + 1 : 0;
+                    if (SPLITS) it.j0 = left * size, it.parts = parts, it.part = idx, it.first = idx - left * p.Hq;
+                    it.nb0 = min(max((it.pos0 + min(it.n_tok, kRows) - 1) / kBlock + 1 - left * size, 0), size);
+                    it.nb1 = it.n_tok > kRows ? min(max(nb - left * size, 0), size) : 0;
                 }
                 if (k >= kItemSlots)
                     ok = __all_sync(0xffffffffu, mbar_wait(bar_taken + k % kItemSlots * 8, (k / kItemSlots - 1) & 1));
@@ -300,12 +359,14 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 Item it{};
                 while (take_item(it)) {
                     const int nb0 = it.nb0, nb1 = it.nb1, nb = max(nb0, nb1);
-                    ok = mbar_wait(bar_q, turns[0] & 1);
-                    if (ok) issue_s(0, 0, true, nb1 == 0);
-                    if (nb1 > 0) ok = ok && mbar_wait(bar_q + 8, turns[1] & 1);
-                    if (ok && nb1 > 0) issue_s(1, 0, false, true);
+                    const bool two = nb1 > 0, one = !SPLITS || nb0 > 0;  // the first tile may see nothing of a stretch
+                    if (one) ok = mbar_wait(bar_q, turns[0] & 1);
+                    if (ok && one) issue_s(0, 0, true, !two);
+                    if (two) ok = ok && mbar_wait(bar_q + 8, turns[1] & 1);
+                    if (ok && two) issue_s(1, 0, !one, true);
                     // the rows have read what the tiles' last items left in O
-                    ok = ok && mbar_wait(bar_done, (turns[0] & 1) ^ 1) && (nb1 == 0 || mbar_wait(bar_done + 8, (turns[1] & 1) ^ 1));
+                    if (one) ok = ok && mbar_wait(bar_done, (turns[0] & 1) ^ 1);
+                    if (two) ok = ok && mbar_wait(bar_done + 8, (turns[1] & 1) ^ 1);
                     // the tile that meets a block first waits for it, the one that meets it last hands it back
                     for (int j = 0; j < nb && ok; ++j) {
                         const bool u0 = j < nb0, u1 = j < nb1, n0 = j + 1 < nb0, n1 = j + 1 < nb1;
@@ -316,8 +377,8 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     }
                     if (!ok) break;
                     k_mask ^= fills<kKSlots>(nb), v_mask ^= fills<kVSlots>(nb);
-                    done[0] ^= nb0 & 1, turns[0] ^= 1;
-                    if (nb1 > 0) done[1] ^= nb1 & 1, turns[1] ^= 1;
+                    if (one) done[0] ^= nb0 & 1, turns[0] ^= 1;
+                    if (two) done[1] ^= nb1 & 1, turns[1] ^= 1;
                 }
                 if (!ok) latch(p.status, kDevTimeout, it.b, blockIdx.x);
                 umma_commit(bar_drain);  // nothing may be in flight when the tensor memory is freed
@@ -333,13 +394,13 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 int32_t kv_id[kBlockPages], r_id[kBlockPages];  // the next block's pages
                 Item it{};
                 while (take_item(it)) {
-                    const int nb = max(it.nb0, it.nb1), n_pages = (it.len + kPageSize - 1) / kPageSize;
+                    const int nb = max(it.nb0, it.nb1), j0 = SPLITS ? it.j0 : 0, n_pages = (it.len + kPageSize - 1) / kPageSize;
                     const int32_t *kv_row = lp.kv_table + static_cast<size_t>(it.b) * p.MP;
                     const int32_t *r_row = p.page_table + static_cast<size_t>(it.b) * p.MP;
                     auto load_ids = [&](int j) {
 #pragma unroll
                         for (int g = 0; g < kBlockPages; ++g) {
-                            const int page = j * kBlockPages + g;
+                            const int page = (j0 + j) * kBlockPages + g;
                             kv_id[g] = page < n_pages ? __ldg(kv_row + page) : 0;
                             if (is_k) r_id[g] = page < n_pages ? __ldg(r_row + page) : 0;
                         }
@@ -355,8 +416,8 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         int32_t kv_page[kBlockPages], r_page[kBlockPages];
 #pragma unroll
                         for (int g = 0; g < kBlockPages; ++g) {
-                            kv_page[g] = checked(kv_id[g], j * kBlockPages + g, lp.kv_num_pages);
-                            r_page[g] = is_k ? checked(r_id[g], j * kBlockPages + g, p.num_pages) : 0;
+                            kv_page[g] = checked(kv_id[g], (j0 + j) * kBlockPages + g, lp.kv_num_pages);
+                            r_page[g] = is_k ? checked(r_id[g], (j0 + j) * kBlockPages + g, p.num_pages) : 0;
                         }
                         if (j + 1 < nb) load_ids(j + 1);
                         if (is_k && j == max(nb - 2, 0)) mbar_arrive(bar_claim);
@@ -410,13 +471,13 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             }
         };
         const Item *it = &next_item(), *after = it;
-        if (ok && it->nb0 > 0) copy_q(*it);
-        while (ok && it->nb0 > 0) {
+        if (ok && it->n_tok > 0) copy_q(*it);
+        while (ok && it->n_tok > 0) {
             const int my_nb = t == 0 ? it->nb0 : it->nb1;
             const int tok = t * kRows + row;                      // token index inside the item
             const int my_pos = it->pos0 + min(tok, it->n_tok - 1);  // padding rows mirror the last token
+            cp_async_wait_all();
             if (my_nb > 0) {
-                cp_async_wait_all();
                 fence_proxy_async();  // written through the generic proxy, read by the tensor core through the async one
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_q + t * 8);
@@ -427,7 +488,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 ok = mbar_wait(bar_s + t * 8, done & 1);
                 tc_fence_after_sync();
                 if (!ok) break;
-                const int t0 = j * kBlock;
+                const int t0 = ((SPLITS ? it->j0 : 0) + j) * kBlock;
                 const bool masked = t0 + kBlock - 1 > my_pos;  // the block reaches past this row's position
                 // V rows past the context inside the last page may hold NaN; 0 * NaN is NaN, so the warpgroup whose products of
                 // this block come first clears them
@@ -479,11 +540,11 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     for (int c = 0; c < kBlock; ++c)
                         if (c >= visible) v[c] = 0xff800000u;
                 }
-                if (j == 0) {  // the reference: the row's largest logit of the block, finite because position 0 is visible
+                if (j == 0) {  // the reference: the row's largest logit of the block, or 0 where it sees none of the stretch
                     float top = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < kBlock; c += 2) top = max3(top, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-                    m_run = top * p.scale_log2;
+                    m_run = SPLITS && top == -INFINITY ? 0.f : top * p.scale_log2;
                 }
                 const float xmax = weigh();
                 if (__any_sync(0xffffffffu, xmax > kRaise)) {
@@ -521,44 +582,109 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             }
             if (!ok) break;
             after = &next_item();  // this item's last logits are in registers: the next one's queries may come
-            if (ok && after->nb0 > 0) copy_q(*after);
+            if (ok && after->n_tok > 0) copy_q(*after);
             v_mask ^= fills<kVSlots>(max(it->nb0, it->nb1));
 
             // ---- O_t / l -> bf16 rows
+            auto store_cols = [&](__nv_bfloat16 *to, const uint32_t (&o)[32], float inv, bool wide) {  // 32 columns of a row
+#pragma unroll
+                for (int i = 0; i < 32; i += 16) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) w[k] = pack_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
+                    if (wide) {
+                        store32(to + i, w);
+                    } else {
+                        *reinterpret_cast<uint4 *>(to + i) = make_uint4(w[0], w[1], w[2], w[3]);
+                        *reinterpret_cast<uint4 *>(to + i + 8) = make_uint4(w[4], w[5], w[6], w[7]);
+                    }
+                }
+            };
+            auto o_read = [&]() {
+                tc_fence_before_sync();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_done + t * 8);
+            };
             if (my_nb > 0) {
                 ok = mbar_wait(bar_o + t * 8, (done - 1) & 1);
                 if (!ok) break;
                 tc_fence_after_sync();
-                const float inv = 1.f / l_run;
-                const bool row_valid = tok < it->n_tok, wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
-                const size_t at = static_cast<size_t>(it->row0 + min(tok, it->n_tok - 1)) * p.Hq + it->head;
-                __nv_bfloat16 *orow = p.out + at * kLatentHead;
+            }
+            const bool row_valid = tok < it->n_tok, wide = (reinterpret_cast<uintptr_t>(p.out) & 31u) == 0;
+            const size_t at = static_cast<size_t>(it->row0 + min(tok, it->n_tok - 1)) * p.Hq + it->head;
+            __nv_bfloat16 *orow = p.out + at * kLatentHead;
+            if (!SPLITS || it->parts == 1) {
+                if (my_nb > 0) {
+                    const float inv = 1.f / l_run;
 #pragma unroll
-                for (int c = 0; c < kLatentHead; c += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(o_buf + c, o);
-                    tmem_wait_ld();
-                    if (c == kLatentHead - 32) {  // O_t has been read
-                        tc_fence_before_sync();
-                        __syncwarp();
-                        if (lane == 0) mbar_arrive(bar_done + t * 8);
+                    for (int c = 0; c < kLatentHead; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_buf + c, o);
+                        tmem_wait_ld();
+                        if (c == kLatentHead - 32) o_read();
+                        if (row_valid) store_cols(orow + c, o, inv, wide);
                     }
-                    if (row_valid) {
+                    if (p.lse != nullptr && row_valid) p.lse[at] = (m_run + log2f(l_run)) * kLn2f;
+                }
+            } else if (t * kRows < it->n_tok) {
+                // A partial result; the warp that counts the last stretch of its 32 rows joins them, in their order.
+                auto part_of = [&](int i) { return lp.part + static_cast<size_t>(it->first + i * p.Hq) * kPartFloats; };
+                auto ml_of = [&](int i) { return reinterpret_cast<float2 *>(part_of(i) + kTiles * kPartTile) + t * kRows + row; };
+                const int mine = (it->part - it->first) / p.Hq, parts = it->parts, at_row = t * kPartTile + row * 4;
+                if (my_nb > 0) {
 #pragma unroll
-                        for (int i = 0; i < 32; i += 16) {
-                            uint32_t w[8];
+                    for (int c = 0; c < kLatentHead; c += 32) {
+                        uint32_t o[32];
+                        tmem_ld32(o_buf + c, o);
+                        tmem_wait_ld();
+                        if (c == kLatentHead - 32) o_read();
 #pragma unroll
-                            for (int k = 0; k < 8; ++k) w[k] = pack_bf16x2(__uint_as_float(o[i + 2 * k]) * inv, __uint_as_float(o[i + 2 * k + 1]) * inv);
-                            if (wide) {
-                                store32(orow + c + i, w);
-                            } else {
-                                *reinterpret_cast<uint4 *>(orow + c + i) = make_uint4(w[0], w[1], w[2], w[3]);
-                                *reinterpret_cast<uint4 *>(orow + c + i + 8) = make_uint4(w[4], w[5], w[6], w[7]);
-                            }
-                        }
+                        for (int k = 0; k < 8; ++k)
+                            *reinterpret_cast<uint4 *>(part_of(mine) + at_row + (c / 4 + k) * kRows * 4) =
+                                make_uint4(o[4 * k], o[4 * k + 1], o[4 * k + 2], o[4 * k + 3]);
                     }
                 }
-                if (p.lse != nullptr && row_valid) p.lse[at] = (m_run + log2f(l_run)) * kLn2f;
+                *ml_of(mine) = make_float2(m_run, l_run);
+                int32_t *arrived = lp.arrived + it->first * kSoftmaxWarps + warp;
+                int before = 0;
+                __threadfence();
+                __syncwarp();
+                if (lane == 0) before = atomicAdd(arrived, 1);
+                if (__shfl_sync(0xffffffffu, before, 0) == parts - 1) {
+                    if (lane == 0) *arrived = 0;
+                    __threadfence();
+                    float top = -INFINITY, sum = 0.f;
+                    for (int i = 0; i < parts; ++i) {
+                        const float2 ml = __ldcg(ml_of(i));
+                        if (!(ml.y == 0.f)) top = fmaxf(top, ml.x);
+                    }
+                    for (int i = 0; i < parts; ++i) {
+                        const float2 ml = __ldcg(ml_of(i));
+                        if (!(ml.y == 0.f)) sum += ml.y * fast_exp2(ml.x - top);
+                    }
+                    const float inv = 1.f / sum;
+#pragma unroll 1
+                    for (int c = 0; c < kLatentHead; c += 32) {
+                        float acc[32] = {};
+#pragma unroll 4
+                        for (int i = 0; i < parts; ++i) {
+                            const float2 ml = __ldcg(ml_of(i));
+                            const bool seen = !(ml.y == 0.f);  // a tile without blocks in a stretch has written no outputs
+                            const float w = seen ? fast_exp2(ml.x - top) : 0.f;
+                            const float *from = part_of(i) + at_row + c * kRows;
+#pragma unroll
+                            for (int k = 0; k < 8; ++k) {
+                                const float4 x = seen ? __ldcg(reinterpret_cast<const float4 *>(from + k * kRows * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                                acc[4 * k] += w * x.x, acc[4 * k + 1] += w * x.y, acc[4 * k + 2] += w * x.z, acc[4 * k + 3] += w * x.w;
+                            }
+                        }
+                        uint32_t o[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(acc[k]);
+                        if (row_valid) store_cols(orow + c, o, inv, wide);
+                    }
+                    if (p.lse != nullptr && row_valid) p.lse[at] = (top + log2f(sum)) * kLn2f;
+                }
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar_taken + (taken - 2) % kItemSlots * 8);
@@ -576,11 +702,13 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
 }  // namespace
 
 cudaError_t prepare_prefill_attn_latent() {
-    return cudaFuncSetAttribute(prefill_attn_latent_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+    const cudaError_t e = cudaFuncSetAttribute(prefill_attn_latent_kernel<false>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(prefill_attn_latent_kernel<true>, cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(kSmemBytes));
 }
 
 cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMap &tm_v, const CUtensorMap &tm_r,
-                                       const LatentPrefillParams &base, int max_q_len, int num_sms, int *launched, cudaStream_t stream) {
+                                       const LatentPrefillParams &base, int max_q_len, int *launched, cudaStream_t stream) {
     LatentPrefillParams p = base;
     *launched = 0;
     if (p.a.B <= 32) p.a.order = nullptr;
@@ -590,9 +718,12 @@ cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMa
         *launched = 1;
     }
     *launched += 1;
-    const long long most = static_cast<long long>((max_q_len + kTiles * kRows - 1) / (kTiles * kRows)) * p.a.Hq * p.a.B;  // items
-    const dim3 grid(static_cast<unsigned>(most < num_sms ? most : num_sms));
-    return launch_pdl(prefill_attn_latent_kernel, grid, dim3(kThreads), kSmemBytes, stream, p.a.pdl != 0, tm_k, tm_v, tm_r, p);
+    // Contexts are cut only where there may be fewer than two items per SM: beyond that the heaviest-first order evens them out.
+    const long long most = static_cast<long long>((max_q_len + kTiles * kRows - 1) / (kTiles * kRows)) * p.a.Hq * p.a.B;
+    const bool splits = p.a.B <= 32 && most <= 2 * p.num_sms;
+    const dim3 grid(static_cast<unsigned>(p.num_sms));
+    return launch_pdl(splits ? prefill_attn_latent_kernel<true> : prefill_attn_latent_kernel<false>, grid, dim3(kThreads), kSmemBytes, stream,
+                      p.a.pdl != 0, tm_k, tm_v, tm_r, p);
 }
 
 }  // namespace pd

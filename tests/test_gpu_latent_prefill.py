@@ -175,6 +175,20 @@ def test_prefill_more_items_than_blocks(batch):
     check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
 
 
+@pytest.mark.parametrize("heads,before,new", [(1, [9000], [1]), (8, [6000], [300]), (32, [4000], [128]), (5, [5000, 0, 40], [130, 600, 0]),
+                                              (3, [20000], [129]), (2, [1300, 2600, 10], [1, 1, 1]), (16, [0], [2304])])
+def test_prefill_few_items_on_long_contexts(heads, before, new):
+    """Contexts are cut into stretches whose partial results are joined: the same bits in every call, whatever ran in between."""
+    lens, pages, table, to, k, v, q = turn(before, new, heads, heads)
+    with Latent(heads, len(new), table.shape[1], pages.shape[0]) as ctx:
+        out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens)
+        other = np.asarray(lens) - np.asarray(new) // 2
+        prefill(ctx, q, np.asarray(new) - np.asarray(new) // 2, k, v, to, pages, table, other)
+        again, lse2 = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=int(max(new)) + 5)
+        assert torch.equal(out, again) and torch.equal(lse, lse2) and ctx.pd.pd_device_status(ctx.h)[0] == 0
+    check(out, lse, ol.prefill(f64(q), indptr_of(new), np.nan_to_num(f64(k)), np.nan_to_num(f64(v)), to, np.nan_to_num(f64(pages)), table, lens, SCALE32))
+
+
 def test_prefill_logits_that_rise_and_jump():
     new, before = [300], [500]
     for name in ("rise", "jump"):
