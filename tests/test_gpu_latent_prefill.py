@@ -244,6 +244,31 @@ def test_prefill_capture():
         assert torch.equal(out, want)
 
 
+def test_two_contexts_on_two_streams():
+    """Blocks of both calls share the SMs; neither waits for the other's."""
+    H, sides = 8, []
+    for n, (before, new) in enumerate((([7000, 20], [200, 300]), ([900, 0, 33], [130, 1, 513]))):
+        lens, pages, table, to, k, v, q = turn(before, new, H, 40 + n)
+        ctx = Latent(H, len(new), table.shape[1], pages.shape[0])
+        out = torch.empty((int(np.sum(new)), H, 128), dtype=torch.bfloat16, device=DEV)
+        args = (q, dev(indptr_of(new)), k, v, dev(to), pages, dev(table), dev(lens.astype(np.int32)), out)
+        sides.append((ctx, args, int(max(new)), torch.cuda.Stream()))
+    want = []
+    for ctx, args, m, _ in sides:
+        ctx.pd.pd_prefill_attn_latent(ctx.h, *args, max_q_len=m, sm_scale=SCALE)
+        torch.cuda.synchronize()
+        want.append(args[-1].clone())
+        args[-1].zero_()
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for ctx, args, m, stream in sides:
+            ctx.pd.pd_prefill_attn_latent(ctx.h, *args, max_q_len=m, sm_scale=SCALE, stream=stream)
+    torch.cuda.synchronize()
+    for (ctx, args, _, _), x in zip(sides, want):
+        assert torch.equal(args[-1], x) and ctx.pd.pd_device_status(ctx.h)[0] == 0
+        ctx.pd.pd_destroy(ctx.h)
+
+
 def test_expanded_pages_past_4_gb():
     """The last pages of pools of 5.2 GB each give what the first ones do."""
     H, NP = 64, 20000
