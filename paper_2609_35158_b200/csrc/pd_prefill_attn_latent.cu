@@ -11,7 +11,7 @@
 // products take 2560. With 80 columns of S and 40 of P beside them, S(j+1) waits only until the row threads hold the logits of
 // block j in registers, and runs during their softmax. What bounds it now is shared memory: an S product reads 4 KB of Q and
 // 2.5 KB of K in 51 cycles (128 bytes each), 1864 cycles a block with O, and the copies write 50 KB (400 cycles) beside that;
-// a block takes 2200. Eight turns, 9.6K new tokens on contexts of up to 18K, 32 heads: 1836 us, 1.20 PFLOP/s; under sustained load
+// a block takes 2200. Eight turns, 9.6K new tokens on contexts of up to 18K, 32 heads: 1.79 to 1.83 ms, 1.22 PFLOP/s; under sustained load
 // the power limit lowers the clock.
 // A page's 128 columns come as one box in the order [8-row group][64-column half][8 rows]: row groups follow one another
 // at the same distance across pages, as both operand forms want it.
