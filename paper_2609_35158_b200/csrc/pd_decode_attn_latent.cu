@@ -18,7 +18,7 @@
 // Softmax: one thread holds a quarter of the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
 // tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
 // than 32 log2 units (P and the sums keep fp32's exponent range, so 2^32 costs no accuracy): a tile needs one vote and no
-// reduction over tokens. P is rounded to bf16 (off by at most 2^-8 of itself: a second product for its remainder would make 128
+// reduction over tokens. Where it is raised the tile's weights are formed again from its logits. P is rounded to bf16 (off by at most 2^-8 of itself: a second product for its remainder would make 128
 // heads a third slower); the sum that normalises the output adds the rounded values, lse takes the unrounded sum.
 //
 // More than 64 heads go in groups: neighbouring CTAs read the same pages for different heads, the second one from L2.
@@ -33,6 +33,8 @@
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_tcgen05.cuh"
+
+#include <cfloat>
 
 namespace pd {
 
@@ -578,14 +580,14 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 if (i == 0) {
                     tile_max(m);  // (the last segment's products are over, P's buffer is free)
 #pragma unroll
-                    for (int k = 0; k < K; ++k) m[k] = fmaxf(m[k], -1e30f);
+                    for (int k = 0; k < K; ++k) m[k] = fmaxf(m[k], -FLT_MAX);  // (where the tile has no finite logit: below any that comes)
                 }
-                float x[K], e[K], over = -INFINITY;
+                float e[K], over = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    x[k] = dead ? -INFINITY : fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]);
-                    over = fmaxf(over, x[k]);
-                    e[k] = fast_exp2(x[k]);
+                    const float x = dead ? -INFINITY : fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]);
+                    over = fmaxf(over, x);
+                    e[k] = fast_exp2(x);
                 }
                 uint32_t pk[K / 2];
                 auto pack = [&]() {
@@ -605,8 +607,9 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                             float alpha = 1.f;
                             if (top[k] - m[k] > kRaise) {
                                 alpha = fast_exp2(m[k] - top[k]);
-                                e[k] = fast_exp2(x[k] + (m[k] - top[k]));
                                 m[k] = top[k];
+                                // from the logit again: its difference from the last reference has lost what a far lower one's rounding took
+                                e[k] = dead ? 0.f : fast_exp2(fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]));
                             }
                             l[k] *= alpha;
                             lr[k] *= alpha;

@@ -1,0 +1,64 @@
+"""Shared latent vectors whose first tokens have logits far below the others', as left padding or a mask in the key part gives them."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import latent as ol
+import workloads as wl
+from test_gpu_latent import DEV, Latent, P, cache_for, check, decode, f64
+
+pytestmark = pytest.mark.gpu
+
+# Logits are one product each, exact in fp32; what is left are the roundings of scale * log2(e), of differences below 2^5 and of 2^x: less
+# than 2^-18 of a logit's unit.
+SHIFT = 2.0 ** -18
+FACTORS = (1.0, 0.5, 0.25)          # what the heads multiply every logit by
+LOW_AND_BASE = [(-np.inf, 0), (-np.inf, 400), (-np.inf, -400), (-1e38, 0), (-1e38, 400), (-1e9, -400), (-1e8, 0), (-1e5, 0)]
+
+
+def masked_rows(rows, n_low, low, base, seed):
+    """Rows [n][576] whose first n_low tokens have the logit `low` and the others base plus one of -2, 0, 4, 6, through the key part alone."""
+    n = rows.shape[0]
+    logit = torch.from_numpy(base + np.random.default_rng(seed).choice([-2.0, 0.0, 4.0, 6.0], n)).to(rows.dtype)
+    logit[:n_low] = low
+    rows[:, 512:] = 0.0
+    rows[:, 512] = logit.to(rows.device)
+    return logit.double().numpy()
+
+
+def factors(heads):
+    return np.resize(FACTORS, heads)
+
+
+def attend(z, v, own_sum):
+    """(out, lse, out bound, lse bound) of one query's logits z [H][n], -inf not in every place, over v [n][D] or per head [H][n][D]."""
+    out, lse, bound = [], [], []
+    for h in range(len(z)):
+        top = z[h].max()
+        e = np.exp(z[h] - top)
+        o, b = ol._attend((e / e.sum())[None], v if v.ndim == 2 else v[h], np.array([SHIFT]), own_sum)
+        out.append(o[0]), bound.append(b[0]), lse.append(top + np.log(e.sum()))
+    lse = np.array(lse)
+    return np.array(out), lse, np.array(bound), SHIFT + 2.0 ** -18 + 2.0 ** -21 * np.abs(lse)
+
+
+@pytest.mark.parametrize("heads", [3, 20, 40, 100])
+@pytest.mark.parametrize("low,base", LOW_AND_BASE)
+def test_decode_behind_low_logits(heads, low, base):
+    n_low = [0, 1, 63, 64, 65, 130, 299]
+    lens = [300] * len(n_low)
+    pages, table = cache_for(lens, heads)
+    q = torch.zeros((len(lens), heads, 576), dtype=torch.bfloat16, device=DEV)
+    q[..., 512] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, k in enumerate(n_low):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:300].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = masked_rows(rows, k, low, base, b)
+        pages.view(-1, 576)[at] = rows
+        ref.append(attend(factors(heads)[:, None] * logit[None], f64(rows)[:, :512], True))
+    with Latent(heads, len(lens), table.shape[1], pages.shape[0]) as ctx:
+        for split in (0, 4, 7, 19, 40):            # from one tile a segment to whole sequences
+            out, lse = decode(ctx, q, pages, table, lens, scale=1.0, split=split)
+            check(out, lse, tuple(np.stack(x) for x in zip(*ref)))
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
