@@ -28,6 +28,8 @@
 #include "pd_ptx.cuh"
 #include "pd_tcgen05.cuh"
 
+#include <cfloat>
+
 namespace pd {
 
 namespace {
@@ -514,17 +516,17 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 if (lane == 0) mbar_arrive(bar_sfree + t * 8);  // S_t(j+1) may come
                 float sum = 0.f;
                 // x = s * scale - m against the reference as it stands, P = 2^x and its sum at once, so that the special-function unit
-                // starts with the first logits; the largest x is looked at behind them
+                // starts with the first logits; the largest logit is looked at behind them
                 auto weigh = [&]() {
                     const float2 nm2 = make_float2(-m_run, -m_run);
-                    float xm[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+                    float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     float2 a[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int c = 0; c < kBlock; c += 4) {
                         const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, nm2);
                         const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, nm2);
-                        xm[(c >> 2) & 1] = max3(xm[(c >> 2) & 1], x.x, x.y);
-                        xm[2 + ((c >> 2) & 1)] = max3(xm[2 + ((c >> 2) & 1)], y.x, y.y);
+                        top[(c >> 2) & 1] = max3(top[(c >> 2) & 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
+                        top[2 + ((c >> 2) & 1)] = max3(top[2 + ((c >> 2) & 1)], __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
                         const float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y)), f = make_float2(fast_exp2(y.x), fast_exp2(y.y));
                         a[0] = __fadd2_rn(a[0], e);
                         a[1] = __fadd2_rn(a[1], f);
@@ -532,7 +534,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         pk[(c >> 1) + 1] = pack_bf16x2(f.x, f.y);
                     }
                     sum = (a[0].x + a[0].y) + (a[1].x + a[1].y);
-                    return fmaxf(fmaxf(xm[0], xm[1]), fmaxf(xm[2], xm[3]));
+                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
                 };
                 if (__any_sync(0xffffffffu, masked)) {  // masked logits become -inf, their exponentials exact zeros
                     const int visible = my_pos - t0 + 1;
@@ -540,17 +542,18 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     for (int c = 0; c < kBlock; ++c)
                         if (c >= visible) v[c] = 0xff800000u;
                 }
-                if (j == 0) {  // the reference: the row's largest logit of the block, or 0 where it sees none of the stretch
+                if (j == 0) {  // the reference: the row's largest logit of the block; where there is no finite one, below any that comes
                     float top = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < kBlock; c += 2) top = max3(top, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-                    m_run = SPLITS && top == -INFINITY ? 0.f : top * p.scale_log2;
+                    m_run = fmaxf(top * p.scale_log2, -FLT_MAX);
                 }
-                const float xmax = weigh();
-                if (__any_sync(0xffffffffu, xmax > kRaise)) {
-                    // rare: the row's reference rises by its largest x, what it has accumulated is rescaled, and the block is weighed again
-                    const float shift = xmax > kRaise ? xmax : 0.f, alpha = fast_exp2(-shift);
-                    m_run += shift;
+                const float top = weigh();
+                if (__any_sync(0xffffffffu, top - m_run > kRaise)) {
+                    // rare: the row's reference rises to its largest logit, what it has accumulated is rescaled, and the block is weighed
+                    // again (its x have lost to their rounding what the last reference was lower)
+                    const float raised = top - m_run > kRaise ? top : m_run, alpha = fast_exp2(m_run - raised);
+                    m_run = raised;
                     if (j > 0) {
                         ok = mbar_wait(bar_o + t * 8, (done - 1) & 1);
                         tc_fence_after_sync();

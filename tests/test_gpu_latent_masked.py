@@ -6,6 +6,7 @@ import torch
 from oracle import latent as ol
 import workloads as wl
 from test_gpu_latent import DEV, Latent, P, cache_for, check, decode, f64
+from test_gpu_latent_prefill import prefill, turn
 
 pytestmark = pytest.mark.gpu
 
@@ -61,4 +62,29 @@ def test_decode_behind_low_logits(heads, low, base):
         for split in (0, 4, 7, 19, 40):            # from one tile a segment to whole sequences
             out, lse = decode(ctx, q, pages, table, lens, scale=1.0, split=split)
             check(out, lse, tuple(np.stack(x) for x in zip(*ref)))
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+@pytest.mark.parametrize("before,n_low,new", [([200] * 6, [0, 79, 80, 81, 160, 199], [70] * 6), ([2100, 1500], [1900, 700], [33, 150])])
+@pytest.mark.parametrize("low,base", LOW_AND_BASE)
+def test_prefill_behind_low_logits(before, n_low, new, low, base):
+    heads = 3
+    lens, pages, table, to, k, v, q = turn(before, new, heads, 3)
+    q.zero_()
+    q[..., 128] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, n in enumerate(lens):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:n].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = masked_rows(rows, n_low[b], low, base, b)
+        pages.view(-1, 576)[at] = rows
+        ids = torch.from_numpy(to[b, :-(-n // P)].astype(np.int64)).to(DEV)
+        values = f64(v[ids].transpose(0, 1).reshape(heads, -1, 128)[:, :n].contiguous())
+        for i in range(int(before[b]), n):
+            ref.append(attend(factors(heads)[:, None] * logit[None, :i + 1], values[:, :i + 1], False))
+    ref = tuple(np.stack(x) for x in zip(*ref))
+    with Latent(heads, len(new), table.shape[1], pages.shape[0]) as ctx:
+        for max_q in (max(new), 1000000):                   # the kernel that cuts contexts, and the one that does not
+            out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=max_q, scale=1.0)
+            check(out, lse, ref)
         assert ctx.pd.pd_device_status(ctx.h)[0] == 0
