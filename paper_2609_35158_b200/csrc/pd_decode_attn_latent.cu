@@ -15,7 +15,8 @@
 // The ring holds pairs of 64-column blocks (128 latents of a tile, 16 KB) and, apart, the rotated parts (8 KB): a tile's
 // pairs are handed back one by one as the output products pass over them, so nearly two tiles are in flight beside 72 KB of Q.
 //
-// Softmax: one thread holds a quarter of the heads of one token (tcgen05.ld 16x32bx2). A head's reference m is the same for all
+// Softmax: one thread holds a quarter of the heads of one token (tcgen05.ld 16x32bx2). Weights are 2^((s - m) scale): a scaled and rounded
+// m would be off by 2^-24 of itself, more than 2^x holds where logits are beyond 1e9. A head's reference m is the same for all
 // tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
 // than 32 log2 units (P and the sums keep fp32's exponent range, so 2^32 costs no accuracy): a tile needs one vote and no
 // reduction over tokens. Where it is raised the tile's weights are formed again from its logits. P is rounded to bf16 (off by at most 2^-8 of itself: a second product for its remainder would make 128
@@ -222,6 +223,11 @@ __device__ __forceinline__ void reduce_half_warp(float (&v)[K], int lane) {
             }
         }
     }
+}
+
+// Natural logarithm of sum * 2^(reference * scale).
+__device__ __forceinline__ float log_sum(float reference, float sum, float scale_log2) {
+    return fmaf(reference, scale_log2 * kLn2, log2f(sum) * kLn2);
 }
 
 template <int N>
@@ -568,7 +574,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 auto tile_max = [&](float (&top)[K]) {
                     float v[K];
 #pragma unroll
-                    for (int k = 0; k < K; ++k) v[k] = dead ? -INFINITY : __uint_as_float(sreg[k]) * p.a.scale_log2;
+                    for (int k = 0; k < K; ++k) v[k] = dead ? -INFINITY : __uint_as_float(sreg[k]);
                     reduce_half_warp<K, true>(v, lane);
                     scratch[wq * 64 + hb + lane % K] = v[0];
                     softmax_sync();
@@ -585,7 +591,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 float e[K], over = -INFINITY;
 #pragma unroll
                 for (int k = 0; k < K; ++k) {
-                    const float x = dead ? -INFINITY : fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]);
+                    const float x = dead ? -INFINITY : (__uint_as_float(sreg[k]) - m[k]) * p.a.scale_log2;
                     over = fmaxf(over, x);
                     e[k] = fast_exp2(x);
                 }
@@ -605,11 +611,11 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
 #pragma unroll
                         for (int k = 0; k < K; ++k) {
                             float alpha = 1.f;
-                            if (top[k] - m[k] > kRaise) {
-                                alpha = fast_exp2(m[k] - top[k]);
+                            if ((top[k] - m[k]) * p.a.scale_log2 > kRaise) {
+                                alpha = fast_exp2((m[k] - top[k]) * p.a.scale_log2);
                                 m[k] = top[k];
                                 // from the logit again: its difference from the last reference has lost what a far lower one's rounding took
-                                e[k] = dead ? 0.f : fast_exp2(fmaf(__uint_as_float(sreg[k]), p.a.scale_log2, -m[k]));
+                                e[k] = dead ? 0.f : fast_exp2((__uint_as_float(sreg[k]) - m[k]) * p.a.scale_log2);
                             }
                             l[k] *= alpha;
                             lr[k] *= alpha;
@@ -671,7 +677,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 const float slr = (sum_lr[tid] + sum_lr[64 + tid]) + (sum_lr[128 + tid] + sum_lr[192 + tid]);
                 if (s.whole) {
                     inv[tid] = 1.f / slr;
-                    if (p.a.lse != nullptr) p.a.lse[static_cast<size_t>(s.b) * p.a.Hq + h0 + tid] = (ref[tid] + log2f(sl)) * kLn2;
+                    if (p.a.lse != nullptr) p.a.lse[static_cast<size_t>(s.b) * p.a.Hq + h0 + tid] = log_sum(ref[tid], sl, p.a.scale_log2);
                 } else {
                     p.part_ml[static_cast<size_t>(s.slot) * p.a.Hq + h0 + tid] = make_float4(ref[tid], sl, slr, 0.f);
                 }
@@ -748,14 +754,14 @@ __global__ void __launch_bounds__(kMergeThreads) latent_merge_kernel(const Laten
 #pragma unroll
         for (int v = 0; v < VECS; ++v) o[v] = make_float4(0.f, 0.f, 0.f, 0.f);
         auto raise = [&](float top) {
-            const float keep = m == top ? 1.f : fast_exp2(m - top);
+            const float keep = m == top ? 1.f : fast_exp2((m - top) * p.a.scale_log2);
 #pragma unroll
             for (int v = 0; v < VECS; ++v) o[v].x *= keep, o[v].y *= keep, o[v].z *= keep, o[v].w *= keep;
             l *= keep, lr *= keep;
             m = top;
         };
         auto join = [&](float pm, float pl, float plr, const float4 (&x)[VECS]) {  // pm <= m
-            const float a = pm == -INFINITY ? 0.f : fast_exp2(pm - m);
+            const float a = pm == -INFINITY ? 0.f : fast_exp2((pm - m) * p.a.scale_log2);
 #pragma unroll
             for (int v = 0; v < VECS; ++v)
                 o[v].x = fmaf(a, x[v].x, o[v].x), o[v].y = fmaf(a, x[v].y, o[v].y), o[v].z = fmaf(a, x[v].z, o[v].z), o[v].w = fmaf(a, x[v].w, o[v].w);
@@ -804,7 +810,7 @@ __global__ void __launch_bounds__(kMergeThreads) latent_merge_kernel(const Laten
 #pragma unroll
         for (int v = 0; v < VECS; ++v)
             if (group == 0) out[v * LANES] = make_uint2(pack_bf16x2(o[v].x * inv, o[v].y * inv), pack_bf16x2(o[v].z * inv, o[v].w * inv));
-        if (piece == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = (m + log2f(l)) * kLn2;
+        if (piece == 0 && lane == 0 && p.a.lse != nullptr) p.a.lse[row] = log_sum(m, l, p.a.scale_log2);
     }
 }
 

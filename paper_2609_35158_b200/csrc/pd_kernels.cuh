@@ -198,7 +198,7 @@ constexpr int kLatentSegmentPages = 8;       // what a segment of the decode ker
 
 struct LatentAttnParams {
     AttnParams a;                // q [B][Hq][576], out [B][Hq][512], part_o [slots][Hq][512]
-    float4 *part_ml;             // [slots][Hq] reference (log2 units), sum, sum of the rounded weights
+    float4 *part_ml;             // [slots][Hq] reference (a logit before scaling), sum, sum of the rounded weights
     int32_t groups, heads;       // groups of at most 64 heads, heads per group
     int32_t extra;               // units a sequence counts in the plan beside its pages
 };

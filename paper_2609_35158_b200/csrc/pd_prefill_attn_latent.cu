@@ -94,6 +94,11 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
         : "memory");
 }
 
+// Natural logarithm of sum * 2^(reference * scale).
+__device__ __forceinline__ float log_sum(float reference, float sum, float scale_log2) {
+    return fmaf(reference, scale_log2 * kLn2f, log2f(sum) * kLn2f);
+}
+
 // Every item starts the rings at slot 0. Bit s: whether its nb blocks fill slot s an odd number of times.
 template <int SLOTS>
 __device__ __forceinline__ uint32_t fills(int nb) {
@@ -515,16 +520,17 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_sfree + t * 8);  // S_t(j+1) may come
                 float sum = 0.f;
-                // x = s * scale - m against the reference as it stands, P = 2^x and its sum at once, so that the special-function unit
-                // starts with the first logits; the largest logit is looked at behind them
+                // x = (s - m) * scale against the reference as it stands, P = 2^x and its sum at once, so that the special-function unit
+                // starts with the first logits; the largest logit is looked at behind them. The difference comes first: s * scale - m with a
+                // rounded m is off by 2^-24 of m, more than 2^x holds where logits are beyond 1e9 (1 % more time on long turns)
                 auto weigh = [&]() {
                     const float2 nm2 = make_float2(-m_run, -m_run);
                     float top[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
                     float2 a[2] = {make_float2(0.f, 0.f), make_float2(0.f, 0.f)};
 #pragma unroll
                     for (int c = 0; c < kBlock; c += 4) {
-                        const float2 x = __ffma2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), sc2, nm2);
-                        const float2 y = __ffma2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), sc2, nm2);
+                        const float2 x = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(v[c]), __uint_as_float(v[c + 1])), nm2), sc2);
+                        const float2 y = __fmul2_rn(__fadd2_rn(make_float2(__uint_as_float(v[c + 2]), __uint_as_float(v[c + 3])), nm2), sc2);
                         top[(c >> 2) & 1] = max3(top[(c >> 2) & 1], __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
                         top[2 + ((c >> 2) & 1)] = max3(top[2 + ((c >> 2) & 1)], __uint_as_float(v[c + 2]), __uint_as_float(v[c + 3]));
                         const float2 e = make_float2(fast_exp2(x.x), fast_exp2(x.y)), f = make_float2(fast_exp2(y.x), fast_exp2(y.y));
@@ -534,7 +540,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         pk[(c >> 1) + 1] = pack_bf16x2(f.x, f.y);
                     }
                     sum = (a[0].x + a[0].y) + (a[1].x + a[1].y);
-                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * p.scale_log2;
+                    return fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3]));
                 };
                 if (__any_sync(0xffffffffu, masked)) {  // masked logits become -inf, their exponentials exact zeros
                     const int visible = my_pos - t0 + 1;
@@ -546,13 +552,13 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     float top = -INFINITY;
 #pragma unroll
                     for (int c = 0; c < kBlock; c += 2) top = max3(top, __uint_as_float(v[c]), __uint_as_float(v[c + 1]));
-                    m_run = fmaxf(top * p.scale_log2, -FLT_MAX);
+                    m_run = fmaxf(top, -FLT_MAX);
                 }
                 const float top = weigh();
-                if (__any_sync(0xffffffffu, top - m_run > kRaise)) {
+                if (__any_sync(0xffffffffu, (top - m_run) * p.scale_log2 > kRaise)) {
                     // rare: the row's reference rises to its largest logit, what it has accumulated is rescaled, and the block is weighed
                     // again (its x have lost to their rounding what the last reference was lower)
-                    const float raised = top - m_run > kRaise ? top : m_run, alpha = fast_exp2(m_run - raised);
+                    const float raised = (top - m_run) * p.scale_log2 > kRaise ? top : m_run, alpha = fast_exp2((m_run - raised) * p.scale_log2);
                     m_run = raised;
                     if (j > 0) {
                         ok = mbar_wait(bar_o + t * 8, (done - 1) & 1);
@@ -627,7 +633,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         if (c == kLatentHead - 32) o_read();
                         if (row_valid) store_cols(orow + c, o, inv, wide);
                     }
-                    if (p.lse != nullptr && row_valid) p.lse[at] = (m_run + log2f(l_run)) * kLn2f;
+                    if (p.lse != nullptr && row_valid) p.lse[at] = log_sum(m_run, l_run, p.scale_log2);
                 }
             } else if (t * kRows < it->n_tok) {
                 // A partial result; the warp that counts the last stretch of its 32 rows joins them, in their order.
@@ -663,7 +669,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     }
                     for (int i = 0; i < parts; ++i) {
                         const float2 ml = __ldcg(ml_of(i));
-                        if (!(ml.y == 0.f)) sum += ml.y * fast_exp2(ml.x - top);
+                        if (!(ml.y == 0.f)) sum += ml.y * fast_exp2((ml.x - top) * p.scale_log2);
                     }
                     const float inv = 1.f / sum;
 #pragma unroll 1
@@ -673,7 +679,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         for (int i = 0; i < parts; ++i) {
                             const float2 ml = __ldcg(ml_of(i));
                             const bool seen = !(ml.y == 0.f);  // a tile without blocks in a stretch has written no outputs
-                            const float w = seen ? fast_exp2(ml.x - top) : 0.f;
+                            const float w = seen ? fast_exp2((ml.x - top) * p.scale_log2) : 0.f;
                             const float *from = part_of(i) + at_row + c * kRows;
 #pragma unroll
                             for (int k = 0; k < 8; ++k) {
@@ -686,7 +692,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         for (int k = 0; k < 32; ++k) o[k] = __float_as_uint(acc[k]);
                         if (row_valid) store_cols(orow + c, o, inv, wide);
                     }
-                    if (p.lse != nullptr && row_valid) p.lse[at] = (top + log2f(sum)) * kLn2f;
+                    if (p.lse != nullptr && row_valid) p.lse[at] = log_sum(top, sum, p.scale_log2);
                 }
             }
             __syncwarp();

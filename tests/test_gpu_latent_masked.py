@@ -88,3 +88,59 @@ def test_prefill_behind_low_logits(before, n_low, new, low, base):
             out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=max_q, scale=1.0)
             check(out, lse, ref)
         assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+def huge_rows(rows, size, seed):
+    """Rows whose logits are `size` or the next bf16 value below it (half of each), or `size` alone where the seed is even."""
+    n = rows.shape[0]
+    logit = torch.full((n,), size, dtype=rows.dtype)
+    if seed % 2:
+        logit[np.random.default_rng(seed).permutation(n)[:n // 2]] = size * (1 - np.sign(size) * 2.0 ** -7)
+    rows[:, 512:] = 0.0
+    rows[:, 512] = logit.to(rows.device)
+    return logit.double().numpy()
+
+
+@pytest.mark.parametrize("size", [-1e38, -1e30, -1e10, -3e9, 3e9, 1e10, 1e30, 1e38])
+def test_decode_of_huge_logits(size):
+    """Only their differences count: equal ones share the weight, however large they are."""
+    heads, lens = 20, [300, 300, 50, 50, 1, 150]
+    pages, table = cache_for(lens, heads)
+    q = torch.zeros((len(lens), heads, 576), dtype=torch.bfloat16, device=DEV)
+    q[..., 512] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, n in enumerate(lens):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:n].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = huge_rows(rows, size, b)
+        pages.view(-1, 576)[at] = rows
+        ref.append(attend(factors(heads)[:, None] * logit[None], f64(rows)[:, :512], True))
+    with Latent(heads, len(lens), table.shape[1], pages.shape[0]) as ctx:
+        for split in (0, 7, 40):
+            out, lse = decode(ctx, q, pages, table, lens, scale=1.0, split=split)
+            check(out, lse, tuple(np.stack(x) for x in zip(*ref)))
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+@pytest.mark.parametrize("size", [-1e38, -1e30, -1e10, -3e9, 3e9, 1e10, 1e30, 1e38])
+def test_prefill_of_huge_logits(size):
+    heads, before, new = 3, [0, 50, 2500], [90, 140, 20]
+    lens, pages, table, to, k, v, q = turn(before, new, heads, 5)
+    q.zero_()
+    q[..., 128] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, n in enumerate(lens):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:n].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = huge_rows(rows, size, b)
+        pages.view(-1, 576)[at] = rows
+        ids = torch.from_numpy(to[b, :-(-n // P)].astype(np.int64)).to(DEV)
+        values = f64(v[ids].transpose(0, 1).reshape(heads, -1, 128)[:, :n].contiguous())
+        for i in range(int(before[b]), n):
+            ref.append(attend(factors(heads)[:, None] * logit[None, :i + 1], values[:, :i + 1], False))
+    ref = tuple(np.stack(x) for x in zip(*ref))
+    with Latent(heads, len(new), table.shape[1], pages.shape[0]) as ctx:
+        for max_q in (max(new), 1000000):
+            out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=max_q, scale=1.0)
+            check(out, lse, ref)
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
