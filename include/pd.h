@@ -563,7 +563,9 @@ int pd_rope_append_tokens_latent(pd_ctx *ctx, const pd_rope_config *rope, const 
  * lse [batch][num_q_heads] fp32 or NULL. out[b][h] = softmax(sm_scale * q[b][h] . (c, r)) c over the ctx_lens[b] cached tokens;
  * empty contexts, unread slots, sm_scale, split_pages (pages per range of the flattened (sequence, page) list) and error behaviour
  * as in pd_decode_attn. Results are bit-reproducible. Probabilities are rounded to bf16 before the second product; the
- * sum that normalises the output adds the rounded ones, lse the unrounded.
+ * sum that normalises the output adds the rounded ones, lse the unrounded. Logits may have any size; a token of logit -inf has no
+ * weight, and a row without any other gives 0 and lse -inf, here and in pd_prefill_attn_latent. (The weights are relative to a reference that
+ * later tokens may exceed by 2^32 before it is raised: latents and values of V stay below 2^60 in magnitude.)
  */
 int pd_decode_attn_latent(pd_ctx *ctx, const void *q, const void *kv_pages, const int32_t *page_table, const int32_t *ctx_lens,
                           void *out, float *lse, int32_t batch, float sm_scale, int32_t split_pages, void *stream);

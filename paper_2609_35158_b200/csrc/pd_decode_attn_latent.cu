@@ -676,7 +676,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
                 const float sl = (sum_l[tid] + sum_l[64 + tid]) + (sum_l[128 + tid] + sum_l[192 + tid]);
                 const float slr = (sum_lr[tid] + sum_lr[64 + tid]) + (sum_lr[128 + tid] + sum_lr[192 + tid]);
                 if (s.whole) {
-                    inv[tid] = 1.f / slr;
+                    inv[tid] = slr == 0.f ? 0.f : 1.f / slr;  // 0: every logit was -inf, as in an empty context
                     if (p.a.lse != nullptr) p.a.lse[static_cast<size_t>(s.b) * p.a.Hq + h0 + tid] = log_sum(ref[tid], sl, p.a.scale_log2);
                 } else {
                     p.part_ml[static_cast<size_t>(s.slot) * p.a.Hq + h0 + tid] = make_float4(ref[tid], sl, slr, 0.f);
@@ -806,7 +806,7 @@ __global__ void __launch_bounds__(kMergeThreads) latent_merge_kernel(const Laten
                 }
             }
         }
-        const float inv = 1.f / lr;
+        const float inv = lr == 0.f ? 0.f : 1.f / lr;
 #pragma unroll
         for (int v = 0; v < VECS; ++v)
             if (group == 0) out[v * LANES] = make_uint2(pack_bf16x2(o[v].x * inv, o[v].y * inv), pack_bf16x2(o[v].z * inv, o[v].w * inv));

@@ -624,7 +624,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             __nv_bfloat16 *orow = p.out + at * kLatentHead;
             if (!SPLITS || it->parts == 1) {
                 if (my_nb > 0) {
-                    const float inv = 1.f / l_run;
+                    const float inv = l_run == 0.f ? 0.f : 1.f / l_run;  // 0: the row sees nothing but -inf
 #pragma unroll
                     for (int c = 0; c < kLatentHead; c += 32) {
                         uint32_t o[32];
@@ -671,7 +671,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                         const float2 ml = __ldcg(ml_of(i));
                         if (!(ml.y == 0.f)) sum += ml.y * fast_exp2((ml.x - top) * p.scale_log2);
                     }
-                    const float inv = 1.f / sum;
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll 1
                     for (int c = 0; c < kLatentHead; c += 32) {
                         float acc[32] = {};

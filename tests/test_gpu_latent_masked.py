@@ -144,3 +144,50 @@ def test_prefill_of_huge_logits(size):
             out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=max_q, scale=1.0)
             check(out, lse, ref)
         assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+def test_decode_of_sequences_masked_altogether():
+    """Every logit -inf: as an empty context, zeros and a logarithm of -inf; its neighbours are not touched."""
+    heads, lens, gone = 20, [300, 40, 300, 1, 130], [True, False, False, True, True]
+    pages, table = cache_for(lens, heads)
+    q = torch.zeros((len(lens), heads, 576), dtype=torch.bfloat16, device=DEV)
+    q[..., 512] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, n in enumerate(lens):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:n].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = masked_rows(rows, n if gone[b] else 0, -np.inf, 0, b)
+        pages.view(-1, 576)[at] = rows
+        zeros = (np.zeros((heads, 512)), np.full(heads, -np.inf), np.zeros((heads, 512)), np.zeros(heads))
+        ref.append(zeros if gone[b] else attend(factors(heads)[:, None] * logit[None], f64(rows)[:, :512], True))
+    with Latent(heads, len(lens), table.shape[1], pages.shape[0]) as ctx:
+        for split in (0, 1, 7, 40):
+            out, lse = decode(ctx, q, pages, table, lens, scale=1.0, split=split)
+            check(out, lse, tuple(np.stack(x) for x in zip(*ref)))
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+@pytest.mark.parametrize("before,n_low,new", [([0, 0, 100], [30, 200, 0], [90, 200, 5]), ([2000, 0], [2300, 10], [300, 20])])
+def test_prefill_of_rows_masked_altogether(before, n_low, new):
+    """Rows that see -inf alone, ahead of rows that see more: zeros and a logarithm of -inf."""
+    heads = 3
+    lens, pages, table, to, k, v, q = turn(before, new, heads, 7)
+    q.zero_()
+    q[..., 128] = torch.from_numpy(factors(heads)).to(DEV)
+    ref = []
+    for b, n in enumerate(lens):
+        at = torch.from_numpy((table[b].repeat(P) * P + np.tile(np.arange(P), table.shape[1]))[:n].astype(np.int64)).to(DEV)
+        rows = pages.view(-1, 576)[at]
+        logit = masked_rows(rows, n_low[b], -np.inf, 0, b)
+        pages.view(-1, 576)[at] = rows
+        ids = torch.from_numpy(to[b, :-(-n // P)].astype(np.int64)).to(DEV)
+        values = f64(v[ids].transpose(0, 1).reshape(heads, -1, 128)[:, :n].contiguous())
+        zeros = (np.zeros((heads, 128)), np.full(heads, -np.inf), np.zeros((heads, 128)), np.zeros(heads))
+        for i in range(int(before[b]), n):
+            ref.append(zeros if i < n_low[b] else attend(factors(heads)[:, None] * logit[None, :i + 1], values[:, :i + 1], False))
+    ref = tuple(np.stack(x) for x in zip(*ref))
+    with Latent(heads, len(new), table.shape[1], pages.shape[0]) as ctx:
+        for max_q in (max(new), 1000000):
+            out, lse = prefill(ctx, q, new, k, v, to, pages, table, lens, max_q=max_q, scale=1.0)
+            check(out, lse, ref)
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
