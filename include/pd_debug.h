@@ -65,6 +65,13 @@ int pd_read_probe(const void *src, size_t bytes, int32_t blocks, int32_t threads
  */
 int pd_rope_turns(float inv_freq, uint64_t *turns);
 
+/*
+ * Leaves the workspace of a PD_FLAG_LATENT context as a pd_prefill_attn_latent that gave up a wait may leave it: the last call's count of finished
+ * stretches of a cut context stands at `stretches` (not negative) for every group of rows. The calls that follow must not notice; this lets
+ * a test see that without a failing kernel. Waits for `stream`.
+ */
+int pd_leave_arrivals(pd_ctx *ctx, int32_t stretches, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

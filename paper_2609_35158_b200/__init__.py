@@ -37,7 +37,7 @@ EXPORTS = (
     "pd_rope_append_tokens_latent", "pd_decode_attn_latent", "pd_kv_expand_latent", "pd_prefill_attn_latent",
     "pd_pool_create", "pd_pool_resize", "pd_pool_base", "pd_pool_capacity", "pd_pool_chunk_bytes", "pd_pool_resident_bytes",
     "pd_pool_last_error", "pd_pool_destroy",
-    "pd_set_profile_events", "pd_read_probe", "pd_rope_turns", "pd_host_step_counts", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
+    "pd_set_profile_events", "pd_read_probe", "pd_rope_turns", "pd_host_step_counts", "pd_leave_arrivals", "pd_workspace_bytes", "pd_launch_count", "pd_last_plan", "pd_status_string", "pd_last_error", "pd_version",
 )
 
 
@@ -95,6 +95,7 @@ def _load() -> ctypes.CDLL:
     lib.pd_set_profile_events.argtypes = [vp, vp, vp]
     lib.pd_read_probe.argtypes = [vp, ctypes.c_size_t, i32, i32, vp, vp]
     lib.pd_host_step_counts.argtypes = [vp, ctypes.POINTER(i64), ctypes.POINTER(i64)]
+    lib.pd_leave_arrivals.argtypes = [vp, i32, vp]
     lib.pd_read_worker_trace.argtypes = [vp, vp, vp, i32, ctypes.POINTER(i32)]
     lib.pd_workspace_bytes.argtypes = [vp, ctypes.POINTER(ctypes.c_size_t)]
     lib.pd_launch_count.argtypes = [vp, ctypes.POINTER(i64)]
@@ -559,6 +560,11 @@ def pd_host_step_counts(ctx):
     d, s = ctypes.c_int64(0), ctypes.c_int64(0)
     _check(_lib.pd_host_step_counts(ctx, ctypes.byref(d), ctypes.byref(s)), "pd_host_step_counts", ctx)
     return int(d.value), int(s.value)
+
+
+def pd_leave_arrivals(ctx, stretches: int, stream=None) -> None:
+    """For tests: a latent context's workspace as a prefill that gave up a wait may leave it."""
+    _check(_lib.pd_leave_arrivals(ctx, stretches, _stream(stream)), "pd_leave_arrivals", ctx)
 
 
 def pd_read_probe(src, blocks: int, threads: int, sink, stream=None) -> None:

@@ -90,7 +90,7 @@ struct pd_ctx {
     alignas(64) CUtensorMap tm_latent{}, tm_latent_pairs{};
     alignas(64) CUtensorMap tm_latent_q{};
     float4 *part_ml4 = nullptr;
-    int32_t *arrived = nullptr;  // latent prefill: stretches of 32 rows that are done, zero between calls
+    int32_t *arrived = nullptr;  // latent prefill: two sets of counts of stretches that are done, and the calls so far
     int32_t max_parts = 0;       // ... and the partial results there is room for
     bool prefill_ready = false;
     bool fp8_ready = false;
@@ -330,7 +330,7 @@ int pd_create(const pd_config *cfg, pd_ctx **out) {
     if (latent) {  // prefill's partial results share the space: two per SM
         ctx->max_parts = 2 * ctx->num_sms;
         b_part_o = std::max(b_part_o, round256(ctx->max_parts * pd::kLatentPrefillPartBytes));
-        b_arrived = round256(static_cast<size_t>(ctx->max_parts) * 8 * sizeof(int32_t));
+        b_arrived = round256((2 * static_cast<size_t>(ctx->max_parts) * 8 + 1) * sizeof(int32_t));
     }
     const size_t b_part_ml = round256(ctx->slots * group * (latent ? sizeof(float4) : sizeof(float2)));
     const size_t b_cum = round256((static_cast<size_t>(cfg->max_batch) + 1) * sizeof(int32_t));
@@ -1256,10 +1256,6 @@ int pd_device_status(pd_ctx *ctx, void *stream, int32_t *code, int32_t *seq, int
     if (err == cudaSuccess) err = cudaMemsetAsync(ctx->status, 0, sizeof host, s);
     if (err == cudaSuccess) err = cudaStreamSynchronize(s);
     if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "status read", err);
-    if (host[0] == pd::kDevTimeout && ctx->max_parts > 0) {  // a latent prefill that gave up may have left counts behind
-        err = cudaMemsetAsync(ctx->arrived, 0, static_cast<size_t>(ctx->max_parts) * 8 * sizeof(int32_t), s);
-        if (err != cudaSuccess) return fail(ctx, PD_ERR_CUDA, "status read", err);
-    }
     int rc = PD_OK;
     if (host[0] == pd::kDevBadPage || host[0] == pd::kDevBadLength) rc = PD_ERR_DEVICE_FAULT;
     else if (host[0] == pd::kDevTimeout) rc = PD_ERR_TIMEOUT;
@@ -1267,6 +1263,23 @@ int pd_device_status(pd_ctx *ctx, void *stream, int32_t *code, int32_t *seq, int
     if (seq != nullptr) *seq = rc == PD_OK ? -1 : host[1];
     if (detail != nullptr) *detail = rc == PD_OK ? 0 : host[2];
     return rc;
+}
+
+int pd_leave_arrivals(pd_ctx *ctx, int32_t stretches, void *stream) {
+    if (ctx == nullptr || stretches < 0) return PD_ERR_INVALID_ARG;
+    if (!ctx->latent) return fail(ctx, PD_ERR_UNSUPPORTED, "the call needs a context created with PD_FLAG_LATENT");
+    DeviceGuard guard(ctx->cfg.device);
+    if (!guard.ok) return fail(ctx, PD_ERR_CUDA, "cudaSetDevice");
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int32_t groups = ctx->max_parts * 8;
+    int32_t calls = 0;
+    cudaError_t err = cudaMemcpyAsync(&calls, ctx->arrived + 2 * groups, sizeof calls, cudaMemcpyDeviceToHost, s);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(s);
+    int32_t *last = ctx->arrived + ((calls & 1) ^ 1) * groups;
+    for (int32_t i = 0; i < groups && err == cudaSuccess; ++i)
+        err = cudaMemcpyAsync(last + i, &stretches, sizeof stretches, cudaMemcpyHostToDevice, s);
+    if (err == cudaSuccess) err = cudaStreamSynchronize(s);
+    return err == cudaSuccess ? PD_OK : fail(ctx, PD_ERR_CUDA, "pd_leave_arrivals", err);
 }
 
 int pd_plan_ranges(int64_t total_units, int32_t n_workers, int32_t split_pages, int32_t max_ranges, int32_t min_pages,

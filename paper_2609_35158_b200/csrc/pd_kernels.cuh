@@ -240,7 +240,9 @@ struct LatentPrefillParams {
     int32_t num_sms;
     int32_t max_parts;           // partial results there is room for
     float *part;                 // [max_parts] of kLatentPrefillPartBytes
-    int32_t *arrived;            // [max_parts][8] stretches of a group of 32 rows that are done; zero between calls
+    // [2][max_parts][8] stretches of a group of 32 rows that are done, then the calls so far. Calls use the two sets in turn and clear the other one:
+    // what a call leaves whose waits ran out is never part of a count.
+    int32_t *arrived;
 };
 constexpr size_t kLatentPrefillPartBytes = 2 * (128 * 128 + 2 * 128) * sizeof(float);
 

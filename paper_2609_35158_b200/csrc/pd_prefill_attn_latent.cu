@@ -128,6 +128,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
     extern __shared__ uint8_t smem_raw[];
     __shared__ uint32_t tmem_slot;
     __shared__ Item items[kItemSlots];
+    __shared__ int32_t arrived_set;  // where this call counts stretches
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     constexpr int kItemTok = kTiles * kRows;
 
@@ -259,8 +260,15 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     if (lane >= o) incl += x;
                 }
             };
+            const int groups = lp.max_parts * kSoftmaxWarps;
+            const int calls = SPLITS ? __ldcg(lp.arrived + 2 * groups) : 0;
             int idx = blockIdx.x, before = 0, w = 0;
             window(0);
+            if (SPLITS) {
+                const int set = calls & 1;
+                for (int i = blockIdx.x * 32 + lane; i < groups; i += gridDim.x * 32) lp.arrived[(set ^ 1) * groups + i] = 0;
+                if (lane == 0) arrived_set = set * groups;  // (read behind the first item)
+            }
             for (int k = 0; ok; ++k) {
                 while (w * 32 < p.B && idx >= before + __shfl_sync(0xffffffffu, incl, 31)) {
                     before += __shfl_sync(0xffffffffu, incl, 31);
@@ -318,6 +326,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 if (atomicAdd(p.status + kSchedDone, 1) == static_cast<int>(gridDim.x) - 1) {
                     p.status[kSchedNext] = 0;
                     p.status[kSchedDone] = 0;
+                    if (SPLITS) lp.arrived[2 * groups] = calls + 1;  // (every block has read it)
                 }
             }
         } else if (warp == kSoftmaxWarps) {
@@ -654,13 +663,12 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     }
                 }
                 *ml_of(mine) = make_float2(m_run, l_run);
-                int32_t *arrived = lp.arrived + it->first * kSoftmaxWarps + warp;
+                int32_t *arrived = lp.arrived + arrived_set + it->first * kSoftmaxWarps + warp;
                 int before = 0;
                 __threadfence();
                 __syncwarp();
                 if (lane == 0) before = atomicAdd(arrived, 1);
                 if (__shfl_sync(0xffffffffu, before, 0) == parts - 1) {
-                    if (lane == 0) *arrived = 0;
                     __threadfence();
                     float top = -INFINITY, sum = 0.f;
                     for (int i = 0; i < parts; ++i) {
