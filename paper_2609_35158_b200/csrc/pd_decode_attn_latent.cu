@@ -714,6 +714,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             softmax_sync();
             if (lane == 0) mbar_arrive(bar_o);
         }
+        ok = __all_sync(0xffffffffu, ok);
         if (!ok && lane == 0) latch_status(p.a.status, kDevTimeout, s.b, blockIdx.x);
     }
     __syncwarp();

@@ -486,7 +486,10 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 cp_async16(a, src + static_cast<size_t>(min(r, rows - 1)) * p.Hq * kQDim + c * 8, r < rows ? 16 : 0);
             }
         };
+        // A wait that runs out may do so in some lanes of a warp: those go on without waiting, since the others need them in what the warp does
+        // together, until the warp decides as one at the item's end.
         const Item *it = &next_item(), *after = it;
+        ok = __all_sync(0xffffffffu, ok);
         if (ok && it->n_tok > 0) copy_q(*it);
         while (ok && it->n_tok > 0) {
             const int my_nb = t == 0 ? it->nb0 : it->nb1;
@@ -500,10 +503,9 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
             }
             float m_run = 0.f, l_run = 0.f;
             const float2 sc2 = make_float2(p.scale_log2, p.scale_log2);
-            for (int j = 0; j < my_nb && ok; ++j, ++done) {
-                ok = mbar_wait(bar_s + t * 8, done & 1);
+            for (int j = 0; j < my_nb; ++j, ++done) {
+                ok = ok && mbar_wait(bar_s + t * 8, done & 1);
                 tc_fence_after_sync();
-                if (!ok) break;
                 const int t0 = ((SPLITS ? it->j0 : 0) + j) * kBlock;
                 const bool masked = t0 + kBlock - 1 > my_pos;  // the block reaches past this row's position
                 // V rows past the context inside the last page may hold NaN; 0 * NaN is NaN, so the warpgroup whose products of
@@ -512,8 +514,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     const int valid_rows = it->len - t0;
                     const int last = min(kBlock, (valid_rows + kPageSize - 1) / kPageSize * kPageSize);
                     const int slot = j % kVSlots;
-                    ok = mbar_wait(bar_v + slot * 8, (v_mask >> slot ^ j / kVSlots) & 1);  // it must have landed
-                    if (!ok) break;
+                    ok = ok && mbar_wait(bar_v + slot * 8, (v_mask >> slot ^ j / kVSlots) & 1);  // it must have landed
                     for (int x = row; x < (last - valid_rows) * (kLatentHead / 8); x += kRows) {
                         const int r = valid_rows + x / (kLatentHead / 8), c = x % (kLatentHead / 8);
                         st_shared_zero16(v_ring + slot * kKvBytes + (r >> 3) * 2048 + (c >> 3) * 1024 + (r & 7) * 128 + (c & 7) * 16);
@@ -570,7 +571,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     const float raised = (top - m_run) * p.scale_log2 > kRaise ? top : m_run, alpha = fast_exp2((m_run - raised) * p.scale_log2);
                     m_run = raised;
                     if (j > 0) {
-                        ok = mbar_wait(bar_o + t * 8, (done - 1) & 1);
+                        ok = ok && mbar_wait(bar_o + t * 8, (done - 1) & 1);
                         tc_fence_after_sync();
 #pragma unroll 1
                         for (int c = 0; c < kLatentHead; c += 16) {
@@ -588,7 +589,6 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 }
                 l_run += sum;
                 ok = ok && mbar_wait(bar_o + t * 8, (done & 1) ^ 1);  // P_t has been used by the last block's product
-                if (!ok) break;
                 tc_fence_after_sync();
                 tmem_st16(p_buf, *reinterpret_cast<uint32_t(*)[16]>(pk));
                 tmem_st16(p_buf + 16, *reinterpret_cast<uint32_t(*)[16]>(pk + 16));
@@ -598,9 +598,10 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_p + t * 8);
             }
-            if (!ok) break;
             after = &next_item();  // this item's last logits are in registers: the next one's queries may come
-            if (ok && after->n_tok > 0) copy_q(*after);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            if (after->n_tok > 0) copy_q(*after);
             v_mask ^= fills<kVSlots>(max(it->nb0, it->nb1));
 
             // ---- O_t / l -> bf16 rows
@@ -624,7 +625,7 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                 if (lane == 0) mbar_arrive(bar_done + t * 8);
             };
             if (my_nb > 0) {
-                ok = mbar_wait(bar_o + t * 8, (done - 1) & 1);
+                ok = __all_sync(0xffffffffu, mbar_wait(bar_o + t * 8, (done - 1) & 1));
                 if (!ok) break;
                 tc_fence_after_sync();
             }
