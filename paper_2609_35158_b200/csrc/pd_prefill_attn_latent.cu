@@ -737,7 +737,7 @@ cudaError_t launch_prefill_attn_latent(const CUtensorMap &tm_k, const CUtensorMa
     }
     *launched += 1;
     // Contexts are cut only where there may be fewer than two items per SM: beyond that the heaviest-first order evens them out.
-    const long long most = static_cast<long long>((max_q_len + kTiles * kRows - 1) / (kTiles * kRows)) * p.a.Hq * p.a.B;
+    const long long most = static_cast<long long>((max_q_len - 1) / (kTiles * kRows) + 1) * p.a.Hq * p.a.B;
     const bool splits = p.a.B <= 32 && most <= 2 * p.num_sms;
     const dim3 grid(static_cast<unsigned>(p.num_sms));
     return launch_pdl(splits ? prefill_attn_latent_kernel<true> : prefill_attn_latent_kernel<false>, grid, dim3(kThreads), kSmemBytes, stream,

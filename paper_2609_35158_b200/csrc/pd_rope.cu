@@ -238,7 +238,7 @@ cudaError_t launch_rope(const RopeParams &base, int append, int max_q_len, int n
     if (append == kAppendQ4 && p.tile > kRopeRowBytes / (p.Hkv * p.D * 2)) p.tile = kRopeRowBytes / (p.Hkv * p.D * 2);
     if (append == kAppendQ4 && p.Hkv * p.D * 2 > kRopeRowBytes) return cudaErrorInvalidValue;
     p.tile = p.tile < 1 ? 1 : (p.tile > most_tokens ? most_tokens : p.tile);
-    const int tiles = (max_q_len + p.tile - 1) / p.tile, want = (num_sms * 64 + seqs - 1) / seqs;
+    const int tiles = (max_q_len - 1) / p.tile + 1, want = (num_sms * 64 + seqs - 1) / seqs;
     const dim3 grid(tiles < want ? tiles : want, seqs);
     p.single = max_q_len == 1;
     const size_t dyn = append == kAppendQ4 ? static_cast<size_t>(p.tile) * p.Hkv * p.D * 2 : 0;

@@ -188,7 +188,7 @@ cudaError_t launch_rope_append_latent(const LatentAppendParams &base, int max_q_
     if (most <= 0) return cudaSuccess;
     // one token per CTA until that fills the device
     p.tile = most <= num_sms * 8 ? 1 : kMaxTile;
-    const int tiles = (max_q_len + p.tile - 1) / p.tile, want = (num_sms * 64 + p.B - 1) / p.B;
+    const int tiles = (max_q_len - 1) / p.tile + 1, want = (num_sms * 64 + p.B - 1) / p.B;
     const dim3 grid(tiles < want ? tiles : want, p.B);
     const cudaError_t err = launch_pdl(rope_append_latent_kernel, grid, dim3(kThreads), 0, stream, p.pdl != 0, p);
     if (err != cudaSuccess) return err;
