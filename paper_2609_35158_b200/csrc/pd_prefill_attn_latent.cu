@@ -225,10 +225,9 @@ prefill_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_k, const __gri
                     n = p.q_indptr[b + 1] - from;
                     L = p.ctx_lens[b];
                 }
-                const bool real = z < p.B && n > 0;
-                L = min(max(L, 0), p.MP * kPageSize);
-                if (real && L < n && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);  // the cache must hold the new tokens
-                if (!real || L < n) n = 0;
+                const bool real = z < p.B && n > 0, fits = L >= n && L <= p.MP * kPageSize;  // the cache must hold the new tokens
+                if (real && !fits && blockIdx.x == 0) latch(p.status, kDevBadLength, b, L);
+                if (!real || !fits) n = L = 0;
                 if (SPLITS) {
                     // Few items: a context is cut where whole ones would leave SMs idle. In blocks of 1.0 to 1.5 us: a stretch costs about 4
                     // more, joining one about 1, and where there are more stretches than SMs the last ones end half a stretch late.
