@@ -459,18 +459,22 @@ def pd_decode_attn_latent(ctx, q, kv_pages, page_table, ctx_lens, out, lse=None,
            "pd_decode_attn_latent", ctx)
 
 
+def _pool_pages(k_pages, v_pages) -> int:
+    return k_pages.shape[0] if v_pages is None else min(k_pages.shape[0], v_pages.shape[0])
+
+
 def pd_kv_expand_latent(ctx, w_kv, kv_pages, page_table, first_token, ctx_lens, k_pages, v_pages, expanded_table, batch=None, stream=None):
-    """``first_token`` may be None (every sequence from its first token). The expanded pools' page count is ``k_pages.shape[0]``."""
+    """``first_token`` may be None (every sequence from its first token). The expanded pools' page count is that of the smaller one."""
     batch = ctx_lens.shape[0] if batch is None else batch
     _check(_lib.pd_kv_expand_latent(ctx, _ptr(w_kv), _ptr(kv_pages), _ptr(page_table), _optional_ptr(first_token, batch > 0, "first_token"),
-                                    _ptr(ctx_lens), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), k_pages.shape[0], batch,
+                                    _ptr(ctx_lens), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), _pool_pages(k_pages, v_pages), batch,
                                     _stream(stream)), "pd_kv_expand_latent", ctx)
 
 
 def pd_prefill_attn_latent(ctx, q, q_indptr, k_pages, v_pages, expanded_table, kv_pages, page_table, ctx_lens, out, lse=None, max_q_len=0,
                            batch=None, sm_scale=1.0, stream=None):
     batch = q_indptr.shape[0] - 1 if batch is None else batch
-    _check(_lib.pd_prefill_attn_latent(ctx, _ptr(q), _ptr(q_indptr), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), k_pages.shape[0],
+    _check(_lib.pd_prefill_attn_latent(ctx, _ptr(q), _ptr(q_indptr), _ptr(k_pages), _ptr(v_pages), _ptr(expanded_table), _pool_pages(k_pages, v_pages),
                                        _ptr(kv_pages), _ptr(page_table), _ptr(ctx_lens), _ptr(out),
                                        _optional_ptr(lse, batch > 0 and max_q_len > 0, "lse"), batch, max_q_len, sm_scale, _stream(stream)),
            "pd_prefill_attn_latent", ctx)
