@@ -380,7 +380,7 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
             const uint64_t policy = l2_policy_evict_first();
             const int32_t *row = nullptr;
             Walk w = w0;
-            Segment s;
+            Segment s{};
             int pc = 0, rc = 0, seg = 0;
             auto load_q = [&]() {
                 if (seg > 0) ok = mbar_wait(bar_qempty, (seg - 1) & 1);

@@ -51,6 +51,36 @@ def test_the_shapes_have_such_a_stretch():
 
 
 @pytest.mark.gpu
+def test_cut_contexts_replayed():
+    """A captured call and eager ones of the same context in turn: each counts its stretches afresh."""
+    heads, before, new = SHAPES[1]
+    lens, pages, table, to, k, v, q = turn(before, new, heads, 9)
+    args = [torch.from_numpy(np.ascontiguousarray(x, dtype=np.int32)).to(q.device) for x in (indptr_of(new), to, table, lens)]
+    out = torch.empty(q.shape[:2] + (128,), dtype=torch.bfloat16, device=q.device)
+    with Latent(heads, 1, table.shape[1], pages.shape[0]) as ctx:
+        want, _ = prefill(ctx, q, new, k, v, to, pages, table, lens)
+        few, _ = prefill(ctx, q, [33], k, v, to, pages, table, [5000])
+
+        def call():
+            ctx.pd.pd_prefill_attn_latent(ctx.h, q, args[0], k, v, args[1], pages, args[2], args[3], out, max_q_len=new[0], sm_scale=SCALE32)
+
+        call()
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+            call()
+        for i in range(5):
+            out.zero_()
+            g.replay()
+            if i % 2:
+                assert torch.equal(prefill(ctx, q, [33], k, v, to, pages, table, [5000])[0][:33], few[:33])
+            torch.cuda.synchronize()
+            assert torch.equal(out, want)
+        assert ctx.pd.pd_device_status(ctx.h)[0] == 0
+
+
+@pytest.mark.gpu
 @pytest.mark.parametrize("heads,before,new", SHAPES)
 def test_a_stretch_that_only_the_second_tile_sees(heads, before, new):
     """The first tile's barriers and parities are left alone in it, and what it contributes to the join is nothing."""
