@@ -28,8 +28,8 @@
 //
 // Bounds. 16 heads: memory, 64 contexts of 2K-16K in 110 us, 0.93 of the measured copy bandwidth (0.89 under load). 64 heads: a tile
 // keeps shared memory busy for 2612 cycles (1936 of operands, 576 of the copies' writes, P) and takes 2950; 64 contexts around 8K
-// take 149 us in a burst, 173 under load, where the power limit lowers the clock; 128 heads on 2K-16K 221 and 267 us, 795 and
-// 656 TFLOP/s.
+// take 149 to 156 us in a burst, 174 under load, where the power limit lowers the clock; 128 heads on 2K-16K 221 to 285 us in bursts, from
+// machine to machine, and 270 under load, 649 TFLOP/s.
 #include "pd_decode_plan.cuh"
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
@@ -725,8 +725,9 @@ decode_attn_latent_kernel(const __grid_constant__ CUtensorMap tm_kv, const __gri
 
 // Joins the partials of every (sequence, head) row whose sequence was cut, and writes the rows of empty sequences. A warp takes
 // VECS * 128 / GROUPS columns of a row: 32 / GROUPS lanes of VECS times 4 values each. Where rows are few and partials many, GROUPS sets of
-// lanes share the row's partials and join by shuffles. No shared memory and few registers, so that its blocks stand beside the
-// split kernel's on the same SM and wait there for its end.
+// lanes share the row's partials and join by shuffles. No shared memory, so that its blocks may stand beside the split kernel's on the same
+// SM and wait there for its end: those of <4, 1> (64 registers) beside any, those of <1, 4> (113) beside the kernels of up to 32 heads
+// a group alone; 64 heads leave 11,776 registers, and a block of it starts when one of theirs ends.
 constexpr int kMergeThreads = 128;
 template <int GROUPS, int VECS>
 __global__ void __launch_bounds__(kMergeThreads) latent_merge_kernel(const LatentAttnParams p) {

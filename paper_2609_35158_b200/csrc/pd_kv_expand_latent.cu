@@ -5,7 +5,7 @@
 // A unit is (two tiles of 128 tokens, head): 32 MMAs of 256 x 256 x 16 over a pair of CTAs (a cluster), a tile in each, 4096
 // cycles, for 256 KB of latents, 256 KB of W (from L2) and 128 KB of results. Each CTA holds half of W_h, K's rows in the first
 // and V's in the second, so W crosses from L2 once per 256 tokens. With a product per CTA (128 tokens) it crosses twice as often: 64 bytes
-// a cycle into each SM, and 82K tokens x 32 heads took 579 us, 393 of them without the stores of the results.
+// a cycle into each SM, and 76K tokens x 32 heads took 579 us, 393 of them without the stores of the results.
 // A pair walks a run of units, heads innermost: a tile's latents (8 blocks of 64 columns) stay in shared memory over its heads, W
 // streams through a ring of 16 KB blocks, and each block of the next tile is fetched as soon as the last head's product has
 // passed it. Two accumulators of 256 columns fill tensor memory, so the products of one unit run while the results of the last

@@ -11,19 +11,22 @@
 // products take 2560. With 80 columns of S and 40 of P beside them, S(j+1) waits only until the row threads hold the logits of
 // block j in registers, and runs during their softmax. What bounds it now is shared memory: an S product reads 4 KB of Q and
 // 2.5 KB of K in 51 cycles (128 bytes each), 1864 cycles a block with O, and the copies write 50 KB (400 cycles) beside that;
-// a block takes 2200. Eight turns, 9.6K new tokens on contexts of up to 18K, 32 heads: 1.79 to 1.83 ms, 1.22 PFLOP/s; under sustained load
-// the power limit lowers the clock.
+// a block takes 2200. Eight turns, 9.6K new tokens on contexts of up to 18K, 32 heads: 1.79 to 1.87 ms, 1.18 to 1.23 PFLOP/s; 2.14 ms under
+// sustained load, where the power limit lowers the clock.
+// Probabilities are rounded to bf16, as tcgen05 takes its 16-bit operands (off by at most 2^-8 of themselves); their sum is taken before.
+// Dividing by the sum of the rounded ones instead would take 1 % off the error (0.00224 from 0.00226, root of the mean squares) and costs 120
+// instructions a row and block behind the stores of P: 37.3 from 34.2 us on nine odd turns, 2250 from 2130 on eight long ones.
 // A page's 128 columns come as one box in the order [8-row group][64-column half][8 rows]: row groups follow one another
 // at the same distance across pages, as both operand forms want it.
 // Each tile has its own number of blocks: the first skips those that only the second one sees, and a turn of at most 128 tokens
 // runs one tile. Tensor memory: (S0 80, P0 40) (S1, P1) O0 O1, 128 columns each. Every wait is bounded.
 // Why a counter and not a block per item: the grid would have to be as wide as the longest turn for every sequence, and the next
 // item's queries, keys and values come in during the last one's softmax and stores. Two turns of 2048 among 62 single tokens, 32
-// heads: 235 us, 329 with a block per item; nine odd turns 34.0 from 36.6. The few more instructions of the walk cost long
+// heads: 233 us, 329 with a block per item; nine odd turns 34.0 from 36.6. The few more instructions of the walk cost long
 // turns 2 %.
 // Few tokens on a long context are few items: then an item is a stretch of the context, its unnormalised outputs go to the workspace in
 // fp32, and the warp that counts the last stretch of its 32 rows joins them in their order (the same bits in every call). 128 tokens on
-// 8000, 32 heads: 42 us, 95 whole; 512 on 30000, 8 heads: 90 and 464.
+// 8000, 32 heads: 43 us, 95 whole; 512 on 30000, 8 heads: 91 and 464.
 #include "pd_kernels.cuh"
 #include "pd_ptx.cuh"
 #include "pd_tcgen05.cuh"
