@@ -589,7 +589,8 @@ int pd_kv_expand_latent(pd_ctx *ctx, const void *w_kv, const void *kv_pages, con
  * pages and r from the latent pages, all of which hold the new tokens already (ctx_lens counts them). Results are
  * bit-reproducible; where a batch has few new tokens, long contexts are cut and the order of a row's sums depends on the whole
  * batch and on max_q_len. That rests on max_q_len: contexts are cut for at most 32 sequences with ceil(max_q_len / 256) * num_q_heads *
- * batch <= 2 * SMs, so a loose bound costs such a batch up to several times its time, no accuracy. A sequence whose length is below its new tokens or past the table is left out and latched.
+ * batch <= 2 * SMs, so a loose bound costs such a batch up to several times its time, no accuracy. A sequence whose length is below
+ * its new tokens or past the table is left out and latched.
  */
 int pd_prefill_attn_latent(pd_ctx *ctx, const void *q, const int32_t *q_indptr, const void *k_pages, const void *v_pages,
                            const int32_t *expanded_table, int64_t expanded_num_pages, const void *kv_pages, const int32_t *page_table,

@@ -19,8 +19,8 @@
 // m would be off by 2^-24 of itself, more than 2^x holds where logits are beyond 1e9. A head's reference m is the same for all
 // tokens; it is set from a segment's first tile and raised (with a rescale of O^T) only when a logit exceeds it by more
 // than 32 log2 units (P and the sums keep fp32's exponent range, so 2^32 costs no accuracy): a tile needs one vote and no
-// reduction over tokens. Where it is raised the tile's weights are formed again from its logits. P is rounded to bf16 (off by at most 2^-8 of itself: a second product for its remainder would make 128
-// heads a third slower); the sum that normalises the output adds the rounded values, lse takes the unrounded sum.
+// reduction over tokens. Where it is raised the tile's weights are formed again from its logits. P is rounded to bf16 (off by at most
+// 2^-8 of itself: a second product for its remainder would make 128 heads a third slower); the sum that normalises the output adds the rounded values, lse takes the unrounded sum.
 //
 // More than 64 heads go in groups: neighbouring CTAs read the same pages for different heads, the second one from L2.
 // A segment (the part of a range inside one sequence) that covers its sequence writes the result, any other an fp32 partial;
